@@ -227,6 +227,115 @@ int kv_quantize_pack_pt(const minikv_pt_shape *shape, const minikv_f16 *K, const
 int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, const minikv_pt_cache *cache,
                           float sm_scale, minikv_f16 *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Variant: a paged 8-BIT cache for batches whose requests come and go, and attention of packed prompts of
+ * different lengths -- what a serving loop needs around the calls above when its requests do not share one length.
+ * Four entry points, used in a row once per step: kv_assign_blk (blocks and slots), selective_flash_attn_packed
+ * (new prompts) or minikv_decode_attn_blk (one new token per request), kv_quantize_blk (filing of the new rows).
+ *
+ * The cache is a pool of n_blocks blocks of `block` tokens.  Block i of KV head h holds `block` rows of 128 codes
+ * in 8-bit floating point (e4m3: 4 exponent and 3 mantissa bits, largest value 448) for keys and as many for
+ * values, and ONE binary32 scale for each; a row stands for code * scale.  kv_quantize_blk makes every scale a
+ * power of two, so that a block whose scale grows later keeps its codes' bits (its rows are only rounded again
+ * where they become subnormal codes); the attention takes any finite non-negative scale.
+ * Request r owns the blocks table[r][0], table[r][1], ...; its token i is row i % block of block
+ * table[r][i / block], its SLOT is table[r][i / block] * block + i % block.  A block may stand in several tables
+ * (a shared prefix) as long as nothing is filed into it.
+ *
+ *   K, V    uint8 [n_blocks][Hkv][block][128]     Ks, Vs  float [n_blocks][Hkv]
+ *   table   int32 [R][max_blocks]                 q_len   int32 [R]   tokens held by each request
+ *   ring    int32 [n_blocks], ring_state int32 [2] = {head, n_free}: the free blocks are ring[(head + i) % n_blocks],
+ *           i < n_free.  At the start: ring = 0 .. n_blocks-1, head = 0, n_free = n_blocks.
+ *
+ * Rows of queries, keys, values and outputs are fp16 or bf16 (`dtype`).  Token t's heads lie side by side
+ * ([Hq or Hkv][128], contiguous), tokens are `stride` elements apart: a slice of a fused projection is taken as it is.
+ * Strides are multiples of 8 elements, at most 2^23, pointers 16-byte aligned.  Inputs must be finite.
+ * Shape rules: D == 128; block in {16, 32, 64, 128}; Hq % Hkv == 0 and Hq / Hkv <= 8; 1 <= R <= 8192; Hkv <= 65535;
+ * n_blocks * block and R * Hkv * (max_blocks * block / 64 + 1) < 2^31; max_blocks * block <= 2^30. */
+typedef enum { MINIKV_F16 = 0, MINIKV_BF16 = 1 } minikv_dtype;
+
+typedef struct minikv_blk_shape {
+    int32_t R, Hq, Hkv, D, block, n_blocks, max_blocks, dtype;
+} minikv_blk_shape;
+
+typedef struct minikv_blk_cache {
+    uint8_t *K, *V;
+    float   *Ks, *Vs;
+} minikv_blk_cache;
+
+/* Bytes of a buffer of the pool: MINIKV_BUF_KC (K), MINIKV_BUF_KS (Ks), MINIKV_BUF_VC (V), MINIKV_BUF_VS (Vs), 0 for any
+ * other and for an invalid shape; bytes of the workspace of minikv_decode_attn_blk. */
+size_t minikv_blk_cache_bytes(const minikv_blk_shape *shape, int which);
+size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
+
+/* Block tables and slot map of one step, from lengths that live on the device.  Request r wants n_new[r] more tokens
+ * (0: none; negative: the request is over).  In the order of the requests, those whose new blocks still fit get them:
+ *   need[r] = ceil((q_len[r] + n_new[r]) / block) - ceil(q_len[r] / block) blocks, 0 for a request that is over, that
+ *   would need more than max_blocks in all or whose tokens end behind slots[n_slots - 1]; it is ACCEPTED if none of
+ *   the last three holds and need[r] is 0 or need[0] + ... + need[r] <= n_free.
+ * An accepted request's new blocks are the next ones of the ring.  The blocks of a request that is over go back behind the
+ * ring's last one (they can be handed out from the next call on).
+ *   q_len, n_new      int32 [R]                                                   (device, read)
+ *   table             int32 [R][max_blocks]: the entries of new blocks            (device, read and written)
+ *   ring, ring_state  as above; only entries behind the last free block           (device, read; ring written)
+ *   q_len_next        int32 [R], not q_len: q_len + n_new if accepted, 0 if over, else q_len          (device, written)
+ *   ring_state_next   int32 [2], not ring_state                                    (device, written)
+ *   cu                int32 [R+1]: cu[r] = sum of max(n_new, 0) over the requests before r (at most 2^31 - 1): the rows
+ *                     of the packed step                                          (device, written)
+ *   slots             int32 [n_slots]: the slot of row cu[r] + i, that is of token q_len[r] + i of request r; -1 for
+ *                     the rows of a request that was not accepted and behind cu[R]  (device, written)
+ * The next step takes q_len_next and ring_state_next (swap the pointers: every workgroup reads the old ones).  Lengths
+ * outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside 0 .. n_blocks are clamped.  A table
+ * entry of a request that is over is put back as it is. */
+int kv_assign_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *n_new, int32_t *table,
+                  int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *ring_state_next, int32_t *cu,
+                  int32_t *slots, int32_t n_slots, void *stream);
+
+/* Files the rows of n_tok tokens at their slots.  For every block that gets rows, every KV head, and K and V each:
+ *   s = the smallest power of two (at least 2^-126) with max |x| <= 448 s over the new rows, 0 if they are all zero;
+ *   rows already there: if a new row goes to the block's offset 0 the block starts afresh (whatever scale and rows its last
+ *   use left do not count), else s becomes at least the block's scale, and where it is larger all the block's other rows are
+ *   re-expressed: code = e4m3_rne(code * old scale / s);
+ *   new rows: code = e4m3_rne(x / s) (round to nearest, ties to even, subnormal codes included), 0 if s is 0.
+ *   K, V    fp16 / bf16 [n_tok][Hkv][128], tokens k_stride, v_stride elements apart     (device, read)
+ *   slots   int32 [n_tok]; rows of one block stand together (as kv_assign_blk gives them); a slot outside
+ *           0 .. n_blocks * block - 1 (padding: -1) is skipped                            (device, read)
+ * Two rows of one call with the same slot, or rows of one block with others (or padding) between them, leave that block's
+ * contents unspecified.  Nothing else is touched. */
+int kv_quantize_blk(const minikv_blk_shape *shape, int32_t n_tok, const void *K, int64_t k_stride, const void *V,
+                    int64_t v_stride, const int32_t *slots, const minikv_blk_cache *cache, void *stream);
+
+/* out[r][hq] = softmax(sm_scale * q[r][hq] . K^T) . V over the q_len[r] tokens of request r that its table names, KV head
+ * hq / (Hq/Hkv), fp32 accumulation; one launch for all requests, whatever their lengths.  A request without tokens gives
+ * zeros.  Table entries outside 0 .. n_blocks-1 count as absent: their tokens contribute nothing.  Lengths are clamped
+ * to 0 .. max_blocks * block.  What lies behind a request's last token in its last block is not used, whatever it holds.
+ * The raw products q . codes are formed in binary32 and must not overflow there.
+ *   q      fp16 / bf16 [R][Hq][128], requests q_stride elements apart   (device, read)
+ *   out    fp16 / bf16 [R][Hq][128]                                     (device, written)
+ *   workspace  device scratch of at least minikv_blk_workspace_bytes(shape) bytes, 16-byte aligned, ZERO-FILLED ONCE after
+ *              allocation (every call returns its ticket counters to zero).  Calls of any shapes may take turns on one
+ *              workspace of sufficient size; two calls that share a workspace must be ordered (same stream). */
+int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t q_stride, const minikv_blk_cache *cache,
+                           const int32_t *table, const int32_t *q_len, float sm_scale, void *out, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* selective_flash_attn (below) for a batch of prompts of different lengths, packed one behind the other: prompt b is rows
+ * cu[b] .. cu[b+1]-1 of Q, K, V and X_O, and each attends to itself alone, causally.
+ *   B        prompts, 1 .. 8192; T rows in all (a host-side bound of cu[B]); max_len a host-side upper bound of every
+ *            prompt's length (sizes the launch): a longer prompt, or one that does not lie inside rows 0 .. T-1, is left
+ *            alone, as are the rows behind the last prompt.  A prompt of length 0 has no rows.
+ *   cu       int32 [B+1], non-decreasing                                          (device, read)
+ *   Q        fp16 / bf16 [T][Hq][128]; K, V [T][Hkv][128], tokens q_stride, k_stride, v_stride elements apart (device, read)
+ *   X_O      fp16 / bf16 [T][Hq][128], contiguous                                 (device, written)
+ *   lse, A_cumul  fp32 [T * Hq], A_cumul or NULL: the values of prompt b, of length n, are the n * Hq ones from cu[b] * Hq
+ *            on, a row of n for each query head -- what kv_select_hh_rw takes for that prompt as it is  (device, written)
+ * dtype a minikv_dtype, max_len <= 2^23, T * Hq < 2^31, strides <= 2^23, sm_scale finite and > 0.  T == 0 is no error and
+ * writes nothing. */
+int selective_flash_attn_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype,
+                                const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V,
+                                int64_t v_stride, const int32_t *cu, float sm_scale, void *X_O, float *lse,
+                                float *A_cumul, void *stream);
+
 /* Section 3.2 (selective flash attention) / Algorithm 1 line 2: causal attention of the prompt with itself that
  * also returns the cumulative attention score of every prompt token, in memory linear in L.  For batch b and
  * query head hq (reading KV head hq / (Hq/Hkv)), with P[i][j] = softmax_j(sm_scale * Q[i].K[j]) over j <= i:

@@ -37,6 +37,17 @@ class MinikvPtCache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in PT_BUF_NAMES]
 
 
+class MinikvBlkShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("R", "Hq", "Hkv", "D", "block", "n_blocks", "max_blocks", "dtype")]
+
+
+class MinikvBlkCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("K", "V", "Ks", "Vs")]
+
+
+DTYPES = {torch.float16: 0, torch.bfloat16: 1}         # minikv_dtype
+
+
 class MinikvError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -104,6 +115,20 @@ def lib():
                                            C.c_size_t, P]
         l.selective_flash_attn_workspace_bytes.restype = C.c_size_t
         l.selective_flash_attn_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int64]
+        S = C.POINTER(MinikvBlkShape)
+        l.minikv_blk_cache_bytes.restype = C.c_size_t
+        l.minikv_blk_cache_bytes.argtypes = [S, C.c_int]
+        l.minikv_blk_workspace_bytes.restype = C.c_size_t
+        l.minikv_blk_workspace_bytes.argtypes = [S]
+        l.kv_assign_blk.restype = C.c_int
+        l.kv_assign_blk.argtypes = [S, P, P, P, P, P, P, P, P, P, C.c_int32, P]
+        l.kv_quantize_blk.restype = C.c_int
+        l.kv_quantize_blk.argtypes = [S, C.c_int32, P, C.c_int64, P, C.c_int64, P, C.POINTER(MinikvBlkCache), P]
+        l.minikv_decode_attn_blk.restype = C.c_int
+        l.minikv_decode_attn_blk.argtypes = [S, P, C.c_int64, C.POINTER(MinikvBlkCache), P, P, C.c_float, P, P, C.c_size_t, P]
+        l.selective_flash_attn_packed.restype = C.c_int
+        l.selective_flash_attn_packed.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, P, C.c_int64,
+                                                  P, C.c_int64, P, C.c_int64, P, C.c_float, P, P, P, P]
         l.minikv_diag_redo_count.restype = C.c_int
         l.minikv_diag_redo_count.argtypes = [C.POINTER(MinikvShape), P, C.POINTER(C.c_int32)]
         l.minikv_stream_read_probe.restype = C.c_int
@@ -328,3 +353,103 @@ def minikv_decode_attn_pt(shape, q, cache, sm_scale, out, stream=None):
     ws = cache.workspace
     _check(lib().minikv_decode_attn_pt(C.byref(shape), _ptr(q), C.byref(cc), float(sm_scale), _ptr(out), _ptr(ws),
                                        ws.numel(), _stream(stream)), "minikv_decode_attn_pt")
+
+
+# ---------------------------------------------------------------------------------------------------------
+# paged 8-bit cache and packed prompts
+
+def _stride(x, heads):
+    """Elements between the tokens of x [tokens][heads][128], whose heads lie side by side."""
+    n, h, d = x.shape
+    t, s, one = x.stride()
+    if h != heads or d != 128 or one != 1 or (s != 128 and h > 1):
+        raise ValueError("rows are [tokens][%d][128] with the heads of a token side by side: got shape %s, strides %s"
+                         % (heads, tuple(x.shape), x.stride()))
+    return t if n > 1 else heads * 128                 # (one token: any stride will do)
+
+
+def _need(t, dtype, n, name):
+    """What a raw pointer does not tell the library: the type, and that n elements lie one behind the other."""
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s: a contiguous tensor of at least %d %s is needed, got %s of %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def make_blk_shape(R, Hq, Hkv, D, block, n_blocks, max_blocks, dtype):
+    """dtype: torch.float16 or torch.bfloat16, of queries, keys, values and outputs."""
+    return MinikvBlkShape(R, Hq, Hkv, D, block, n_blocks, max_blocks, DTYPES[dtype])
+
+
+class BlkCache:
+    """Caller-owned device buffers of one paged 8-bit cache, sized by minikv_blk_cache_bytes; given ones are taken as they are.
+    K, V: float8_e4m3fn [n_blocks][Hkv][block][128]; Ks, Vs: float32 [n_blocks][Hkv]; and the attention's workspace."""
+
+    def __init__(self, shape, device="cuda", K=None, V=None, Ks=None, Vs=None):
+        self.shape = shape
+        codes, scales = int(lib().minikv_blk_cache_bytes(C.byref(shape), 0)), int(lib().minikv_blk_cache_bytes(C.byref(shape), 1))
+        if not codes:
+            raise ValueError("invalid shape")
+        if K is not None:
+            device = K.device
+        rows = (shape.n_blocks, shape.Hkv)
+        e4m3 = torch.float8_e4m3fn
+        self.K = torch.zeros(rows + (shape.block, 128), dtype=torch.uint8, device=device).view(e4m3) if K is None else K
+        self.V = torch.zeros(rows + (shape.block, 128), dtype=torch.uint8, device=device).view(e4m3) if V is None else V
+        self.Ks = torch.zeros(rows, dtype=torch.float32, device=device) if Ks is None else Ks
+        self.Vs = torch.zeros(rows, dtype=torch.float32, device=device) if Vs is None else Vs
+        self._c = MinikvBlkCache(_need(self.K, e4m3, codes, "K"), _need(self.V, e4m3, codes, "V"),
+                                 _need(self.Ks, torch.float32, scales // 4, "Ks"), _need(self.Vs, torch.float32, scales // 4, "Vs"))
+        self.workspace = torch.zeros(int(lib().minikv_blk_workspace_bytes(C.byref(shape))), dtype=torch.uint8, device=device)   # zeroed once
+
+    def c(self):
+        return self._c
+
+
+def kv_assign_blk(shape, q_len, n_new, table, ring, ring_state, q_len_next, ring_state_next, cu, slots, stream=None):
+    i32, R = torch.int32, shape.R
+    _check(lib().kv_assign_blk(C.byref(shape), _need(q_len, i32, R, "q_len"), _need(n_new, i32, R, "n_new"),
+                               _need(table, i32, R * shape.max_blocks, "table"), _need(ring, i32, shape.n_blocks, "ring"),
+                               _need(ring_state, i32, 2, "ring_state"), _need(q_len_next, i32, R, "q_len_next"),
+                               _need(ring_state_next, i32, 2, "ring_state_next"), _need(cu, i32, R + 1, "cu"),
+                               _need(slots, i32, 0, "slots"), slots.numel(), _stream(stream)), "kv_assign_blk")
+
+
+def _rows(x, dtype, heads, name):
+    if DTYPES.get(x.dtype) != dtype:
+        raise ValueError("%s: got %s" % (name, x.dtype))
+    return x.data_ptr(), _stride(x, heads)
+
+
+def kv_quantize_blk(shape, K, V, slots, cache, stream=None):
+    """K, V: [tokens][Hkv][128], possibly slices of a fused projection; slots: one per token."""
+    n = K.shape[0]
+    if V.shape[0] != n:
+        raise ValueError("K has %d tokens, V %d" % (n, V.shape[0]))
+    (k, ks), (v, vs) = _rows(K, shape.dtype, shape.Hkv, "K"), _rows(V, shape.dtype, shape.Hkv, "V")
+    _check(lib().kv_quantize_blk(C.byref(shape), n, k, ks, v, vs, _need(slots, torch.int32, n, "slots"), C.byref(cache.c()),
+                                 _stream(stream)), "kv_quantize_blk")
+
+
+def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspace=None, stream=None):
+    """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous."""
+    (p, qs), ws = _rows(q, shape.dtype, shape.Hq, "q"), cache.workspace if workspace is None else workspace
+    if q.shape[0] < shape.R:
+        raise ValueError("q has %d rows, the shape %d requests" % (q.shape[0], shape.R))
+    _check(lib().minikv_decode_attn_blk(C.byref(shape), p, qs, C.byref(cache.c()),
+                                        _need(table, torch.int32, shape.R * shape.max_blocks, "table"),
+                                        _need(q_len, torch.int32, shape.R, "q_len"), float(sm_scale),
+                                        _need(out, q.dtype, shape.R * shape.Hq * 128, "out"), ws.data_ptr(),
+                                        ws.numel() * ws.element_size(), _stream(stream)), "minikv_decode_attn_blk")
+
+
+def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X_O, lse, A_cumul, stream=None):
+    """Q: [T][Hq][128], K, V: [T][Hkv][128], possibly slices of a fused projection; X_O: contiguous; A_cumul may be None."""
+    dtype = DTYPES[Q.dtype]
+    (q, qs), (k, ks), (v, vs) = _rows(Q, dtype, Hq, "Q"), _rows(K, dtype, Hkv, "K"), _rows(V, dtype, Hkv, "V")
+    if min(Q.shape[0], K.shape[0], V.shape[0]) < T:
+        raise ValueError("fewer than %d rows" % T)
+    _check(lib().selective_flash_attn_packed(int(B), int(Hq), int(Hkv), int(T), int(max_len), dtype, q, qs, k, ks, v, vs,
+                                             _need(cu, torch.int32, B + 1, "cu"), float(sm_scale),
+                                             _need(X_O, Q.dtype, T * Hq * 128, "X_O"), _need(lse, torch.float32, T * Hq, "lse"),
+                                             None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul"),
+                                             _stream(stream)), "selective_flash_attn_packed")

@@ -16,7 +16,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libminikv.so")
 
 SOURCES = ["api.hip", "quantize.hip", "decode_scalar.hip", "decode_tiled.hip", "decode_static.hip", "select.hip",
-           "prefill_attn.hip", "pt.hip"]
+           "prefill_attn.hip", "pt.hip", "blocks.hip", "decode_blk.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

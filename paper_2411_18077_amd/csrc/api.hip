@@ -47,6 +47,34 @@ int validate_cache(const minikv_shape &s, const minikv_cache *c)
     return MINIKV_OK;
 }
 
+static bool aligned4(const void *p) { return p && ((uintptr_t)p & 3u) == 0; }
+
+static int validate_blk(const minikv_blk_shape *s)
+{
+    if (!s) return MINIKV_EINVAL;
+    if (s->D != kD) return MINIKV_EUNSUPPORTED;
+    if (!(s->block == 16 || s->block == 32 || s->block == 64 || s->block == 128)) return MINIKV_EUNSUPPORTED;
+    if (s->dtype != MINIKV_F16 && s->dtype != MINIKV_BF16) return MINIKV_EUNSUPPORTED;
+    if (s->R < 1 || s->R > kMaxRequests || s->Hq < 1 || s->Hkv < 1 || s->Hkv > 65535 || s->Hq % s->Hkv) return MINIKV_EINVAL;
+    if (s->Hq / s->Hkv > kMaxRep) return MINIKV_EUNSUPPORTED;
+    if (s->n_blocks < 1 || s->max_blocks < 1) return MINIKV_EINVAL;
+    const int64_t most = (int64_t)s->max_blocks * s->block;                            // tokens of a request
+    if ((int64_t)s->n_blocks * s->block > 0x7fffffff || most > (1 << 30)) return MINIKV_EINVAL;
+    if ((int64_t)s->R * s->Hkv > 0x7fffffff / (most / kBlkTile + 1)) return MINIKV_EINVAL;
+    return MINIKV_OK;
+}
+
+static bool valid_blk_cache(const minikv_blk_cache *c)
+{
+    return c && aligned16(c->K) && aligned16(c->V) && aligned4(c->Ks) && aligned4(c->Vs);
+}
+
+// rows of `heads` x 128 elements, 16-byte loads; a stride is far below where an offset inside a tile of rows would leave 32 bits
+static bool valid_stride(int64_t stride, int32_t heads)
+{
+    return stride >= (int64_t)heads * kD && stride % 8 == 0 && stride <= (1 << 23);
+}
+
 // Reference point for the bandwidth figures: reads a buffer once with 128-bit loads, 2048 workgroups striding
 // through it, and folds it into one word per workgroup (so that the loads cannot be dropped).
 __global__ __launch_bounds__(256) void stream_read_kernel(const uint4 *__restrict__ src, size_t n16,
@@ -81,7 +109,7 @@ const char *minikv_strerror(int status)
     switch (status) {
     case MINIKV_OK: return "ok";
     case MINIKV_EINVAL: return "invalid argument (null or misaligned pointer, or a shape rule violated)";
-    case MINIKV_EUNSUPPORTED: return "unsupported shape (D must be 128, G in {16,32,64,128}, Hq/Hkv <= 8)";
+    case MINIKV_EUNSUPPORTED: return "unsupported shape (D must be 128, G or block in {16,32,64,128}, Hq/Hkv <= 8, a known dtype)";
     case MINIKV_EWORKSPACE: return "workspace too small (see minikv_workspace_bytes)";
     case MINIKV_ELAUNCH: return "HIP launch failed";
     default: return "unknown status";
@@ -186,6 +214,66 @@ int minikv_decode_step(const minikv_shape *s, const minikv_f16 *q, const minikv_
     return launch_decode(*s, q, *c, sm_scale, out, workspace, 0, (hipStream_t)stream, &ap);
 }
 
+size_t minikv_blk_cache_bytes(const minikv_blk_shape *s, int which)
+{
+    if (validate_blk(s) != MINIKV_OK) return 0;
+    const size_t rows = (size_t)s->n_blocks * s->Hkv;
+    switch (which) {
+    case MINIKV_BUF_KC:
+    case MINIKV_BUF_VC: return rows * s->block * kD;
+    case MINIKV_BUF_KS:
+    case MINIKV_BUF_VS: return rows * sizeof(float);
+    default: return 0;
+    }
+}
+
+size_t minikv_blk_workspace_bytes(const minikv_blk_shape *s)
+{
+    if (validate_blk(s) != MINIKV_OK) return 0;
+    // a ticket counter and two partials per workgroup, at the same places for every shape
+    return (size_t)kBlkGroups * (sizeof(int) + 2 * kBlkPartial * sizeof(float));
+}
+
+int kv_assign_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *n_new, int32_t *table, int32_t *ring,
+                  const int32_t *ring_state, int32_t *q_len_next, int32_t *ring_state_next, int32_t *cu, int32_t *slots,
+                  int32_t n_slots, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (!aligned4(q_len) || !aligned4(n_new) || !aligned4(table) || !aligned4(ring) || !aligned4(ring_state) ||
+        !aligned4(q_len_next) || !aligned4(ring_state_next) || !aligned4(cu) || n_slots < 0 || (n_slots && !aligned4(slots)))
+        return MINIKV_EINVAL;
+    if (q_len_next == q_len || q_len_next == n_new || ring_state_next == ring_state) return MINIKV_EINVAL;
+    return launch_assign_blk(*s, q_len, n_new, table, ring, ring_state, q_len_next, ring_state_next, cu, slots, n_slots,
+                             (hipStream_t)stream);
+}
+
+int kv_quantize_blk(const minikv_blk_shape *s, int32_t n_tok, const void *K, int64_t k_stride, const void *V, int64_t v_stride,
+                    const int32_t *slots, const minikv_blk_cache *c, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (n_tok < 0 || !valid_blk_cache(c)) return MINIKV_EINVAL;
+    if (n_tok == 0) return MINIKV_OK;
+    if (!aligned16(K) || !aligned16(V) || !aligned4(slots)) return MINIKV_EINVAL;
+    if (!valid_stride(k_stride, s->Hkv) || !valid_stride(v_stride, s->Hkv)) return MINIKV_EINVAL;
+    return launch_quantize_blk(*s, n_tok, K, k_stride, V, v_stride, slots, *c, (hipStream_t)stream);
+}
+
+int minikv_decode_attn_blk(const minikv_blk_shape *s, const void *q, int64_t q_stride, const minikv_blk_cache *c,
+                           const int32_t *table, const int32_t *q_len, float sm_scale, void *out, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (!valid_blk_cache(c) || !aligned16(q) || !aligned16(out) || !aligned16(workspace) || !aligned4(table) || !aligned4(q_len))
+        return MINIKV_EINVAL;
+    if (!valid_stride(q_stride, s->Hq)) return MINIKV_EINVAL;
+    if (sm_scale - sm_scale != 0.0f) return MINIKV_EINVAL;                             // NaN / Inf
+    if (workspace_bytes < minikv_blk_workspace_bytes(s)) return MINIKV_EWORKSPACE;
+    return launch_decode_blk(*s, q, q_stride, *c, table, q_len, sm_scale, out, workspace, (hipStream_t)stream);
+}
+
 size_t selective_flash_attn_workspace_bytes(int32_t B, int32_t Hkv, int64_t L)
 {
     if (B <= 0 || Hkv <= 0 || L < 1) return 0;
@@ -204,6 +292,22 @@ int selective_flash_attn(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const mi
     if ((int64_t)B * Hq * ((L + 127) / 128) > 0x7fffffff || (int64_t)B * Hkv > 65535) return MINIKV_EINVAL;
     if (workspace_bytes < selective_flash_attn_workspace_bytes(B, Hkv, L)) return MINIKV_EWORKSPACE;
     return launch_prefill(B, Hq, Hkv, L, Q, K, V, sm_scale, X_O, lse, A_cumul, (hipStream_t)stream);
+}
+
+int selective_flash_attn_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype, const void *Q,
+                                int64_t q_stride, const void *K, int64_t k_stride, const void *V, int64_t v_stride,
+                                const int32_t *cu, float sm_scale, void *X_O, float *lse, float *A_cumul, void *stream)
+{
+    if (B < 1 || B > kMaxRequests || Hq <= 0 || Hkv <= 0 || Hq % Hkv || T < 0 || max_len < 0 || max_len > (1 << 23)) return MINIKV_EINVAL;
+    if (dtype != MINIKV_F16 && dtype != MINIKV_BF16) return MINIKV_EUNSUPPORTED;
+    if ((int64_t)T * Hq > 0x7fffffff) return MINIKV_EINVAL;
+    if (!(sm_scale > 0.0f) || sm_scale - sm_scale != 0.0f) return MINIKV_EINVAL;       // positive and finite
+    if (!valid_stride(q_stride, Hq) || !valid_stride(k_stride, Hkv) || !valid_stride(v_stride, Hkv)) return MINIKV_EINVAL;
+    if (T == 0 || max_len == 0) return MINIKV_OK;                                      // no rows (a null pointer is one of an empty tensor)
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(X_O) || !aligned4(lse) || !aligned4(cu)) return MINIKV_EINVAL;
+    if (A_cumul && !aligned4(A_cumul)) return MINIKV_EINVAL;
+    return launch_prefill_packed(B, Hq, Hkv, T, max_len, dtype, Q, q_stride, K, k_stride, V, v_stride, cu, sm_scale, X_O, lse, A_cumul,
+                                 (hipStream_t)stream);
 }
 
 size_t kv_select_workspace_bytes(int32_t units, int32_t rep, int64_t L)

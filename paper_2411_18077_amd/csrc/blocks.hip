@@ -1,0 +1,308 @@
+// The paged 8-bit cache: block tables and slot maps from lengths on the device (kv_assign_blk), and the filing of new rows
+// as e4m3 codes with one power-of-two scale per (block, head) (kv_quantize_blk).  See include/minikv.h for what they compute.
+#include "common.h"
+
+namespace minikv {
+
+// =====================================================================================================================
+// kv_assign_blk
+
+struct AssignArgs {
+    const int32_t *q_len, *n_new, *state;
+    int32_t *table, *ring, *q_len_next, *state_next, *cu, *slots;
+    int R, N, width, shift, n_slots;
+};
+
+constexpr int kAsThreads = 256;
+constexpr int kAsRun = 4;                              // consecutive slots a thread looks up at once
+constexpr uint32_t kRefused = 0x80000000u;
+
+// Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap < 2^31;
+// min(a + b, cap) is associative, so a scan in any order gives the same.)
+__device__ inline uint32_t sat_add(uint32_t a, uint32_t b, uint32_t cap) { return min(a + b, cap); }
+
+// exclusive scan over the workgroup's threads; `total` receives the whole sum
+__device__ inline uint32_t block_scan(uint32_t v, uint32_t cap, uint32_t *part, uint32_t &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t in = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(in, d, 64);
+        if (lane >= d) in = sat_add(in, o, cap);
+    }
+    if (lane == 63) part[wave] = in;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kAsThreads / 64; ++w) {
+        if (w == wave) before = all;
+        all = sat_add(all, part[w], cap);
+    }
+    total = all;
+    uint32_t ex = __shfl_up(in, 1, 64);
+    if (lane == 0) ex = 0;
+    __syncthreads();
+    return sat_add(before, ex, cap);
+}
+
+// last i in [0, n) with (v[i] without its top bit) <= x; v ascends, v[0] = 0
+__device__ inline int find(const uint32_t *v, int n, uint32_t x)
+{
+    int lo = 0;
+    for (int step = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0; step; step >>= 1)
+        if (lo + step < n && (v[lo + step] & ~kRefused) <= x) lo += step;
+    return lo;
+}
+
+// Every workgroup scans all the requests (two scans: rows first, because a request whose rows do not fit asks for no blocks)
+// and keeps three prefix sums in local memory; after that slots, table entries and returned blocks are three flat loops over
+// the grid, each element finding its request by bisection.  New slots are computed from the ring, not from the table entries
+// that another workgroup may not have written yet, so one launch does it all and nothing waits for anything.  What bounds
+// it is latency: two dependent loads and the scans.
+__global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
+{
+    extern __shared__ uint32_t lds[];
+    uint32_t *rows = lds, *need = lds + a.R, *over = lds + 2 * a.R;     // exclusive prefix sums per request
+    __shared__ uint32_t part[kAsThreads / 64], popped;
+    const int tid = threadIdx.x, gtid = blockIdx.x * kAsThreads + tid, gsize = gridDim.x * kAsThreads;
+    const int64_t most = (int64_t)a.width << a.shift;
+    const int head = min(max(a.state[0], 0), a.N - 1), n_free = min(max(a.state[1], 0), a.N);
+    const uint32_t kRows = 0x7fffffff, back = a.N - n_free;            // blocks that can come back
+
+    auto len_of = [&](int r) { return (int)min((int64_t)max(a.q_len[r], 0), most); };
+    auto blocks = [&](int64_t tokens) { return (int64_t)((tokens + (1 << a.shift) - 1) >> a.shift); };
+
+    const int per = (a.R + kAsThreads - 1) / kAsThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+    if (tid == 0) popped = 0;
+    uint32_t sum = 0, total_rows, total_need, total_over;
+    for (int r = r0; r < r1; ++r) sum = sat_add(sum, max(a.n_new[r], 0), kRows);
+    uint32_t row = block_scan(sum, kRows, part, total_rows);
+    uint32_t sum_need = 0, sum_over = 0;
+    for (int r = r0; r < r1; ++r) {                    // (need <= new rows <= n_slots in all: no overflow)
+        const int len = len_of(r), add = a.n_new[r];
+        const uint32_t end = sat_add(row, max(add, 0), kRows);
+        const int64_t after = blocks((int64_t)len + max(add, 0));
+        const bool fits = add >= 0 && after <= a.width && end <= (uint32_t)a.n_slots;
+        const uint32_t nd = fits ? (uint32_t)(after - blocks(len)) : 0u;
+        rows[r] = row, need[r] = nd | (fits ? 0u : kRefused);
+        over[r] = add < 0 ? (uint32_t)min(blocks(len), (int64_t)back) : 0u;
+        sum_need += nd, sum_over = sat_add(sum_over, over[r], back);
+        row = end;
+    }
+    uint32_t at_need = block_scan(sum_need, kRows, part, total_need), at_over = block_scan(sum_over, back, part, total_over);
+    for (int r = r0; r < r1; ++r) {
+        const uint32_t nd = need[r] & ~kRefused, end = at_need + nd, ov = over[r];
+        const bool ok = !(need[r] & kRefused) && (nd == 0 || end <= (uint32_t)n_free);
+        if (ok && nd) atomicMax(&popped, end);         // (ascending in the accepted ones)
+        need[r] = at_need | (ok ? 0u : kRefused), over[r] = at_over;
+        at_need = end, at_over = sat_add(at_over, ov, back);
+        if (blockIdx.x == 0) {
+            const int len = len_of(r), add = a.n_new[r];
+            a.q_len_next[r] = add < 0 ? 0 : ok ? len + add : len;
+            a.cu[r] = (int)rows[r];
+        }
+    }
+    __syncthreads();
+    const uint32_t pop = popped;
+    auto wrap = [&](uint32_t i) { return i >= (uint32_t)a.N ? i - a.N : i; };          // i < 2 N
+    if (blockIdx.x == 0 && tid == 0) {
+        a.cu[a.R] = (int)total_rows;
+        a.state_next[0] = (int)wrap(head + pop), a.state_next[1] = n_free - (int)pop + (int)total_over;
+    }
+    for (int t0 = gtid * kAsRun; t0 < a.n_slots; t0 += gsize * kAsRun) {
+        int r = find(rows, a.R, t0);
+#pragma unroll
+        for (int k = 0; k < kAsRun; ++k) {
+            const int t = t0 + k;
+            if (t >= a.n_slots) break;
+            while (r + 1 < a.R && rows[r + 1] <= (uint32_t)t) ++r;
+            int slot = -1;
+            if ((uint32_t)t < total_rows && !(need[r] & kRefused)) {
+                const int len = len_of(r), pos = len + (t - (int)rows[r]);
+                const int b = pos >> a.shift, held = (int)blocks(len);
+                const int id = b < held ? a.table[(int64_t)r * a.width + b] : a.ring[wrap(head + need[r] + (b - held))];
+                slot = (id << a.shift) + (pos & ((1 << a.shift) - 1));
+            }
+            a.slots[t] = slot;
+        }
+    }
+    for (uint32_t p = gtid; p < pop; p += gsize) {
+        const int r = find(need, a.R, p);
+        a.table[(int64_t)r * a.width + blocks(len_of(r)) + (p - need[r])] = a.ring[wrap(head + p)];
+    }
+    for (uint32_t p = gtid; p < total_over; p += gsize) {
+        const int r = find(over, a.R, p);
+        a.ring[wrap(wrap(head + n_free) + p)] = a.table[(int64_t)r * a.width + (p - over[r])];
+    }
+}
+
+int launch_assign_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *n_new, int32_t *table, int32_t *ring,
+                      const int32_t *state, int32_t *q_len_next, int32_t *state_next, int32_t *cu, int32_t *slots,
+                      int32_t n_slots, hipStream_t st)
+{
+    AssignArgs a;
+    a.q_len = q_len, a.n_new = n_new, a.state = state, a.table = table, a.ring = ring;
+    a.q_len_next = q_len_next, a.state_next = state_next, a.cu = cu, a.slots = slots;
+    a.R = s.R, a.N = s.n_blocks, a.width = s.max_blocks, a.shift = __builtin_ctz(s.block), a.n_slots = n_slots;
+    const int64_t grid = ((int64_t)n_slots + kAsThreads * kAsRun - 1) / (kAsThreads * kAsRun);
+    hipLaunchKernelGGL(assign_blk_kernel, dim3((unsigned)(grid < 1 ? 1 : grid < kComputeUnits ? grid : kComputeUnits)),
+                       dim3(kAsThreads), 3 * s.R * sizeof(uint32_t), st, a);
+    return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
+}
+
+// =====================================================================================================================
+// kv_quantize_blk
+
+typedef float float2v __attribute__((ext_vector_type(2)));
+
+struct FileArgs {
+    const uint16_t *X[2];                              // K and V rows
+    int64_t stride[2];
+    uint8_t *codes[2];
+    float *scales[2];
+    const int32_t *slots;
+    int n_tok, Hkv, shift, rows;                       // rows = n_blocks * block
+};
+
+__device__ inline uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
+}
+template <bool BF16> __device__ inline float from16(uint32_t bits)
+{
+    if (BF16) return __uint_as_float(bits << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+
+// The smallest power of two s >= 2^-126 with amax <= 448 s: 448 = 1.75 * 2^8, so from the exponent of amax alone, one more
+// where its mantissa is beyond 1.75.
+__device__ inline float scale_for(float amax)
+{
+    if (amax == 0.0f) return 0.0f;
+    const uint32_t bits = __float_as_uint(amax);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000);
+    return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
+}
+
+// A wave takes the runs (consecutive tokens of one block) that begin among its CHUNK tokens, for one head and one of K
+// and V, so that a block's scale has one owner and no barrier or atomic is needed.  Sixteen lanes hold a row, four rows an
+// instruction; up to 64 rows stay in registers between the maximum (on the 16-bit magnitudes, whose order is that of the
+// unsigned integers for fp16 and bf16 alike) and the rounding, more are read again.
+template <int CHUNK, bool BF16>
+__global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, sub = lane >> 4;
+    const int first = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * CHUNK;
+    const int h = blockIdx.y, which = blockIdx.z;
+    if (first >= a.n_tok) return;
+    const uint16_t *X = a.X[which] + (int64_t)h * kD + c * 8;
+    const int64_t stride = a.stride[which];
+    auto block_of = [&](int i) {                       // block of token i, -1: none
+        const int slot = a.slots[i];
+        return (uint32_t)slot < (uint32_t)a.rows ? slot >> a.shift : -1;
+    };
+    bool begins = false;
+    if (lane < CHUNK && first + lane < a.n_tok) {
+        const int b = block_of(first + lane);
+        begins = b >= 0 && (first + lane == 0 || block_of(first + lane - 1) != b);
+    }
+    for (uint64_t todo = __ballot(begins); todo; todo &= todo - 1) {
+        const int i = first + __builtin_ctzll(todo), blk = __builtin_amdgcn_readfirstlane(block_of(i));
+        int n = 0;                                     // rows of the run
+        bool fresh = false;                            // one of them is the block's first
+        for (uint64_t same = ~0ull; same == ~0ull; n += same == ~0ull ? 64 : __builtin_ctzll(~same)) {
+            const int j = i + n + lane, slot = j < a.n_tok ? a.slots[j] : -1;
+            const bool mine = (uint32_t)slot < (uint32_t)a.rows && slot >> a.shift == blk;
+            same = __ballot(mine);
+            const uint64_t run = same == ~0ull ? ~0ull : (1ull << __builtin_ctzll(~same)) - 1;
+            fresh |= (__ballot(mine && (slot & ((1 << a.shift) - 1)) == 0) & run) != 0;
+        }
+        uint4 x[16];
+        auto load = [&](int base) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (base + 4 * k < n) x[k] = *(const uint4 *)(X + (int64_t)(i + min(base + 4 * k + sub, n - 1)) * stride);
+        };
+        uint32_t mx = 0;
+        for (int base = 0; base < n; base += 64) {
+            load(base);
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (base + 4 * k < n) {
+                    const uint32_t lo = max_u16x2(x[k].x & 0x7fff7fff, x[k].y & 0x7fff7fff);
+                    const uint32_t hi = max_u16x2(x[k].z & 0x7fff7fff, x[k].w & 0x7fff7fff);
+                    mx = max_u16x2(mx, max_u16x2(lo, hi));
+                }
+        }
+        mx = max(mx & 0xffff, mx >> 16);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, d, 64));
+        const int64_t at = (int64_t)blk * a.Hkv + h;
+        float *scale = a.scales[which] + at;
+        uint8_t *codes = a.codes[which] + ((at << a.shift) * kD);
+        float s = scale_for(from16<BF16>(mx));
+        if (!fresh) {
+            const float old = *scale;
+            if (old > s) s = old;
+            if (s != old) {                            // every row of the block under the new scale
+                const float ratio = old / s;
+                for (int k = lane; k < (8 << a.shift); k += 64) {
+                    uint4 w = ((const uint4 *)codes)[k];
+                    uint32_t *p = &w.x;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(p[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(p[j], true);
+                        int v = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * ratio, lo[1] * ratio, 0, false);
+                        p[j] = __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * ratio, hi[1] * ratio, v, true);
+                    }
+                    ((uint4 *)codes)[k] = w;
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // before the new rows go to places among them
+            }
+        }
+        const float inv = s > 0.0f ? 1.0f / s : 0.0f;
+        for (int base = 0; base < n; base += 64) {
+            if (n > 64) load(base);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int row = base + 4 * k + sub;
+                if (base + 4 * k < n && row < n) {
+                    const uint32_t *p = &x[k].x;
+                    int v[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t lo = p[2 * j], hi = p[2 * j + 1];
+                        v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(lo & 0xffff) * inv, from16<BF16>(lo >> 16) * inv, 0, false);
+                        v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(hi & 0xffff) * inv, from16<BF16>(hi >> 16) * inv, v[j], true);
+                    }
+                    const int off = a.slots[i + row] & ((1 << a.shift) - 1);
+                    *(int2 *)(codes + off * kD + c * 8) = int2{v[0], v[1]};
+                }
+            }
+        }
+        if (lane == 0) *scale = s;
+    }
+}
+
+int launch_quantize_blk(const minikv_blk_shape &s, int32_t n_tok, const void *K, int64_t k_stride, const void *V,
+                        int64_t v_stride, const int32_t *slots, const minikv_blk_cache &c, hipStream_t st)
+{
+    FileArgs a;
+    a.X[0] = (const uint16_t *)K, a.X[1] = (const uint16_t *)V, a.stride[0] = k_stride, a.stride[1] = v_stride;
+    a.codes[0] = c.K, a.codes[1] = c.V, a.scales[0] = c.Ks, a.scales[1] = c.Vs, a.slots = slots;
+    a.n_tok = n_tok, a.Hkv = s.Hkv, a.shift = __builtin_ctz(s.block), a.rows = s.n_blocks * s.block;
+    // A wave per token while that is what the compute units can hold at once (a step of single tokens, each a run of its
+    // own); else a wave per 16 tokens, the smallest block, most of them with at most one run to begin.
+    const bool single = (int64_t)n_tok * s.Hkv * 2 <= 16 * 4 * kComputeUnits;
+    const int chunk = single ? 1 : 16;
+    const dim3 grid((unsigned)(((int64_t)n_tok + 4 * chunk - 1) / (4 * chunk)), (unsigned)s.Hkv, 2);
+    if (single && s.dtype == MINIKV_BF16) hipLaunchKernelGGL((quantize_blk_kernel<1, true>), grid, dim3(256), 0, st, a);
+    else if (single) hipLaunchKernelGGL((quantize_blk_kernel<1, false>), grid, dim3(256), 0, st, a);
+    else if (s.dtype == MINIKV_BF16) hipLaunchKernelGGL((quantize_blk_kernel<16, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((quantize_blk_kernel<16, false>), grid, dim3(256), 0, st, a);
+    return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
+}
+
+}  // namespace minikv

@@ -97,8 +97,24 @@ int launch_decode_parts(const minikv_shape &s, const minikv_f16 *q, const minikv
 int validate_cache(const minikv_shape &s, const minikv_cache *c);
 bool aligned16(const void *p);
 
+// the paged 8-bit cache
+constexpr int kMaxRequests = 8192;   // a workgroup holds a few words per request in local memory
+constexpr int kBlkTile = 64;         // tokens a wave of the attention takes at once
+constexpr int kBlkGroups = 512;      // most workgroups of the attention: two per compute unit
+constexpr int kBlkPartial = kMaxRep * (kD + 2);      // floats of a workgroup's partial: m and l of each head, then o
+int launch_assign_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *n_new, int32_t *table, int32_t *ring,
+                      const int32_t *state, int32_t *q_len_next, int32_t *state_next, int32_t *cu, int32_t *slots,
+                      int32_t n_slots, hipStream_t st);
+int launch_quantize_blk(const minikv_blk_shape &s, int32_t n_tok, const void *K, int64_t k_stride, const void *V,
+                        int64_t v_stride, const int32_t *slots, const minikv_blk_cache &c, hipStream_t st);
+int launch_decode_blk(const minikv_blk_shape &s, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
+                      const int32_t *q_len, float sm_scale, void *out, void *workspace, hipStream_t st);
+
 int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f16 *Q, const minikv_f16 *K,
                    const minikv_f16 *V, float sm_scale, minikv_f16 *XO, float *lse, float *A_cumul, hipStream_t st);
+int launch_prefill_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype, const void *Q,
+                          int64_t q_stride, const void *K, int64_t k_stride, const void *V, int64_t v_stride, const int32_t *cu,
+                          float sm_scale, void *XO, float *lse, float *A_cumul, hipStream_t st);
 size_t select_workspace_bytes(int32_t units, int32_t rep, int64_t L);
 bool set_decode_weights(int mode); // 0 = by shape, 1 = the work line, 2 = the work line with unit weights
 bool set_select_path(int path);   // 0 = by shape, 1 = one workgroup per unit, 2 = several (when the prompt allows)

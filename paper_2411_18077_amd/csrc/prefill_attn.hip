@@ -38,11 +38,91 @@ struct PrefillArgs {
     int Hq, rep, nblk;
     long L;
     float scale_log2;                // sm_scale * log2(e): the softmax runs on powers of two
+    // packed prompts (PACKED instances only): prompt b is rows cu[b] .. cu[b+1]-1 of T, tokens *_pitch bytes apart
+    const int32_t *cu;
+    int B, T, max_len;
+    unsigned q_pitch, k_pitch, v_pitch;
 };
 
+// 16-bit operands are kept as halves whatever they are; BF16 instances differ in the product and in the two roundings.
+typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
+
+template <bool BF16 = false>
 __device__ __forceinline__ float16v mfma32(half8 a, half8 b, float16v c)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    if constexpr (BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bfloat8, a), __builtin_bit_cast(bfloat8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+template <bool BF16>
+__device__ __forceinline__ _Float16 to16(float v)
+{
+    if constexpr (BF16) return __builtin_bit_cast(_Float16, (__bf16)v);
+    else return (_Float16)v;
+}
+
+// Packed prompts: which row block of which prompt a workgroup takes.  The blocks of all prompts are dealt in the order of
+// what they cost (HEAVY_LAST: row blocks, whose last ones see the most keys; else column blocks, whose first ones are
+// seen by the most queries): with `level` the number of blocks of the prompt behind it, counted from the heavy end, the r-th block is
+// found by bisection over the level, of which the number of blocks at or beyond is a sum over the prompts.  Each wave
+// does that for itself with the prompts' block counts in local memory (which tiles overwrite: a barrier follows).
+struct PackedBlock {
+    int first, L, index;             // first row and length of the prompt (length 0: no block is left), block inside it
+};
+__device__ __forceinline__ int wave_sum(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return __builtin_amdgcn_readlane(v, 63);
+}
+template <int ROWS, bool HEAVY_LAST>
+__device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int rank, int *counts)
+{
+    const int lane = threadIdx.x & 63;
+    auto length = [&](int b) {                         // 0: no prompt, or one to be left alone
+        const int at = a.cu[b], end = a.cu[b + 1];
+        return at >= 0 && end > at && end <= a.T && end - at <= a.max_len ? end - at : 0;
+    };
+    int one = 0, levels = (a.max_len + ROWS - 1) / ROWS;
+    if (a.B <= 64) {
+        one = lane < a.B ? (length(lane) + ROWS - 1) / ROWS : 0;
+    } else {
+        for (int b = lane; b < a.B; b += 64) counts[b] = (length(b) + ROWS - 1) / ROWS;
+    }
+    auto beyond = [&](int q) {                         // blocks with at least q others behind them, seen from the heavy end
+        int sum = 0;
+        if (a.B <= 64) sum = max(one - q, 0);
+        else for (int b = lane; b < a.B; b += 64) sum += max(counts[b] - q, 0);
+        return wave_sum(sum);
+    };
+    PackedBlock p{0, 0, 0};
+    if (rank < beyond(0)) {
+        int lo = 0;                                    // the largest level with more than `rank` blocks at or beyond it
+        for (int step = levels > 1 ? 1 << (31 - __builtin_clz(levels - 1)) : 0; step; step >>= 1)
+            if (lo + step < levels && beyond(lo + step) > rank) lo += step;
+        int left = rank - beyond(lo + 1), b = 0;       // the left-th of the prompts with a block on this level
+        for (;; b += 64) {
+            const uint64_t has = __ballot((a.B <= 64 ? one : b + lane < a.B ? counts[b + lane] : 0) > lo);
+            const int n = __builtin_popcountll(has);
+            if (left < n) {
+                const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+                b += __builtin_ctzll(__ballot((has >> lane & 1) && before == left));
+                break;
+            }
+            left -= n;
+        }
+        p.first = a.cu[b], p.L = length(b);
+        p.index = HEAVY_LAST ? lo : (p.L + ROWS - 1) / ROWS - 1 - lo;
+    }
+    p.first = __builtin_amdgcn_readfirstlane(p.first), p.L = __builtin_amdgcn_readfirstlane(p.L);
+    p.index = __builtin_amdgcn_readfirstlane(p.index);
+    if (a.B > 64) __syncthreads();
+    return p;
 }
 
 // Row of accumulator element i (0..15) inside a 32x32 result tile, for a lane of half-wave g.
@@ -115,7 +195,7 @@ constexpr unsigned fwd_lds_bytes(int split, int buffers, int scored_queries = 0)
     return split * 2 * buffers * kPfTile * sizeof(_Float16) + scored_queries * (1 + scored_queries / 32) * sizeof(float);
 }
 
-template <int WAVES, int SPLIT, int BUF, bool SCORES>
+template <int WAVES, int SPLIT, int BUF, bool SCORES, bool PACKED = false, bool BF16 = false>
 __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(PrefillArgs a)
 {
     constexpr int kRows = kPfN / WAVES, kLoads = kRows / 4;     // rows of a tile one wave loads, four per instruction
@@ -126,17 +206,27 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int set = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6) / WAVES;
     _Float16 *Ks = tiles + set * 2 * BUF * kPfTile, *Vs = Ks + BUF * kPfTile;
     // heaviest row blocks (the last ones: they see the most keys) first
-    const int nbh = (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
-    const int qb = a.nblk - 1 - (int)blockIdx.x / nbh;
+    const int nbh = PACKED ? a.Hq : (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
+    PackedBlock pb{};
+    if constexpr (PACKED) {
+        pb = packed_block<32 * WAVES, true>(a, (int)blockIdx.x / nbh, (int *)tiles);
+        if (pb.L == 0) return;
+    }
+    const int qb = PACKED ? pb.index : a.nblk - 1 - (int)blockIdx.x / nbh;
     const long bh = head, kvh = (head / a.Hq) * (a.Hq / a.rep) + (head % a.Hq) / a.rep;
-    const int L = (int)a.L;
-    const _Float16 *Qh = a.Q + bh * L * kPfD, *Kh = a.K + kvh * L * kPfD, *Vh = a.V + kvh * L * kPfD;
+    const int L = PACKED ? pb.L : (int)a.L;
+    // (pitches in bytes; a packed prompt's head lies 256 bytes into each of its tokens)
+    const unsigned q_pitch = PACKED ? a.q_pitch : 256u, k_pitch = PACKED ? a.k_pitch : 256u, v_pitch = PACKED ? a.v_pitch : 256u;
+    const _Float16 *Qh = PACKED ? a.Q + (long)pb.first * (q_pitch / 2) + head * kPfD : a.Q + bh * L * kPfD;
+    const _Float16 *Kh = PACKED ? a.K + (long)pb.first * (k_pitch / 2) + kvh * kPfD : a.K + kvh * L * kPfD;
+    const _Float16 *Vh = PACKED ? a.V + (long)pb.first * (v_pitch / 2) + kvh * kPfD : a.V + kvh * L * kPfD;
+    const long stat = PACKED ? (long)pb.first * a.Hq + (long)head * L : bh * L;      // of the head's LSE and column sums
 
     const int q0 = qb * (32 * WAVES) + wave * 32;      // first query of this wave
     const int query = q0 + r;                          // this lane's query column
     half8 qf[8];                                       // B operand of S^T = K Q^T: Q[query][16 ks + 8 g ..]
     {
-        const _Float16 *qp = Qh + (long)min(query, L - 1) * kPfD + g * 8;
+        const _Float16 *qp = Qh + (long)min(query, L - 1) * (q_pitch / 2) + g * 8;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(qp + ks * 16);
     }
@@ -148,21 +238,24 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int mytiles = of_set(min((q0 + 31) / kPfN + 1, all)), nfull = min(of_set((q0 + 1) / kPfN), mytiles);
 
     // tile loads
-    const unsigned v_off = (lane >> 4) * 256u + (((lane & 15) ^ v_swizzle(lane >> 4)) << 4);
+    const unsigned v_off = (lane >> 4) * v_pitch + (((lane & 15) ^ v_swizzle(lane >> 4)) << 4);
     // (of the first load; the i-th one is four rows further for each i, which flips bits 2 and 3 of the chunk)
-    const unsigned k_off = (lane >> 4) * 256u + (((lane & 15) ^ ((wave * kRows + (lane >> 4)) & 15)) << 4);
+    const unsigned k_row = PACKED ? (lane >> 4) * k_pitch : 0;           // (apart from the chunk: a pitch need not be a multiple of 256)
+    const unsigned k_off = (PACKED ? 0 : (lane >> 4) * 256u) + (((lane & 15) ^ ((wave * kRows + (lane >> 4)) & 15)) << 4);
     const unsigned k_lds = lds_offset(Ks) + wave * (kRows * 256u), v_lds = lds_offset(Vs) + wave * (kRows * 256u);
     // (no branch: code motion across one would take the interleaving below apart.  Lanes whose row lies past the
     // prompt load the last chunk of its last row, any finite value will do: their weights are 0.  For a tile past the
     // last one that counts every lane loads the same bytes, into a buffer nobody reads any more: nearly nothing moves.)
     auto request = [&](const _Float16 *base, int n, bool is_v) {
         const int t = n * SPLIT + set, row0 = min(t, all - 1) * kPfN + wave * kRows;
-        const char *tile = (const char *)(base + (long)min(row0, L - 1) * kPfD);
+        const unsigned pitch = is_v ? v_pitch : k_pitch;
+        const char *tile = (const char *)(base + (long)min(row0, L - 1) * (pitch / 2));
         const unsigned lds = (is_v ? v_lds : k_lds) + (BUF == 2 ? (n & 1) * (kPfTile * 2u) : 0u);
-        const int end = t < all ? max(L - 1 - row0, 0) * 256 + 240 : 0;
+        const int after = max(L - 1 - row0, 0);
+        const int end = t < all ? (PACKED ? min(after, kRows) : after) * (int)pitch + 240 : 0;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            load_to_lds(tile, (unsigned)min((int)(is_v ? v_off : k_off ^ ((i & 3) << 6)) + i * 1024, end), lds + i * 1024u);
+            load_to_lds(tile, (unsigned)min((int)(is_v ? v_off : k_row + (k_off ^ ((i & 3) << 6))) + i * 4 * (int)pitch, end), lds + i * 1024u);
     };
     // all loads of this wave have landed and its fragment reads have returned (their buffer is about to be refilled); then
     // the barrier that hands every wave's share over
@@ -225,7 +318,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     // for this wave.
     auto step = [&](float16v (&cur)[2], float16v (&next)[2], int n, auto multiply, auto parity, auto masked) {
         constexpr int odd = decltype(parity)::value;
-        half8 pb[4];                                   // B operands of the output product: the weights as fp16
+        half8 wb[4];                                   // B operands of the output product: the weights as fp16
         float x[2], y[2], sum[2] = {0.0f, 0.0f};
         // weights 2e, 2e+1 of this lane pass through three stages (exponent, power, sum) in three consecutive slots
         auto slot = [&](int e) {
@@ -233,7 +326,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
                 const int w = 2 * (e - 2);
                 sum[0] += y[0], sum[1] += y[1];
                 asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));      // (else the sums of the last step sink to where they are used, and every weight lives until then)
-                pb[w >> 3][w & 7] = (_Float16)y[0], pb[w >> 3][(w & 7) + 1] = (_Float16)y[1];
+                wb[w >> 3][w & 7] = to16<BF16>(y[0]), wb[w >> 3][(w & 7) + 1] = to16<BF16>(y[1]);
             }
             if (e >= 1 && e <= 16) y[0] = __builtin_amdgcn_exp2f(x[0]), y[1] = __builtin_amdgcn_exp2f(x[1]);
             if (e <= 15) {
@@ -252,7 +345,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             if (decltype(multiply)::value) {
-                next[j & 1] = mfma32(kf[j & 3], qf[j >> 1], next[j & 1]);
+                next[j & 1] = mfma32<BF16>(kf[j & 3], qf[j >> 1], next[j & 1]);
                 if (j < 12) kf[j & 3] = read_k(j + 4, !odd);
             }
             if (j < 13) slot(j + 1);
@@ -268,7 +361,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            o[j & 3] = mfma32(vf[j & 3], pb[j >> 2], o[j & 3]);
+            o[j & 3] = mfma32<BF16>(vf[j & 3], wb[j >> 2], o[j & 3]);
             if (j < 12) vf[j & 3] = read_v(j + 4, odd);
             if (BUF == 2 && decltype(multiply)::value && j >= 12) kf[j & 3] = read_k(j & 3, odd);   // (past the last tile: unused)
             if (j < 4) slot(j + 14);
@@ -302,7 +395,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
 #pragma unroll
             for (int i = 0; i < 16; ++i) sa[t][i] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sa[j & 1] = mfma32(read_k(j, 0), qf[j >> 1], sa[j & 1]);
+        for (int j = 0; j < 16; ++j) sa[j & 1] = mfma32<BF16>(read_k(j, 0), qf[j >> 1], sa[j & 1]);
         if (nfull < 1) mask(sa, 0);
         float mx = -INFINITY;
 #pragma unroll
@@ -384,15 +477,15 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         hand_over();
     }
     if (query < L) {
-        if (g == 0) a.lse[bh * L + query] = lse2 * kLn2;
-        _Float16 *orow = a.XO + (bh * L + query) * kPfD;
+        if (g == 0) a.lse[stat + query] = lse2 * kLn2;
+        _Float16 *orow = a.XO + (PACKED ? ((long)pb.first + query) * a.Hq + head : bh * L + query) * kPfD;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int iq = 0; iq < 4; ++iq) {
                 half4 h;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = (_Float16)(o[db][iq * 4 + j] * inv);
+                for (int j = 0; j < 4; ++j) h[j] = to16<BF16>(o[db][iq * 4 + j] * inv);
                 *(half4 *)(orow + db * 32 + iq * 8 + g * 4) = h;
             }
     }
@@ -411,7 +504,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[j & 1] = mfma32(qf[j >> 1], read_k(j, n), s[j & 1]);
+            for (int j = 0; j < 16; ++j) s[j & 1] = mfma32<BF16>(qf[j >> 1], read_k(j, n), s[j & 1]);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int key = n * kPfN + t * 32 + r, first = key - q0 - 4 * g;     // first row that sees the key
@@ -429,7 +522,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         if (tid < L) {                                 // (the waves of the rows before the key have nothing to add)
             float total = 0.0f;
             for (int w = tid >> 5; w < WAVES; ++w) total += part[w * (32 * WAVES) + tid];
-            a.A_cumul[bh * L + tid] = total;
+            a.A_cumul[stat + tid] = total;
         }
     }
 }
@@ -449,7 +542,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
 // -> 33.2, but 32 x 400 9.1 -> 10.3, 32 x 777 12.2 -> 13.0, 32 x 4096 80 -> 95).
 constexpr int kColWaves = 4;
 
-template <int KW>
+template <int KW, bool PACKED = false, bool BF16 = false>
 __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(PrefillArgs a)
 {
     constexpr int kKeys = 64 * KW, QW = kColWaves / KW, kTile = 32 * QW;   // keys of the workgroup, queries of a tile
@@ -463,17 +556,26 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kw = wave % KW, qw = wave / KW;
     // column blocks in natural order: block 0 is seen by every query and is the heaviest
-    const int nbh = (int)gridDim.x / a.nblk, kb = (int)blockIdx.x / nbh, head = (int)blockIdx.x % nbh;
+    const int nbh = PACKED ? a.Hq : (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
+    PackedBlock pb{};
+    if constexpr (PACKED) {
+        pb = packed_block<kKeys, false>(a, (int)blockIdx.x / nbh, (int *)Qs);
+        if (pb.L == 0) return;
+    }
+    const int kb = PACKED ? pb.index : (int)blockIdx.x / nbh;
     const long bh = head, kvh = (head / a.Hq) * (a.Hq / a.rep) + (head % a.Hq) / a.rep;
-    const int L = (int)a.L;
-    const _Float16 *Qh = a.Q + bh * L * kPfD, *Kh = a.K + kvh * L * kPfD;
-    const float *lseh = a.lse + bh * L;
+    const int L = PACKED ? pb.L : (int)a.L;
+    const unsigned q_pitch = PACKED ? a.q_pitch : 256u, k_pitch = PACKED ? a.k_pitch : 256u;
+    const _Float16 *Qh = PACKED ? a.Q + (long)pb.first * (q_pitch / 2) + head * kPfD : a.Q + bh * L * kPfD;
+    const _Float16 *Kh = PACKED ? a.K + (long)pb.first * (k_pitch / 2) + kvh * kPfD : a.K + kvh * L * kPfD;
+    const long stat = PACKED ? (long)pb.first * a.Hq + (long)head * L : bh * L;
+    const float *lseh = a.lse + stat;
 
     const int k0 = kb * kKeys + kw * 64;               // first key of this wave
     half8 kf[2][8];                                    // B operands of S = Q K^T: K[key][16 ks + 8 g ..]
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const _Float16 *kr = Kh + (long)min(k0 + t * 32 + r, L - 1) * kPfD + g * 8;
+        const _Float16 *kr = Kh + (long)min(k0 + t * 32 + r, L - 1) * (k_pitch / 2) + g * 8;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kf[t][ks] = *(const half8 *)(kr + ks * 16);
     }
@@ -483,16 +585,20 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
     // A wave loads kRows consecutive rows of a tile; lanes whose row lies past the prompt load the last chunk of its last
     // row (their weights are masked), and for a tile past the last every lane loads the same bytes: nearly nothing moves.
     const unsigned q_lds = lds_offset(Qs) + wave * (kRows * 256u);
-    const unsigned q_off = (wave * kRows + (lane >> 4)) * 256u + (((lane & 15) ^ (lane >> 4)) << 4);    // of the first load
+    const unsigned q_row = PACKED ? (wave * kRows + (lane >> 4)) * q_pitch : 0;
+    const unsigned q_off = (PACKED ? 0 : (wave * kRows + (lane >> 4)) * 256u) + (((lane & 15) ^ (lane >> 4)) << 4);    // of the first load
     const int lse0 = wave % (kTile / 64) * 64;   // (uniform)
     auto request = [&](int n) -> float {               // returns the LSE of query lse0 + lane of the tile
-        const unsigned tile = (unsigned)min(n, ntiles - 1) * (kTile * 256u);
-        const unsigned end = n < ntiles ? (unsigned)(L - 1) * 256u + 240u : 0u;
+        // (a packed prompt's rows may lie too far apart for one 32-bit offset: the tile is in the base there)
+        const int row0 = min(n, ntiles - 1) * kTile;
+        const unsigned tile = PACKED ? 0u : (unsigned)min(n, ntiles - 1) * (kTile * 256u);
+        const unsigned end = n >= ntiles ? 0u : PACKED ? (unsigned)min(L - 1 - row0, kTile) * q_pitch + 240u : (unsigned)(L - 1) * 256u + 240u;
+        const _Float16 *base = PACKED ? Qh + (long)row0 * (q_pitch / 2) : Qh;
         unsigned off = q_off;
         if (KW == 1) asm volatile("" : "+v"(off));     // (opaque: its four forms are not kept over the loop, which has no register for them)
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            load_to_lds(Qh, min((off ^ ((i & 3) << 6)) + i * 1024u + tile, end), q_lds + (n & 1) * (kTile * 256u) + i * 1024u);
+            load_to_lds(base, min(q_row + (off ^ ((i & 3) << 6)) + i * 4u * q_pitch + tile, end), q_lds + (n & 1) * (kTile * 256u) + i * 1024u);
         return lseh[min((n * kTile + lse0) + lane, L - 1)];  // (some waves the same 64: no branch in the stream)
     };
     float lr = 0.0f;
@@ -540,7 +646,7 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 16; ++m) {                 // element pair 2m, 2m+1 of the 32 weights of a lane
-            next[m & 1] = mfma32(qf[m >> 1], kf[m & 1][m >> 1], next[m & 1]);
+            next[m & 1] = mfma32<BF16>(qf[m >> 1], kf[m & 1][m >> 1], next[m & 1]);
             if (m & 1) read_q(m >> 1, n + 2);
             const float y0 = __builtin_amdgcn_exp2f(x[0]), y1 = __builtin_amdgcn_exp2f(x[1]);
             if (m) cs[(m - 1) >> 3] += y[0];
@@ -586,7 +692,7 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
 #pragma unroll
         for (int i = 0; i < 16; ++i) sa[t][i] = 0.0f;
 #pragma unroll
-    for (int m = 0; m < 16; ++m) sa[m & 1] = mfma32(qf[m >> 1], kf[m & 1][m >> 1], sa[m & 1]);
+    for (int m = 0; m < 16; ++m) sa[m & 1] = mfma32<BF16>(qf[m >> 1], kf[m & 1][m >> 1], sa[m & 1]);
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) read_q(ks, tile0 + 1);
     settle(tile0 + 2);
@@ -615,7 +721,7 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
     float total = sum;
 #pragma unroll
     for (int w = 0; w < QW - 1; ++w) total += part_sum[w * kKeys + kw * 64 + lane];
-    a.A_cumul[bh * L + k0 + lane] = total;
+    a.A_cumul[stat + k0 + lane] = total;
 }
 
 int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f16 *Q, const minikv_f16 *K,
@@ -681,6 +787,41 @@ int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f
         if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
     }
     return MINIKV_OK;
+}
+
+template <bool BF16>
+static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
+{
+    // workgroups per head, at most: a prompt's last block may be a part of one
+    auto blocks = [&](int rows) {
+        const int64_t by_rows = a.T / rows + a.B, by_prompt = (int64_t)a.B * ((a.max_len + rows - 1) / rows);
+        return (by_rows < by_prompt ? by_rows : by_prompt) * a.Hq;
+    };
+    if (blocks(64) > 0x7fffffff) return MINIKV_EINVAL;
+    if (scores && a.max_len <= 128) {
+        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, true, true, BF16>), dim3((unsigned)blocks(128)), dim3(256), fwd_lds_bytes(1, 2, 128), st, a);
+        return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
+    }
+    hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, false, true, BF16>), dim3((unsigned)blocks(128)), dim3(256), fwd_lds_bytes(1, 2), st, a);
+    if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
+    if (scores) {
+        hipLaunchKernelGGL((prefill_colsum_kernel<2, true, BF16>), dim3((unsigned)blocks(128)), dim3(64 * kColWaves), 0, st, a);
+        if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
+    }
+    return MINIKV_OK;
+}
+
+int launch_prefill_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype, const void *Q,
+                          int64_t q_stride, const void *K, int64_t k_stride, const void *V, int64_t v_stride, const int32_t *cu,
+                          float sm_scale, void *XO, float *lse, float *A_cumul, hipStream_t st)
+{
+    PrefillArgs a{};
+    a.Q = (const _Float16 *)Q, a.K = (const _Float16 *)K, a.V = (const _Float16 *)V;
+    a.XO = (_Float16 *)XO, a.lse = lse, a.A_cumul = A_cumul;
+    a.Hq = Hq, a.rep = Hq / Hkv, a.scale_log2 = sm_scale * kLog2e;
+    a.cu = cu, a.B = B, a.T = T, a.max_len = max_len < T ? max_len : T;
+    a.q_pitch = (unsigned)q_stride * 2, a.k_pitch = (unsigned)k_stride * 2, a.v_pitch = (unsigned)v_stride * 2;
+    return dtype == MINIKV_BF16 ? launch_packed<true>(a, A_cumul != nullptr, st) : launch_packed<false>(a, A_cumul != nullptr, st);
 }
 
 }  // namespace minikv
