@@ -230,8 +230,8 @@ size_t minikv_blk_cache_bytes(const minikv_blk_shape *s, int which)
 size_t minikv_blk_workspace_bytes(const minikv_blk_shape *s)
 {
     if (validate_blk(s) != MINIKV_OK) return 0;
-    // a ticket counter and two partials per workgroup, at the same places for every shape
-    return (size_t)kBlkGroups * (sizeof(int) + 2 * kBlkPartial * sizeof(float));
+    // ticket counters and two partials per workgroup, at the same places for every shape
+    return (size_t)kBlkTickets * sizeof(int) + (size_t)kBlkGroups * 2 * kBlkPartial * sizeof(float);
 }
 
 int kv_assign_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *n_new, int32_t *table, int32_t *ring,

@@ -100,7 +100,8 @@ bool aligned16(const void *p);
 // the paged 8-bit cache
 constexpr int kMaxRequests = 8192;   // a workgroup holds a few words per request in local memory
 constexpr int kBlkTile = 64;         // tokens a wave of the attention takes at once
-constexpr int kBlkGroups = 512;      // most workgroups of the attention: two per compute unit
+constexpr int kBlkGroups = kComputeUnits;            // most workgroups of the attention
+constexpr int kBlkTickets = kBlkGroups * (1 + kMaxRep / 2);     // of units in several workgroups' parts: see decode_blk.hip
 constexpr int kBlkPartial = kMaxRep * (kD + 2);      // floats of a workgroup's partial: m and l of each head, then o
 int launch_assign_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *n_new, int32_t *table, int32_t *ring,
                       const int32_t *state, int32_t *q_len_next, int32_t *state_next, int32_t *cu, int32_t *slots,

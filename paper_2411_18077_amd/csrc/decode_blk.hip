@@ -14,7 +14,7 @@
 //
 // Weights are rounded to fp16 for the second product (relative 2^-11, to nearest, the sum of weights is kept in fp32 from
 // the unrounded ones), scaled by the block's V scale over the largest one seen so far: at most 1, whatever the scales.
-#include "common.h"
+#include "decode_common.h"
 
 #include <type_traits>
 
@@ -26,9 +26,16 @@ typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 
-constexpr int kBkThreads = 256;
+constexpr int kBkWaves = 8;                            // of a workgroup: two per SIMD, the registers of a compute unit
+constexpr int kBkThreads = 64 * kBkWaves;
 constexpr int kBkRow = kD + 4;                         // floats of a head's state in local memory: m, l, 2 pad, o
+constexpr int kBkEntry = kMaxRep * kBkRow;             // of a part of a unit
 constexpr float kBkNone = -3.0e38f;                    // running maximum before the first token: finite, so that no difference is NaN
+// What a unit costs a wave besides its tiles (table, scales, queries, output), in tiles on the line of work.
+constexpr int kBkUnitCost = 1;
+// Workgroups of their own for every unit beat the line of work (where there are enough of them) while their waves have at most so
+// many tiles more than the line's.
+constexpr int kBkUnitTiles = 3;
 
 struct BlkArgs {
     const uint16_t *q;
@@ -37,10 +44,11 @@ struct BlkArgs {
     const float *Ks, *Vs;
     const int32_t *table, *q_len;
     uint16_t *out;
-    int *tickets;                                      // [kBlkGroups]
-    float *partials;                                   // [2 * kBlkGroups][kBlkPartial]: m and l [8] each, o [8][128]
+    int *tickets;                                      // [kBlkGroups] of the line's units, then [kBlkGroups / 2][kMaxRep] of shared units
+    float *partials;                                   // [2 * kBlkGroups][kBlkPartial]: (m, l) of 8 heads, o [8][128]
     float c;                                           // sm_scale * log2(e)
     int R, Hq, Hkv, rep, n_blocks, width;
+    uint32_t hkv_magic, hkv_shift, units_magic, units_shift;            // division by Hkv and by R Hkv
 };
 
 __device__ inline uint64_t ld8(const float *p)         // device scope: other dies wrote it in this launch
@@ -54,6 +62,15 @@ __device__ inline void st8(float *p, float a, float b)
 }
 __device__ inline float lo8(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ inline float hi8(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+
+// Codes are read once a call, and a program's other layers have caches of their own before this one's turn comes again: loaded
+// with the streaming hint (16 requests of 32768 tokens 195 -> 178 us, 6.0 TB/s; one of 131072 59 -> 56).
+__device__ inline uint4 load_codes(const uint8_t *p)
+{
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    const u4v v = __builtin_nontemporal_load((const u4v *)p);
+    return uint4{v[0], v[1], v[2], v[3]};
+}
 
 template <bool BF16> struct Frag;
 template <> struct Frag<false> {
@@ -80,131 +97,135 @@ template <> struct Frag<true> {
 // maximum / sum over the four lanes n, n + 16, n + 32, n + 48
 __device__ inline float max_over_g(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ inline float sum_over_g(float v)
 {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline float other_half(float v)            // of lane n ^ 8
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xf, 0xf, false));
 }
 
+__device__ inline int wave_max(int v)                  // of values >= 0, the same in every lane
+{
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));       // row_shr 1, 2, 4, 8
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));       // row_bcast 15, 31
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ inline int wave_sum_of(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <bool BF16> __device__ inline uint32_t pack2(float a, float b)
+{
+    if constexpr (BF16) return __builtin_bit_cast(uint32_t, bf2v{(__bf16)a, (__bf16)b});
+    else return __builtin_bit_cast(uint32_t, half2v{(_Float16)a, (_Float16)b});
+}
 
-// Work: the tiles of 64 tokens of all (request, KV head) units laid end to end and cut into equal ranges, one per
-// workgroup, so that lengths of any kind fill the card; every workgroup reads all lengths and finds its range by
-// itself.  Its four waves take quarters of a unit's part and meet in local memory; a unit that lies in several workgroups
-// is merged by the one that finishes last (a ticket per unit, counted at the unit's first workgroup).
+// Work.  A unit is a (request, KV head), its tiles are 64 tokens.  Every workgroup reads all lengths and finds what it does.
+//   The line: tiles of all units laid end to end, each unit behind kBkUnitCost empty ones, cut into equal ranges, one per WAVE, so that
+//   lengths of any kind fill the card.  A unit inside a wave's range is that wave's alone, from queries to output.  Of the
+//   units that its ends cut, a wave leaves its part in local memory (two at most, "A" of a unit that began before, "B" of one that goes
+//   on); behind one barrier the wave with the unit's first part in the workgroup merges the parts, and writes the output or, where
+//   other workgroups have parts too, publishes the result and takes a ticket; the last one's workgroup merges them.
+//   A workgroup per unit, or several, if there are enough of them and no wave gets many more tiles than on the line: one up to eight tiles, else a
+//   power of two of them with about four tiles each, so that every SIMD has one.  (A wave's tile is 2800 cycles of one SIMD, most of them
+//   conversions, and merging between workgroups 4000.)
+// What bounds it: memory, where there is much to read (16 requests of 32768 tokens, 8 KV heads, 1.07 GB: 166 us, 6.5 TB/s, a plain
+// streaming read reaches 6.0; one of 131072 tokens 51 us, 5.3 TB/s; 48 of 1 to 16000 tokens 48 us, 4.2 TB/s); round trips and the
+// first pass through the code where there is little (8 heads of 1024 tokens 7.7 us); the conversions and what a unit costs besides
+// its tiles where there are many short ones (1000 requests of 1 to 300 tokens 47 us).  With a workgroup's four waves on the same unit
+// and a barrier for each, the 48 took 130 us, the 1024 tokens 9.1; on the line alone the 16 took 178 and the 1024 tokens 11.4.
 template <int BS, bool BF16>
 __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
 {
-    constexpr int kIds = BS < kBlkTile ? kBlkTile / BS : 1;             // blocks of a tile
+    constexpr int kIds = BS < kBlkTile ? kBlkTile / BS : 1, kTiles = BS > kBlkTile ? BS / kBlkTile : 1;     // blocks of a tile, tiles of a block
+    constexpr int kRun = BS < kBlkTile ? BS : kBlkTile;                 // tokens of a tile that lie together
     extern __shared__ float lds[];
-    float *parts = lds;                                // [4 waves][2 halves][8 heads][kBkRow]
-    int *before = (int *)(lds + 64 * kBkRow);          // [R+1] tiles of the requests before r (of one KV head)
-    __shared__ int wave_sum[4], ticket;
+    float *parts = lds;                                // [2 * kBkWaves][8 heads][kBkRow]
+    int *before = (int *)(lds + 2 * kBkWaves * kBkEntry);              // [R+1] line of the requests before r (of one KV head)
+    int *lens = before + a.R + 1;                      // [R]
+    __shared__ int wave_sum[kBkWaves], last[2][4]; // units whose last part came from here: r, h, first workgroup, count
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int n = lane & 15, g = lane >> 4, half = n >> 3, head = n & 7;
     const int wg = blockIdx.x;
-    const int64_t most = (int64_t)a.width * BS;
 
-    {                                                  // prefix sums of the requests' tiles
-        auto tiles = [&](int r) { return (int)((min((int64_t)max(a.q_len[r], 0), most) + kBlkTile - 1) / kBlkTile); };
-        const int per = (a.R + kBkThreads - 1) / kBkThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-        int sum = 0;
-        for (int r = r0; r < r1; ++r) sum += tiles(r);
-        int in = sum;
+    f4v o[16];                                         // this lane's sums, see the top of the file
+    float m, l, vref;                                  // maximum and sum of weights, largest V scale
+    auto entry_of = [&](int t) { return t * kIds / kTiles; };
+    // What is loaded for: the unit, its table entries batch + lane (block, K factor, V scale), its queries, one tile of codes.
+    int ld_h = 0, ld_len = 0, batch = 0, id = -1;
+    const int32_t *ld_row = nullptr;
+    float kf = 0.0f, vs = 0.0f;
+    typename Frag<BF16>::type qf[4];
+    uint4 kx[4][2], vx[8];
+    // found: in lane i, table entry `entry` + i (anything where the request has none)
+    auto take = [&](int entry, int found) {
+        batch = entry;
+        id = (batch + lane) * BS < ld_len && (uint32_t)found < (uint32_t)a.n_blocks ? found : -1;
+        const int64_t at = (int64_t)max(id, 0) * a.Hkv + ld_h;
+        kf = a.Ks[at] * a.c, vs = id < 0 ? 0.0f : a.Vs[at];
+    };
+    auto turn_to = [&](int r, int h, int len, int t, int found) {      // tiles from t on of unit (r, h) are loaded next
+        ld_h = h, ld_len = len, ld_row = a.table + (int64_t)r * a.width;
+        const uint16_t *q = a.q + (int64_t)r * a.q_stride + (h * a.rep + min(head, a.rep - 1)) * kD + g * 16;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(in, d, 64);
-            if (lane >= d) in += o;
-        }
-        if (lane == 63) wave_sum[wave] = in;
-        __syncthreads();
-        int at = in - sum;
-        for (int w = 0; w < wave; ++w) at += wave_sum[w];
-        for (int r = r0; r < r1; ++r) before[r] = at, at += tiles(r);
-        if (tid == kBkThreads - 1) before[a.R] = at;
-        __syncthreads();
-    }
-    const int all = uniform(before[a.R] * a.Hkv);
-    const int span = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 4);
-    int x = (int)min((int64_t)wg * span, (int64_t)all);
-    const int end = (int)min((int64_t)x + span, (int64_t)all);
-
-    for (int r = wg; r < a.R; r += gridDim.x)          // requests without tokens
-        if (before[r + 1] == before[r])
-            for (int i = tid; i < a.Hq * kD / 8; i += kBkThreads)
-                ((uint4 *)(a.out + (int64_t)r * a.Hq * kD))[i] = uint4{0, 0, 0, 0};
-
-    while (x < end) {
-        // the unit that tile x belongs to, and the part [t0, t1) of its tiles that lies in this workgroup
-        int r = 0;
-        {
-            const int y = x / a.Hkv;
-            for (int step = a.R > 1 ? 1 << (31 - __builtin_clz(a.R - 1)) : 0; step; step >>= 1)
-                if (r + step < a.R && before[r + step] <= y) r += step;
-            r = uniform(r);
-        }
-        const int line = uniform(before[r] * a.Hkv), nt = uniform(before[r + 1] - before[r]);
-        const int h = (x - line) / nt, t0 = x - line - h * nt, t1 = min(nt, t0 + (end - x));
-        const int len = uniform((int)min((int64_t)max(a.q_len[r], 0), most));
-        const int32_t *row = a.table + (int64_t)r * a.width;
-        const int used = (len + BS - 1) / BS;          // table entries of the request
-
-        typename Frag<BF16>::type qf[4];
-        {
-            const uint16_t *q = a.q + (int64_t)r * a.q_stride + (h * a.rep + min(head, a.rep - 1)) * kD + g * 16;
+        for (int k = 0; k < 4; ++k) qf[k] = *(const typename Frag<BF16>::type *)(q + (k >> 1) * 64 + (k & 1) * 8);
+        take(entry_of(t), found);
+    };
+    auto lane_value = [&](int v, int i) { return __builtin_amdgcn_readlane(v, i); };
+    auto lane_float = [&](float v, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), i)); };
+    // Rows behind the request's last token are not loaded: their lanes repeat a row that is (for V, four rows that begin before it).
+    auto load_k = [&](int t) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) qf[k] = *(const typename Frag<BF16>::type *)(q + (k >> 1) * 64 + (k & 1) * 8);
+        for (int j = 0; j < 4; ++j) {                  // tokens 16 j .. of the tile
+            const int64_t b = max(lane_value(id, entry_of(t) - batch + j * kIds / 4), 0);
+            const int first = t % kTiles * kBlkTile + j * 16 % kRun, there = min(max(ld_len - t * kBlkTile - j * 16, 1), 16);
+            const uint8_t *p = a.K + ((b * a.Hkv + ld_h) * BS + first) * kD;
+            const int at = min(n, there - 1) * kD + g * 16;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) kx[j][k] = load_codes(p + at + k * 64);
         }
-        f4v o[16];
+    };
+    auto load_v = [&](int t) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                  // token quad 4g of the 16 tokens 2 half + k
+            int b = lane_value(id, entry_of(t) - batch + k * kIds / 4);
+            if (kIds > 1) b = half ? lane_value(id, entry_of(t) - batch + (2 + k) * kIds / 4) : b;
+            const int left = ld_len - t * kBlkTile - (2 * half + k) * 16, quad = min(g, max(left - 1, 0) >> 2);
+            const int first = t % kTiles * kBlkTile + (2 * half + k) * 16 % kRun;
+            const uint8_t *p = a.V + (((int64_t)max(b, 0) * a.Hkv + ld_h) * BS + first + quad * 4) * kD + head * 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vx[4 * k + i] = load_codes(p + i * kD);
+        }
+    };
+    // Tiles [t0, t1) of the unit of `len` tokens that is being loaded, its first tile already.  more: another unit's first tile is to be loaded
+    // behind the last one, next() turns to it.
+    auto attend = [&](int len, int t0, int t1, bool more, auto next) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
-        float m = kBkNone, l = 0.0f, vref = 0.0f, ivref = 0.0f;
-
-        const int begin = t0 + (int)((int64_t)(t1 - t0) * wave / 4), stop = t0 + (int)((int64_t)(t1 - t0) * (wave + 1) / 4);
-        int batch = 0, id = -1;                        // table entries batch + lane: block, K factor, V scale
-        float kf = 0.0f, vs = 0.0f;
-        auto fetch = [&](int entry) {
-            batch = entry;
-            id = batch + lane < used ? row[batch + lane] : -1;
-            if ((uint32_t)id >= (uint32_t)a.n_blocks) id = -1;
-            const int64_t at = (int64_t)max(id, 0) * a.Hkv + h;
-            kf = a.Ks[at] * a.c, vs = id < 0 ? 0.0f : a.Vs[at];
-        };
-        auto entry_of = [&](int t) { return BS < kBlkTile ? t * kIds : t / (BS / kBlkTile); };
-        auto lane_value = [&](int v, int i) { return __builtin_amdgcn_readlane(v, i); };
-        auto lane_float = [&](float v, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), i)); };
-        uint4 kx[4][2], vx[8];
-        auto block_base = [&](const uint8_t *p, int t, int i) {         // block i of tile t, its first row of the tile
-            const int64_t b = max(lane_value(id, entry_of(t) - batch + i), 0);
-            return p + ((b * a.Hkv + h) * BS + (BS > kBlkTile ? (t % (BS / kBlkTile)) * kBlkTile : 0)) * kD;
-        };
-        auto load_k = [&](int t) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint8_t *p = block_base(a.K, t, j * kIds / 4) + (j * 16) % (BS < kBlkTile ? BS : kBlkTile) * kD;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) kx[j][k] = *(const uint4 *)(p + n * kD + g * 16 + k * 64);
-            }
-        };
-        auto load_v = [&](int t) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {              // token quad 4g of the 16 tokens 2 half + k
-                int b = lane_value(id, entry_of(t) - batch + k * kIds / 4);
-                if (kIds > 1) b = half ? lane_value(id, entry_of(t) - batch + (2 + k) * kIds / 4) : b;
-                const int first = (BS > kBlkTile ? (t % (BS / kBlkTile)) * kBlkTile : 0) + ((2 * half + k) * 16) % (BS < kBlkTile ? BS : kBlkTile);
-                const uint8_t *p = a.V + (((int64_t)max(b, 0) * a.Hkv + h) * BS + first + g * 4) * kD + head * 16;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vx[4 * k + i] = *(const uint4 *)(p + i * kD);
-            }
-        };
-        if (begin < stop) {
-            fetch(entry_of(begin));
-            load_k(begin), load_v(begin);
-        }
-        for (int t = begin; t < stop; ++t) {
+        m = kBkNone, l = 0.0f, vref = 0.0f;
+        float ivref = 0.0f;
+        for (int t = t0; t < t1; ++t) {
             const int e0 = entry_of(t) - batch;
             bool whole = (t + 1) * kBlkTile <= len;
             float vmax = 0.0f, f[2], vf[2];            // largest V scale; this lane's K factors and V scales (of 16 tokens each)
@@ -224,7 +245,6 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                     absent[k] = (half ? hi : lo) < 0;
                 }
             }
-            const bool more = t + 1 < stop;
             f4v s[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -235,10 +255,14 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                     s[j] = Frag<BF16>::mul(k & 1 ? Frag<BF16>::codes(w.z, w.w) : Frag<BF16>::codes(w.x, w.y), qf[k], s[j]);
                 }
             }
-            if (more) {
-                if (entry_of(t + 1) + kIds > batch + 64) fetch(entry_of(t + 1));
-                load_k(t + 1);
+            int ahead = t + 1;                         // the tile loaded next: of this unit, or the next unit's first
+            if (ahead < t1) {
+                const int entry = entry_of(ahead);
+                if (entry + kIds > batch + 64) take(entry, ld_row[min(entry + lane, a.width - 1)]);
+            } else if (more) {
+                ahead = 0, next();
             }
+            if (ahead < t1 || more) load_k(ahead);
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = (half ? s[2 + (i >> 2)][i & 3] : s[i >> 2][i & 3]) * f[i >> 2];
@@ -288,93 +312,298 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                 for (int i = 0; i < 4; ++i)
                     o[4 * d + i] = Frag<false>::mul(Frag<false>::codes(col[0][i], col[1][i]), p, o[4 * d + i]);
             }
-            if (more) load_v(t + 1);
+            if (ahead < t1 || more) load_v(ahead);
         }
-
-        // the waves' states meet in local memory: 8 parts (wave, half), of each its quadrant
-        {
-            float *part = parts + (wave * 2 + half) * 8 * kBkRow + head * kBkRow;
-            l = sum_over_g(l);
-            if (g == 0) part[0] = m, part[1] = l;
-            if ((g >> 1) == half) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 16; j += 4)
-                        *(float4 *)(part + 4 + (4 * (g & 1) + i) * 16 + j) =
-                            float4{o[j][i] * vref, o[j + 1][i] * vref, o[j + 2][i] * vref, o[j + 3][i] * vref};
-            }
-        }
-        __syncthreads();
-        const int hh = tid >> 5, ch = (tid & 31) * 4;  // this thread's head and channels
-        float M = kBkNone, L = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) M = fmaxf(M, parts[(k * 8 + hh) * kBkRow]);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float *part = parts + (k * 8 + hh) * kBkRow;
-            const float f = __builtin_amdgcn_exp2f(part[0] - M);
-            const float4 v = *(const float4 *)(part + 4 + ch);
-            L += part[1] * f;
-            acc[0] += v.x * f, acc[1] += v.y * f, acc[2] += v.z * f, acc[3] += v.w * f;
-        }
-        auto write_out = [&]() {
-            const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-            uint16_t v[4];
+    };
+    // The wave's sums of a unit to local memory.  o[j][i] belongs to channel 16 (4 (g & 1) + i) + j, in the lanes whose row and
+    // column belong to one half of the tokens.
+    auto leave_halves = [&](int slot) __attribute__((always_inline)) {      // each half to a slot of its own
+        l = sum_over_g(l);
+        float *p = parts + (slot + half) * kBkEntry + head * kBkRow;
+        if (g == 0) p[0] = m, p[1] = l;
+        p += 4 + (g & 1) * 64;
+        if ((g >> 1) == half) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                v[i] = BF16 ? __builtin_bit_cast(uint16_t, (__bf16)(acc[i] * inv)) : __builtin_bit_cast(uint16_t, (_Float16)(acc[i] * inv));
-            *(uint2 *)(a.out + ((int64_t)r * a.Hq + h * a.rep + hh) * kD + ch) =
-                uint2{(uint32_t)v[1] << 16 | v[0], (uint32_t)v[3] << 16 | v[2]};
-        };
-        if (t0 == 0 && t1 == nt) {
-            if (hh < a.rep) write_out();
-        } else {
-            // (device scope throughout: the unit's workgroups run on different dies)
-            const int ustart = line + h * nt, first = ustart / span, count = (ustart + nt - 1) / span - first + 1;
-            float *slot = a.partials + (int64_t)(2 * wg + (t0 == 0)) * kBlkPartial;
-            if (hh < a.rep) {
-                if (ch == 0) st8(slot + 2 * hh, M, L);
-                st8(slot + 16 + hh * kD + ch, acc[0], acc[1]);
-                st8(slot + 16 + hh * kD + ch + 2, acc[2], acc[3]);
+#pragma unroll
+                for (int j = 0; j < 16; j += 4)
+                    *(float4 *)(p + i * 16 + j) = float4{o[j][i] * vref, o[j + 1][i] * vref, o[j + 2][i] * vref, o[j + 3][i] * vref};
+        }
+    };
+    // both to one slot: the second half's lanes put theirs down, the first half's add theirs
+    auto leave_part = [&](int slot) __attribute__((always_inline)) {
+        const float both = fmaxf(m, other_half(m)), mine = __builtin_amdgcn_exp2f(m - both);
+        l = sum_over_g(l) * mine;
+        l += other_half(l);
+        float *p = parts + slot * kBkEntry + head * kBkRow;
+        if (lane < 8) p[0] = both, p[1] = l;
+        const float f = mine * vref;
+        p += 4 + (g & 1) * 64;
+        if (half && g >= 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4)
+                    *(float4 *)(p + i * 16 + j) = float4{o[j][i] * f, o[j + 1][i] * f, o[j + 2][i] * f, o[j + 3][i] * f};
+        }
+        __builtin_amdgcn_wave_barrier();               // (one wave's local memory operations are done in order)
+        if (!half && g < 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const float4 v = *(const float4 *)(p + i * 16 + j);
+                    *(float4 *)(p + i * 16 + j) = float4{v.x + o[j][i] * f, v.y + o[j + 1][i] * f, v.z + o[j + 2][i] * f, v.w + o[j + 3][i] * f};
+                }
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    // parts in slots 0, step, 2 step ... (below end), of head `wave`: a lane takes two channels
+    float M, L, x0, x1;
+    auto merge_slots = [&](int step, int end) __attribute__((always_inline)) {
+        const float *p = parts + wave * kBkRow;
+        M = kBkNone, L = x0 = x1 = 0.0f;
+        for (int w = 0; w < end; w += step) M = fmaxf(M, p[w * kBkEntry]);
+        for (int w = 0; w < end; w += step) {
+            const float *q = p + w * kBkEntry;
+            const float f = __builtin_amdgcn_exp2f(q[0] - M);
+            const float2 v = *(const float2 *)(q + 4 + 2 * lane);
+            L += q[1] * f, x0 += v.x * f, x1 += v.y * f;
+        }
+    };
+    // partials of head hd of the workgroups place(k), k = from, from + step ... < count, sixteen at once
+    auto merge_partials = [&](int hd, int from, int step, int count, auto place) __attribute__((always_inline)) {
+        constexpr int kAtOnce = 16;
+        M = kBkNone, L = x0 = x1 = 0.0f;
+        for (int k0 = from; k0 < count; k0 += kAtOnce * step) {
+            uint64_t ml[kAtOnce], v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const float *src = a.partials + (int64_t)place(min(k0 + k * step, count - 1)) * kBlkPartial;
+                ml[k] = ld8(src + 2 * hd), v[k] = ld8(src + 2 * kMaxRep + hd * kD + 2 * lane);
             }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // this wave's stores are acknowledged ...
-            __syncthreads();                                           // ... and every wave's
-            if (tid == 0) ticket = __hip_atomic_fetch_add(a.tickets + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, lo8(ml[k]));
+            float f = __builtin_amdgcn_exp2f(M - top);
+            M = top, L *= f, x0 *= f, x1 *= f;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                f = k0 + k * step < count ? __builtin_amdgcn_exp2f(lo8(ml[k]) - top) : 0.0f;
+                L += hi8(ml[k]) * f, x0 += lo8(v[k]) * f, x1 += hi8(v[k]) * f;
+            }
+        }
+    };
+    auto write_out = [&](int r, int h, int hd) __attribute__((always_inline)) {
+        const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+        *(uint32_t *)(a.out + ((int64_t)r * a.Hq + h * a.rep + hd) * kD + 2 * lane) = pack2<BF16>(x0 * inv, x1 * inv);
+    };
+
+    const int units = a.R * a.Hkv;
+    const int share = (int)fast_div((uint32_t)wg, a.units_magic, a.units_shift), unit = wg - share * units;      // a unit's workgroups are `units` apart
+    int r = (int)fast_div((uint32_t)unit, a.hkv_magic, a.hkv_shift), h = unit - r * a.Hkv, shares = 1;
+    bool by_unit = units <= (int)gridDim.x;
+    int unit_len = 0, unit_t0 = 0, unit_t1 = 0, unit_first = 0;
+    if (by_unit) {                                     // (lengths, the table and the queries are requested together, as few units wait for)
+        const int64_t most = (int64_t)a.width * BS;
+        auto len_of = [&](int i) { return (int)min((int64_t)max(a.q_len[i], 0), most); };
+        const int32_t *row = a.table + (int64_t)r * a.width;
+        unit_len = uniform(len_of(r));
+        const int e0 = row[min(lane, a.width - 1)];
+        int top = 0, sum = 0;                          // (as many requests as workgroups, at most)
+        for (int i = lane; i < a.R; i += 64) {
+            const int tiles = (len_of(i) + kBlkTile - 1) / kBlkTile;
+            top = max(top, tiles), sum += tiles;
+        }
+        top = wave_max(top), sum = wave_sum_of(sum) * a.Hkv;
+        if (top > kBkWaves)
+            while (shares * 4 < top && 2 * shares * units <= (int)gridDim.x) shares *= 2;
+        by_unit = (top + shares * kBkWaves - 1) / (shares * kBkWaves) <= sum / ((int)gridDim.x * kBkWaves) + kBkUnitTiles;
+        if (by_unit) {
+            if (share >= shares) return;               // (the whole workgroup)
+            const int nt = (unit_len + kBlkTile - 1) / kBlkTile, from = nt * share / shares, n = nt * (share + 1) / shares - from;
+            const int each = n / kBkWaves, more = n % kBkWaves;        // (waves 0 .. 3 are on SIMDs of their own)
+            unit_t0 = from + wave * each + min(wave, more), unit_t1 = unit_t0 + each + (wave < more);
+            const int entry = entry_of(unit_t0);
+            unit_first = __shfl(e0, (entry + lane) & 63, 64);
+            if (entry_of(unit_t1) + kIds > 64) unit_first = row[min(entry + lane, a.width - 1)];
+        }
+    }
+    int total = 0;
+    if (__builtin_expect(!by_unit, 0)) {
+        {
+            auto cost = [&](int len) { return len ? (len + kBlkTile - 1) / kBlkTile + kBkUnitCost : 0; };
+            const int64_t most = (int64_t)a.width * BS;
+            const int per = (a.R + kBkThreads - 1) / kBkThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+            int sum = 0;
+            for (int r = r0; r < r1; ++r) {
+                const int len = (int)min((int64_t)max(a.q_len[r], 0), most);
+                lens[r] = len, sum += cost(len);
+            }
+            int in = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(in, d, 64);
+                if (lane >= d) in += o;
+            }
+            if (lane == 63) wave_sum[wave] = in;
+            if (tid < 2) last[tid][3] = 0;
             __syncthreads();
-            if (ticket == count - 1) {
-                if (tid == 0) __hip_atomic_store(a.tickets + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                M = kBkNone, L = 0.0f, acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
-                if (hh < a.rep) {
-                    constexpr int kAtOnce = 8;
-                    for (int k0 = 0; k0 < count; k0 += kAtOnce) {
-                        uint64_t ml[kAtOnce], v0[kAtOnce], v1[kAtOnce];
+            int at = in - sum;
 #pragma unroll
-                        for (int k = 0; k < kAtOnce; ++k) {
-                            const int kk = min(k0 + k, count - 1);
-                            const float *src = a.partials + (int64_t)(kk == 0 ? 2 * first + 1 : 2 * (first + kk)) * kBlkPartial;
-                            ml[k] = ld8(src + 2 * hh), v0[k] = ld8(src + 16 + hh * kD + ch), v1[k] = ld8(src + 16 + hh * kD + ch + 2);
-                        }
-                        float top = M;
-#pragma unroll
-                        for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, lo8(ml[k]));
-                        float f = __builtin_amdgcn_exp2f(M - top);
-                        M = top, L *= f;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[i] *= f;
-#pragma unroll
-                        for (int k = 0; k < kAtOnce; ++k) {
-                            f = k0 + k < count ? __builtin_amdgcn_exp2f(lo8(ml[k]) - top) : 0.0f;
-                            L += hi8(ml[k]) * f;
-                            acc[0] += lo8(v0[k]) * f, acc[1] += hi8(v0[k]) * f, acc[2] += lo8(v1[k]) * f, acc[3] += hi8(v1[k]) * f;
-                        }
-                    }
-                    write_out();
+            for (int w = 0; w < kBkWaves; ++w)
+                if (w < wave) at += wave_sum[w];
+            for (int r = r0; r < r1; ++r) before[r] = at, at += cost(lens[r]);
+            if (tid == kBkThreads - 1) before[a.R] = at;
+            __syncthreads();
+        }
+        for (int r = wg; r < a.R; r += gridDim.x)          // requests without tokens
+            if (lens[r] == 0)
+                for (int i = tid; i < a.Hq * kD / 8; i += kBkThreads)
+                    ((uint4 *)(a.out + (int64_t)r * a.Hq * kD))[i] = uint4{0, 0, 0, 0};
+        total = uniform(before[a.R] * a.Hkv);
+        if (total == 0) return;
+    }
+    // The line: tile t of a unit that begins at `start` on it stands at start + kBkUnitCost + t.
+    const int span = by_unit ? 1 : max((total + (int)gridDim.x * kBkWaves - 1) / ((int)gridDim.x * kBkWaves), kBkUnitCost + 1);
+    const int64_t from = (int64_t)(wg * kBkWaves + wave) * span;
+    int x = (int)min(from, (int64_t)total);
+    const int end = (int)min(from + span, (int64_t)total);
+    // the units of this wave's parts A and B: which, and their first and last wave with tiles
+    int a_r = -1, a_h = 0, a_first = 0, a_stop = 0, b_r = -1, b_h = 0, b_first = 0, b_stop = 0;
+    int len = unit_len, t0 = unit_t0, t1 = unit_t1, first = unit_first, start = 0, c = 0;
+    // where unit (r, h) lies on the line and which of its tiles are this wave's
+    auto locate = [&](int r, int h, int &len, int &t0, int &t1, int &start, int &c) {
+        len = uniform(lens[r]), c = uniform(before[r + 1] - before[r]), start = uniform(before[r] * a.Hkv) + h * c;
+        t0 = max(x - start - kBkUnitCost, 0), t1 = min(end - start, c) - kBkUnitCost;
+    };
+    if (!by_unit && x < end) {
+        const int y = (int)fast_div((uint32_t)x, a.hkv_magic, a.hkv_shift);
+        r = 0;
+        for (int step = a.R > 1 ? 1 << (31 - __builtin_clz(a.R - 1)) : 0; step; step >>= 1)
+            if (r + step < a.R && before[r + step] <= y) r += step;
+        r = uniform(r);
+        h = uniform((x - before[r] * a.Hkv) / (before[r + 1] - before[r]));
+        locate(r, h, len, t0, t1, start, c);
+        if (t0 < t1) first = a.table[(int64_t)r * a.width + min(entry_of(t0) + lane, a.width - 1)];
+    }
+    if (t0 < t1) {
+        turn_to(r, h, len, t0, first);
+        load_k(t0), load_v(t0);
+    }
+    while (by_unit || t0 < t1) {                       // (a range that has none of a unit's tiles ends before them)
+        int r2 = r, h2 = h + 1, len2 = 0, from2 = 0, to2 = 0, start2 = 0, c2 = 0, first2 = 0;
+        if (!by_unit) {                                // the next unit, and its table while this one's tiles are worked on
+            x = start + c;
+            if (x < end) {
+                if (h2 == a.Hkv) {
+                    h2 = 0, ++r2;
+                    while (before[r2 + 1] == before[r2]) ++r2;         // (x < end: there is one)
+                    r2 = uniform(r2);
+                }
+                locate(r2, h2, len2, from2, to2, start2, c2);
+                if (from2 < to2) first2 = a.table[(int64_t)r2 * a.width + min(lane, a.width - 1)];
+            }
+        }
+        attend(len, t0, t1, from2 < to2, [&]() { turn_to(r2, h2, len2, 0, first2); });
+        const bool goes_on = !by_unit && t0 == 0, alone = goes_on && t1 == c - kBkUnitCost;
+        const int slot = 2 * wave + goes_on;           // (a part B is a wave's last: until then its slot is free)
+        if (by_unit) {
+            leave_halves(slot);
+            break;
+        }
+        leave_part(slot);
+        if (alone) {
+            for (int hd = 0; hd < a.rep; ++hd) {
+                const float *p = parts + slot * kBkEntry + hd * kBkRow;
+                const float2 v = *(const float2 *)(p + 4 + 2 * lane);
+                const float inv = p[1] > 0.0f ? 1.0f / p[1] : 0.0f;
+                *(uint32_t *)(a.out + ((int64_t)r * a.Hq + h * a.rep + hd) * kD + 2 * lane) = pack2<BF16>(v.x * inv, v.y * inv);
+            }
+        } else {
+            const int lead = (start + kBkUnitCost) / span, stop = (start + c - 1) / span;
+            if (goes_on) b_r = r, b_h = h, b_first = lead, b_stop = stop;
+            else a_r = r, a_h = h, a_first = lead, a_stop = stop;
+        }
+        r = r2, h = h2, len = len2, t0 = from2, t1 = to2, start = start2, c = c2;
+    }
+    __syncthreads();
+    if (by_unit) {
+        if (wave >= a.rep) return;                     // a wave per head from here on
+        merge_slots(1, 2 * kBkWaves);
+        if (shares > 1) {
+            float *out = a.partials + (int64_t)2 * wg * kBlkPartial;
+            if (lane == 0) st8(out + 2 * wave, M, L);
+            st8(out + 2 * kMaxRep + wave * kD + 2 * lane, x0, x1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // the stores are acknowledged before the ticket is taken
+            int *counter = a.tickets + kBlkGroups + unit * kMaxRep + wave, ticket = 0;
+            if (lane == 0) ticket = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (uniform(ticket) != shares - 1) return;
+            if (lane == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            merge_partials(wave, 0, 1, shares, [&](int k) { return 2 * (unit + k * units); });
+        }
+        write_out(r, h, wave);
+        return;
+    }
+    // the parts of a unit in this workgroup: slot `first`, then the A parts of the next waves; lanes take two channels each
+    auto merge_parts = [&](int cut_r, int cut_h, int cut_first, int cut_stop, int b) __attribute__((always_inline)) {
+        const int lead = b == 0 ? 0 : wave, stop = min(cut_stop - wg * kBkWaves, kBkWaves - 1);
+        const int first_wg = cut_first / kBkWaves, count = cut_stop / kBkWaves - first_wg + 1;
+        float *out = a.partials + (int64_t)(2 * wg + b) * kBlkPartial;
+        for (int hd = 0; hd < a.rep; ++hd) {
+            const float *p0 = parts + (2 * lead + b) * kBkEntry + hd * kBkRow;
+            float M = p0[0];
+            for (int w = lead + 1; w <= stop; ++w) M = fmaxf(M, parts[2 * w * kBkEntry + hd * kBkRow]);
+            float f = __builtin_amdgcn_exp2f(p0[0] - M);
+            float2 v = *(const float2 *)(p0 + 4 + 2 * lane);
+            float L = p0[1] * f, x0 = v.x * f, x1 = v.y * f;
+            for (int w = lead + 1; w <= stop; ++w) {
+                const float *p = parts + 2 * w * kBkEntry + hd * kBkRow;
+                f = __builtin_amdgcn_exp2f(p[0] - M);
+                v = *(const float2 *)(p + 4 + 2 * lane);
+                L += p[1] * f, x0 += v.x * f, x1 += v.y * f;
+            }
+            if (count == 1) {
+                const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+                *(uint32_t *)(a.out + ((int64_t)cut_r * a.Hq + cut_h * a.rep + hd) * kD + 2 * lane) = pack2<BF16>(x0 * inv, x1 * inv);
+            } else {                                   // (device scope throughout: the unit's workgroups run on different dies)
+                if (lane == 0) st8(out + 2 * hd, M, L);
+                st8(out + 2 * kMaxRep + hd * kD + 2 * lane, x0, x1);
+            }
+        }
+        if (count > 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // the stores are acknowledged before the ticket is taken
+            if (lane == 0) {
+                const int ticket = __hip_atomic_fetch_add(a.tickets + first_wg, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (ticket == count - 1) {
+                    __hip_atomic_store(a.tickets + first_wg, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    last[b][0] = cut_r, last[b][1] = cut_h, last[b][2] = first_wg, last[b][3] = count;
                 }
             }
         }
-        __syncthreads();                               // the parts are read: the next unit's may come
-        x += t1 - t0;
+    };
+    if (a_r >= 0 && wave == 0) merge_parts(a_r, a_h, a_first, a_stop, 0);               // (behind another wave's part, that one merges it)
+    if (b_r >= 0) merge_parts(b_r, b_h, b_first, b_stop, 1);
+    __syncthreads();
+    for (int b = 0; b < 2; ++b) {
+        r = uniform(last[b][0]), h = uniform(last[b][1]);
+        const int first_wg = uniform(last[b][2]), count = uniform(last[b][3]);
+        if (count == 0) continue;
+        // the workgroups' partials of a head and of every sets-th workgroup to a wave, sixteen at once; then a wave per head
+        const int sets = kBkWaves / a.rep, set = wave / a.rep, hd = wave - set * a.rep;
+        if (set < sets) {
+            merge_partials(hd, set, sets, count, [&](int k) { return k == 0 ? 2 * first_wg + 1 : 2 * (first_wg + k); });
+            float *p = parts + 2 * set * kBkEntry + hd * kBkRow;
+            if (lane == 0) p[0] = M, p[1] = L;
+            *(float2 *)(p + 4 + 2 * lane) = float2{x0, x1};
+        }
+        __syncthreads();
+        if (wave < a.rep) {
+            merge_slots(2, 2 * sets);
+            write_out(r, h, wave);
+        }
+        __syncthreads();
     }
 }
 
@@ -384,12 +613,15 @@ int launch_decode_blk(const minikv_blk_shape &s, const void *q, int64_t q_stride
     BlkArgs a;
     a.q = (const uint16_t *)q, a.q_stride = q_stride, a.K = c.K, a.V = c.V, a.Ks = c.Ks, a.Vs = c.Vs;
     a.table = table, a.q_len = q_len, a.out = (uint16_t *)out;
-    a.tickets = (int *)workspace, a.partials = (float *)((char *)workspace + kBlkGroups * sizeof(int));
+    a.tickets = (int *)workspace, a.partials = (float *)((char *)workspace + kBlkTickets * sizeof(int));
     a.c = sm_scale * 1.4426950408889634f;
     a.R = s.R, a.Hq = s.Hq, a.Hkv = s.Hkv, a.rep = s.Hq / s.Hkv, a.n_blocks = s.n_blocks, a.width = s.max_blocks;
+    fast_div_setup((uint32_t)s.Hkv, a.hkv_magic, a.hkv_shift);
+    fast_div_setup((uint32_t)(s.R * s.Hkv), a.units_magic, a.units_shift);
     const int64_t tiles = ((int64_t)s.max_blocks * s.block + kBlkTile - 1) / kBlkTile * s.R * s.Hkv;
+    // (a workgroup per unit where that is chosen, else eight waves of at least two places on the line each)
     const dim3 grid((unsigned)(tiles < kBlkGroups ? tiles : kBlkGroups));
-    const size_t lds = (64 * kBkRow + s.R + 1) * sizeof(float);
+    const size_t lds = (2 * kBkWaves * kBkEntry + 2 * s.R + 1) * sizeof(float);
     auto launch = [&](auto bs) {
         constexpr int BS = decltype(bs)::value;
         if (s.dtype == MINIKV_BF16) hipLaunchKernelGGL((decode_blk_kernel<BS, true>), grid, dim3(kBkThreads), lds, st, a);

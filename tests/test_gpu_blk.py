@@ -225,7 +225,7 @@ def attend(api, lens, Hq, Hkv, block, dtype, seed=1, width=None, spread=2, spoil
     out.fill_(float("nan"))
     api.minikv_decode_attn_blk(*args)                                                # the workspace is as it was
     assert torch.equal(first, out)
-    assert not bool(cache.workspace[:2048].any())
+    assert not bool(cache.workspace[:5120].any())
     return out
 
 

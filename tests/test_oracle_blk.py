@@ -123,7 +123,7 @@ def test_paged_sizes_and_arguments_are_checked_on_the_host(api):
     l, shape = api.lib(), api.MinikvBlkShape(*GOOD.values())
     assert [l.minikv_blk_cache_bytes(C.byref(shape), i) for i in range(10)] == [100 * 2 * 32 * 128, 800, 0, 100 * 2 * 32 * 128, 800, 0, 0, 0, 0, 0]
     need = l.minikv_blk_workspace_bytes(C.byref(shape))
-    assert need == 512 * (4 + 2 * 4 * 8 * 130)
+    assert need == 256 * (4 * 5 + 2 * 4 * 8 * 130)
     assert l.minikv_blk_cache_bytes(None, 0) == 0
     rows = ("file", "attend")
     assert calls(api, shape, p=None) == [-1] * 3 and calls(api, shape, p=P(0x1002)) == [-1] * 3
