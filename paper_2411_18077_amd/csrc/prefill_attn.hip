@@ -41,6 +41,7 @@ struct PrefillArgs {
     // packed prompts (PACKED instances only): prompt b is rows cu[b] .. cu[b+1]-1 of T, tokens *_pitch bytes apart
     const int32_t *cu;
     int B, T, max_len;
+    int side;                        // log2 of the query heads (of one KV head) that a workgroup of the first pass takes side by side
     unsigned q_pitch, k_pitch, v_pitch;
 };
 
@@ -80,19 +81,20 @@ __device__ __forceinline__ int wave_sum(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
     return __builtin_amdgcn_readlane(v, 63);
 }
-template <int ROWS, bool HEAVY_LAST>
-__device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int rank, int *counts)
+template <bool HEAVY_LAST>
+__device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int log_rows, int rank, int *counts)
 {
+    auto blocks = [&](int rows) { return (rows + (1 << log_rows) - 1) >> log_rows; };
     const int lane = threadIdx.x & 63;
     auto length = [&](int b) {                         // 0: no prompt, or one to be left alone
         const int at = a.cu[b], end = a.cu[b + 1];
         return at >= 0 && end > at && end <= a.T && end - at <= a.max_len ? end - at : 0;
     };
-    int one = 0, levels = (a.max_len + ROWS - 1) / ROWS;
+    int one = 0, levels = blocks(a.max_len);
     if (a.B <= 64) {
-        one = lane < a.B ? (length(lane) + ROWS - 1) / ROWS : 0;
+        one = lane < a.B ? blocks(length(lane)) : 0;
     } else {
-        for (int b = lane; b < a.B; b += 64) counts[b] = (length(b) + ROWS - 1) / ROWS;
+        for (int b = lane; b < a.B; b += 64) counts[b] = blocks(length(b));
     }
     auto beyond = [&](int q) {                         // blocks with at least q others behind them, seen from the heavy end
         int sum = 0;
@@ -117,7 +119,7 @@ __device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int ra
             left -= n;
         }
         p.first = a.cu[b], p.L = length(b);
-        p.index = HEAVY_LAST ? lo : (p.L + ROWS - 1) / ROWS - 1 - lo;
+        p.index = HEAVY_LAST ? lo : blocks(p.L) - 1 - lo;
     }
     p.first = __builtin_amdgcn_readfirstlane(p.first), p.L = __builtin_amdgcn_readfirstlane(p.L);
     p.index = __builtin_amdgcn_readfirstlane(p.index);
@@ -206,10 +208,16 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int set = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6) / WAVES;
     _Float16 *Ks = tiles + set * 2 * BUF * kPfTile, *Vs = Ks + BUF * kPfTile;
     // heaviest row blocks (the last ones: they see the most keys) first
-    const int nbh = PACKED ? a.Hq : (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
+    // Packed prompts under grouped heads: 2^side waves side by side take as many heads, whose keys are the same, of the same 32
+    // queries, so that a short prompt's rows are not spread over as many workgroups and all waves walk equally far.
+    const int side = PACKED ? a.side : 0, aside = PACKED ? wave & ((1 << side) - 1) : 0;
+    constexpr int kLogRows = WAVES == 8 ? 8 : WAVES == 4 ? 7 : 6;
+    static_assert(1 << kLogRows == 32 * WAVES, "rows of a workgroup");
+    const int rows = 1 << (kLogRows - side);           // queries of the workgroup
+    const int nbh = PACKED ? a.Hq >> side : (int)gridDim.x / a.nblk, head = PACKED ? ((int)blockIdx.x % nbh << side) + aside : (int)blockIdx.x % nbh;
     PackedBlock pb{};
     if constexpr (PACKED) {
-        pb = packed_block<32 * WAVES, true>(a, (int)blockIdx.x / nbh, (int *)tiles);
+        pb = packed_block<true>(a, kLogRows - side, (int)blockIdx.x / nbh, (int *)tiles);
         if (pb.L == 0) return;
     }
     const int qb = PACKED ? pb.index : a.nblk - 1 - (int)blockIdx.x / nbh;
@@ -222,7 +230,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const _Float16 *Vh = PACKED ? a.V + (long)pb.first * (v_pitch / 2) + kvh * kPfD : a.V + kvh * L * kPfD;
     const long stat = PACKED ? (long)pb.first * a.Hq + (long)head * L : bh * L;      // of the head's LSE and column sums
 
-    const int q0 = qb * (32 * WAVES) + wave * 32;      // first query of this wave
+    const int q0 = qb * rows + (wave >> side) * 32;    // first query of this wave
     const int query = q0 + r;                          // this lane's query column
     half8 qf[8];                                       // B operand of S^T = K Q^T: Q[query][16 ks + 8 g ..]
     {
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     // Tile n of this set is tile n * SPLIT + set of the prompt.  Steps of the workgroup (every wave meets each barrier),
     // this set's tiles some query of this wave sees, and those every query of the wave sees whole:
     auto of_set = [&](int n) { return max((n - set + SPLIT - 1) / SPLIT, 0); };
-    const int all = (min((qb + 1) * (32 * WAVES), L) + kPfN - 1) / kPfN;
+    const int all = (min((qb + 1) * rows, L) + kPfN - 1) / kPfN;
     const int ntiles = (all + SPLIT - 1) / SPLIT;
     const int mytiles = of_set(min((q0 + 31) / kPfN + 1, all)), nfull = min(of_set((q0 + 1) / kPfN), mytiles);
 
@@ -559,7 +567,7 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
     const int nbh = PACKED ? a.Hq : (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
     PackedBlock pb{};
     if constexpr (PACKED) {
-        pb = packed_block<kKeys, false>(a, (int)blockIdx.x / nbh, (int *)Qs);
+        pb = packed_block<false>(a, KW == 1 ? 6 : 7, (int)blockIdx.x / nbh, (int *)Qs);
         if (pb.L == 0) return;
     }
     const int kb = PACKED ? pb.index : (int)blockIdx.x / nbh;
@@ -792,23 +800,44 @@ int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f
 template <bool BF16>
 static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
 {
-    // workgroups per head, at most: a prompt's last block may be a part of one
-    auto blocks = [&](int rows) {
+    // workgroups of `rows` rows per head, at most: a prompt's last block may be a part of one
+    auto per_head = [&](int rows) {
         const int64_t by_rows = a.T / rows + a.B, by_prompt = (int64_t)a.B * ((a.max_len + rows - 1) / rows);
-        return (by_rows < by_prompt ? by_rows : by_prompt) * a.Hq;
+        return by_rows < by_prompt ? by_rows : by_prompt;
     };
-    if (blocks(64) > 0x7fffffff) return MINIKV_EINVAL;
+    if (per_head(32) * a.Hq > 0x7fffffff) return MINIKV_EINVAL;
     if (scores && a.max_len <= 128) {
-        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, true, true, BF16>), dim3((unsigned)blocks(128)), dim3(256), fwd_lds_bytes(1, 2, 128), st, a);
+        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, true, true, BF16>), dim3((unsigned)(per_head(128) * a.Hq)), dim3(256),
+                           fwd_lds_bytes(1, 2, 128), st, a);
         return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
     }
-    hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, false, true, BF16>), dim3((unsigned)blocks(128)), dim3(256), fwd_lds_bytes(1, 2), st, a);
+    // Which form, by the rules for prompts of one length (launch_prefill) with the longest prompt as the length and an upper
+    // bound of the blocks, which is what the host knows.
+    const int64_t heads = (int64_t)a.B * a.Hq;
+    auto blocks = [&](int rows) { return a.Hq * per_head(rows); };
+    const bool two_buffers = a.max_len > 96 && 2 * blocks(64) <= (heads <= 20 ? 3 : 2) * kComputeUnits;
+    const bool two_sets_64 = two_buffers || (a.max_len > 384 && blocks(64) <= 2 * kComputeUnits);
+    const bool two_sets_128 = a.max_len >= 1024 && heads <= 32 && 2 * blocks(128) <= (heads <= 20 ? 4 : 3) * kComputeUnits;
+    const int waves = a.max_len >= 4096 && blocks(256) >= 4 * kComputeUnits ? 8 : two_sets_64 ? 2 : 4;
+    while (a.side < 3 && (2 << a.side) <= waves && a.rep % (2 << a.side) == 0) ++a.side;
+    const dim3 grid((unsigned)(per_head(32 * waves >> a.side) * (a.Hq >> a.side)));
+    if (waves == 8)
+        hipLaunchKernelGGL((prefill_fwd_kernel<8, 1, 2, false, true, BF16>), grid, dim3(512), fwd_lds_bytes(1, 2), st, a);
+    else if (two_sets_64 && !two_buffers)
+        hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 1, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 1), st, a);
+    else if (two_sets_64)
+        hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 2), st, a);
+    else if (two_sets_128)
+        hipLaunchKernelGGL((prefill_fwd_kernel<4, 2, 2, false, true, BF16>), grid, dim3(512), fwd_lds_bytes(2, 2), st, a);
+    else
+        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(1, 2), st, a);
     if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
-    if (scores) {
+    if (!scores) return MINIKV_OK;
+    if (blocks(64) <= (heads <= 20 ? 2 : 1) * kComputeUnits)
+        hipLaunchKernelGGL((prefill_colsum_kernel<1, true, BF16>), dim3((unsigned)blocks(64)), dim3(64 * kColWaves), 0, st, a);
+    else
         hipLaunchKernelGGL((prefill_colsum_kernel<2, true, BF16>), dim3((unsigned)blocks(128)), dim3(64 * kColWaves), 0, st, a);
-        if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
-    }
-    return MINIKV_OK;
+    return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
 }
 
 int launch_prefill_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype, const void *Q,
