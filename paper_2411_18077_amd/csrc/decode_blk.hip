@@ -134,6 +134,13 @@ __device__ inline int wave_sum_of(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
     return __builtin_amdgcn_readlane(v, 63);
 }
+// local memory that one wave writes and reads: its operations are done in order, the compiler is told to keep them so
+__device__ inline void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 template <bool BF16> __device__ inline uint32_t pack2(float a, float b)
 {
@@ -346,7 +353,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                 for (int j = 0; j < 16; j += 4)
                     *(float4 *)(p + i * 16 + j) = float4{o[j][i] * f, o[j + 1][i] * f, o[j + 2][i] * f, o[j + 3][i] * f};
         }
-        __builtin_amdgcn_wave_barrier();               // (one wave's local memory operations are done in order)
+        wave_order();
         if (!half && g < 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -356,7 +363,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                     *(float4 *)(p + i * 16 + j) = float4{v.x + o[j][i] * f, v.y + o[j + 1][i] * f, v.z + o[j + 2][i] * f, v.w + o[j + 3][i] * f};
                 }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_order();
     };
 
     // parts in slots 0, step, 2 step ... (below end), of head `wave`: a lane takes two channels

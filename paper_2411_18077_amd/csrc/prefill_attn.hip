@@ -81,21 +81,27 @@ __device__ __forceinline__ int wave_sum(int v)
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
     return __builtin_amdgcn_readlane(v, 63);
 }
+// What a wave keeps of the prompts: with up to 64 of them, prompt `lane`.
+struct PackedLane {
+    int first, L;
+};
+__device__ __forceinline__ PackedLane packed_prompt(const PrefillArgs &a, int b)
+{
+    const int at = a.cu[b], end = a.cu[b + 1];         // (0 rows: no prompt, or one to be left alone)
+    return PackedLane{at, at >= 0 && end > at && end <= a.T && end - at <= a.max_len ? end - at : 0};
+}
+__device__ __forceinline__ PackedLane packed_lane(const PrefillArgs &a)
+{
+    const int lane = threadIdx.x & 63;
+    return a.B <= 64 && lane < a.B ? packed_prompt(a, lane) : PackedLane{0, 0};
+}
 template <bool HEAVY_LAST>
-__device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int log_rows, int rank, int *counts)
+__device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, const PackedLane &mine, int log_rows, int rank, int *counts)
 {
     auto blocks = [&](int rows) { return (rows + (1 << log_rows) - 1) >> log_rows; };
-    const int lane = threadIdx.x & 63;
-    auto length = [&](int b) {                         // 0: no prompt, or one to be left alone
-        const int at = a.cu[b], end = a.cu[b + 1];
-        return at >= 0 && end > at && end <= a.T && end - at <= a.max_len ? end - at : 0;
-    };
-    int one = 0, levels = blocks(a.max_len);
-    if (a.B <= 64) {
-        one = lane < a.B ? blocks(length(lane)) : 0;
-    } else {
-        for (int b = lane; b < a.B; b += 64) counts[b] = blocks(length(b));
-    }
+    const int lane = threadIdx.x & 63, one = blocks(mine.L), levels = blocks(a.max_len);
+    if (a.B > 64)
+        for (int b = lane; b < a.B; b += 64) counts[b] = blocks(packed_prompt(a, b).L);
     auto beyond = [&](int q) {                         // blocks with at least q others behind them, seen from the heavy end
         int sum = 0;
         if (a.B <= 64) sum = max(one - q, 0);
@@ -118,11 +124,14 @@ __device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, int lo
             }
             left -= n;
         }
-        p.first = a.cu[b], p.L = length(b);
-        p.index = HEAVY_LAST ? lo : blocks(p.L) - 1 - lo;
+        if (a.B <= 64) {
+            p.first = __builtin_amdgcn_readlane(mine.first, b), p.L = __builtin_amdgcn_readlane(mine.L, b);
+        } else {
+            const PackedLane at = packed_prompt(a, b);
+            p.first = __builtin_amdgcn_readfirstlane(at.first), p.L = __builtin_amdgcn_readfirstlane(at.L);
+        }
+        p.index = __builtin_amdgcn_readfirstlane(HEAVY_LAST ? lo : blocks(p.L) - 1 - lo);
     }
-    p.first = __builtin_amdgcn_readfirstlane(p.first), p.L = __builtin_amdgcn_readfirstlane(p.L);
-    p.index = __builtin_amdgcn_readfirstlane(p.index);
     if (a.B > 64) __syncthreads();
     return p;
 }
@@ -148,6 +157,14 @@ __device__ __forceinline__ unsigned lds_offset(const void *p)
 // Tiles loaded this way have unpadded rows of 256 bytes; chunk k (16 bytes) of row r sits at place k ^ (r & 15), so
 // that the fragment reads of 32 consecutive rows use all banks evenly.
 __device__ __forceinline__ int tile_place(int row, int chunk) { return row * kPfD + ((chunk ^ (row & 15)) << 3); }
+
+// Local memory that one wave writes and reads: its operations are done in order, the compiler is told to keep them so.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // A workgroup of WAVES waves owns 32 queries per wave (their Q rows in registers) and walks the keys in tiles of 64.
 // Scores are computed TRANSPOSED, S^T = K Q^T, so that a lane holds one query column (see the top of the file).  One
@@ -201,6 +218,10 @@ template <int WAVES, int SPLIT, int BUF, bool SCORES, bool PACKED = false, bool 
 __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(PrefillArgs a)
 {
     constexpr int kRows = kPfN / WAVES, kLoads = kRows / 4;     // rows of a tile one wave loads, four per instruction
+    // Many workgroups of packed prompts: outputs go through local memory, a few rows of the wave at a time, so that rows are stored
+    // whole.  16 bytes of 32 rows an instruction are 512 requests a wave, and those are what short prompts wait for (64 prompts of up to
+    // 320 tokens 52 -> 47 us, 16 of up to 1000 143 -> 136); where a launch is a workgroup or two deep the exchange costs 0.3 us.
+    constexpr bool WHOLE_ROWS = PACKED && SPLIT == 1 && !SCORES;
     extern __shared__ __align__(16) _Float16 tiles[];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
@@ -217,7 +238,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int nbh = PACKED ? a.Hq >> side : (int)gridDim.x / a.nblk, head = PACKED ? ((int)blockIdx.x % nbh << side) + aside : (int)blockIdx.x % nbh;
     PackedBlock pb{};
     if constexpr (PACKED) {
-        pb = packed_block<true>(a, kLogRows - side, (int)blockIdx.x / nbh, (int *)tiles);
+        pb = packed_block<true>(a, packed_lane(a), kLogRows - side, (int)blockIdx.x / nbh, (int *)tiles);
         if (pb.L == 0) return;
     }
     const int qb = PACKED ? pb.index : a.nblk - 1 - (int)blockIdx.x / nbh;
@@ -484,7 +505,34 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         if (g == 0) row_lse2[wave * 32 + r] = lse2;
         hand_over();
     }
-    if (query < L) {
+    if constexpr (WHOLE_ROWS) {
+        constexpr int kPart = WAVES == 8 ? 8 : 16;     // rows at a time
+        char *stage = (char *)tiles + wave * (kPart * 256);
+        hand_over();                                   // (every wave has read the last tile)
+        if (g == 0 && query < L) a.lse[stat + query] = lse2 * kLn2;
+        const int there = L - q0;                      // rows of the wave that exist
+        _Float16 *out = a.XO + (((long)pb.first + q0) * a.Hq + head) * kPfD + (lane & 15) * 8;
+#pragma unroll
+        for (int part = 0; part < 32 / kPart; ++part) {
+            if (r / kPart == part) {
+#pragma unroll
+                for (int chunk = 0; chunk < 16; ++chunk) {             // channels 8 chunk .., this half-wave's four
+                    half4 h;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[j] = to16<BF16>(o[chunk >> 2][(chunk & 3) * 4 + j] * inv);
+                    *(half4 *)(stage + r % kPart * 256 + ((chunk ^ (r & 15)) << 4) + g * 8) = h;
+                }
+            }
+            wave_order();
+#pragma unroll
+            for (int k = 0; k < kPart / 4; ++k) {
+                const int row = part * kPart + 4 * k + (lane >> 4);
+                const half8 v = *(const half8 *)(stage + row % kPart * 256 + (((lane & 15) ^ (row & 15)) << 4));
+                if (row < there) *(half8 *)(out + (long)row * a.Hq * kPfD) = v;
+            }
+            wave_order();
+        }
+    } else if (query < L) {
         if (g == 0) a.lse[stat + query] = lse2 * kLn2;
         _Float16 *orow = a.XO + (PACKED ? ((long)pb.first + query) * a.Hq + head : bh * L + query) * kPfD;
 #pragma unroll
@@ -567,7 +615,7 @@ __global__ __launch_bounds__(64 * kColWaves, 2) void prefill_colsum_kernel(Prefi
     const int nbh = PACKED ? a.Hq : (int)gridDim.x / a.nblk, head = (int)blockIdx.x % nbh;
     PackedBlock pb{};
     if constexpr (PACKED) {
-        pb = packed_block<false>(a, KW == 1 ? 6 : 7, (int)blockIdx.x / nbh, (int *)Qs);
+        pb = packed_block<false>(a, packed_lane(a), KW == 1 ? 6 : 7, (int)blockIdx.x / nbh, (int *)Qs);
         if (pb.L == 0) return;
     }
     const int kb = PACKED ? pb.index : (int)blockIdx.x / nbh;
