@@ -1,6 +1,6 @@
 // The paged 8-bit cache: block tables and slot maps from lengths on the device (kv_assign_blk), and the filing of new rows
 // as e4m3 codes with one power-of-two scale per (block, head) (kv_quantize_blk).  See include/minikv.h for what they compute.
-#include "common.h"
+#include "decode_common.h"
 
 namespace minikv {
 
@@ -162,9 +162,22 @@ struct FileArgs {
     uint8_t *codes[2];
     float *scales[2];
     const int32_t *slots;
-    int n_tok, Hkv, shift, rows;                       // rows = n_blocks * block
+    int n_tok, Hkv, shift, rows, chunk;                // rows = n_blocks * block
+    uint32_t heads_magic, heads_shift;                 // division by 2 Hkv
 };
 
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+
+__device__ inline uint32_t wave_max_u32(uint32_t v)    // the same in every lane
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));     // row_shr 1, 2, 4, 8
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));     // row_bcast 15, 31
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ inline uint32_t max_u16x2(uint32_t a, uint32_t b)
 {
     typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
@@ -186,25 +199,27 @@ __device__ inline float scale_for(float amax)
     return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
 }
 
-// A wave takes the runs (consecutive tokens of one block) that begin among its CHUNK tokens, for one head and one of K
-// and V, so that a block's scale has one owner and no barrier or atomic is needed.  Sixteen lanes hold a row, four rows an
-// instruction; up to 64 rows stay in registers between the maximum (on the 16-bit magnitudes, whose order is that of the
-// unsigned integers for fp16 and bf16 alike) and the rounding, more are read again.
-template <int CHUNK, bool BF16>
+// A wave takes the runs (consecutive tokens of one block) that begin among its `chunk` tokens, for one head and one of K
+// and V (neighbouring waves take the heads of the same tokens, which lie side by side), so that a block's scale has one owner and no barrier or atomic is needed.  Sixteen lanes hold a row, four rows an
+// instruction; up to ROWS rows, a block, stay in registers between the maximum (on the 16-bit magnitudes, whose order is that of the
+// unsigned integers for fp16 and bf16 alike) and the rounding.
+template <int ROWS, bool BF16>
 __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
 {
     const int lane = threadIdx.x & 63, c = lane & 15, sub = lane >> 4;
-    const int first = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * CHUNK;
-    const int h = blockIdx.y, which = blockIdx.z;
-    if (first >= a.n_tok) return;
-    const uint16_t *X = a.X[which] + (int64_t)h * kD + c * 8;
-    const int64_t stride = a.stride[which];
+    const uint32_t item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t part = fast_div(item, a.heads_magic, a.heads_shift), of = item - part * 2 * a.Hkv;
+    const int64_t begin = (int64_t)part * a.chunk;
+    if (begin >= a.n_tok) return;
+    const int first = (int)begin, which = of >= (uint32_t)a.Hkv, h = (int)of - (which ? a.Hkv : 0);
+    const uint16_t *X = (which ? a.X[1] : a.X[0]) + (int64_t)h * kD + c * 8;
+    const int64_t stride = which ? a.stride[1] : a.stride[0];
     auto block_of = [&](int i) {                       // block of token i, -1: none
         const int slot = a.slots[i];
         return (uint32_t)slot < (uint32_t)a.rows ? slot >> a.shift : -1;
     };
     bool begins = false;
-    if (lane < CHUNK && first + lane < a.n_tok) {
+    if (lane < a.chunk && first + lane < a.n_tok) {
         const int b = block_of(first + lane);
         begins = b >= 0 && (first + lane == 0 || block_of(first + lane - 1) != b);
     }
@@ -219,32 +234,30 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
             const uint64_t run = same == ~0ull ? ~0ull : (1ull << __builtin_ctzll(~same)) - 1;
             fresh |= (__ballot(mine && (slot & ((1 << a.shift) - 1)) == 0) & run) != 0;
         }
-        uint4 x[16];
-        auto load = [&](int base) {
+        const int64_t at = (int64_t)blk * a.Hkv + h;
+        float *scale = (which ? a.scales[1] : a.scales[0]) + at;
+        uint8_t *codes = (which ? a.codes[1] : a.codes[0]) + ((at << a.shift) * kD);
+        const float old = *scale;
+        u4v x[ROWS / 4];
+        auto load = [&](int base) {                    // (with the streaming hint: each row is this wave's alone)
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-                if (base + 4 * k < n) x[k] = *(const uint4 *)(X + (int64_t)(i + min(base + 4 * k + sub, n - 1)) * stride);
+            for (int k = 0; k < ROWS / 4; ++k)
+                if (base + 4 * k < n) x[k] = __builtin_nontemporal_load((const u4v *)(X + (int64_t)(i + min(base + 4 * k + sub, n - 1)) * stride));
         };
         uint32_t mx = 0;
-        for (int base = 0; base < n; base += 64) {
+        for (int base = 0; base < n; base += ROWS) {
             load(base);
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
+            for (int k = 0; k < ROWS / 4; ++k)
                 if (base + 4 * k < n) {
-                    const uint32_t lo = max_u16x2(x[k].x & 0x7fff7fff, x[k].y & 0x7fff7fff);
-                    const uint32_t hi = max_u16x2(x[k].z & 0x7fff7fff, x[k].w & 0x7fff7fff);
+                    const uint32_t lo = max_u16x2(x[k][0] & 0x7fff7fff, x[k][1] & 0x7fff7fff);
+                    const uint32_t hi = max_u16x2(x[k][2] & 0x7fff7fff, x[k][3] & 0x7fff7fff);
                     mx = max_u16x2(mx, max_u16x2(lo, hi));
                 }
         }
-        mx = max(mx & 0xffff, mx >> 16);
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, d, 64));
-        const int64_t at = (int64_t)blk * a.Hkv + h;
-        float *scale = a.scales[which] + at;
-        uint8_t *codes = a.codes[which] + ((at << a.shift) * kD);
+        mx = wave_max_u32(max(mx & 0xffff, mx >> 16));
         float s = scale_for(from16<BF16>(mx));
         if (!fresh) {
-            const float old = *scale;
             if (old > s) s = old;
             if (s != old) {                            // every row of the block under the new scale
                 const float ratio = old / s;
@@ -263,17 +276,16 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
             }
         }
         const float inv = s > 0.0f ? 1.0f / s : 0.0f;
-        for (int base = 0; base < n; base += 64) {
-            if (n > 64) load(base);
+        for (int base = 0; base < n; base += ROWS) {
+            if (n > ROWS) load(base);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
+            for (int k = 0; k < ROWS / 4; ++k) {
                 const int row = base + 4 * k + sub;
                 if (base + 4 * k < n && row < n) {
-                    const uint32_t *p = &x[k].x;
                     int v[2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint32_t lo = p[2 * j], hi = p[2 * j + 1];
+                        const uint32_t lo = x[k][2 * j], hi = x[k][2 * j + 1];
                         v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(lo & 0xffff) * inv, from16<BF16>(lo >> 16) * inv, 0, false);
                         v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(hi & 0xffff) * inv, from16<BF16>(hi >> 16) * inv, v[j], true);
                     }
@@ -293,15 +305,20 @@ int launch_quantize_blk(const minikv_blk_shape &s, int32_t n_tok, const void *K,
     a.X[0] = (const uint16_t *)K, a.X[1] = (const uint16_t *)V, a.stride[0] = k_stride, a.stride[1] = v_stride;
     a.codes[0] = c.K, a.codes[1] = c.V, a.scales[0] = c.Ks, a.scales[1] = c.Vs, a.slots = slots;
     a.n_tok = n_tok, a.Hkv = s.Hkv, a.shift = __builtin_ctz(s.block), a.rows = s.n_blocks * s.block;
-    // A wave per token while that is what the compute units can hold at once (a step of single tokens, each a run of its
-    // own); else a wave per 16 tokens, the smallest block, most of them with at most one run to begin.
-    const bool single = (int64_t)n_tok * s.Hkv * 2 <= 16 * 4 * kComputeUnits;
-    const int chunk = single ? 1 : 16;
-    const dim3 grid((unsigned)(((int64_t)n_tok + 4 * chunk - 1) / (4 * chunk)), (unsigned)s.Hkv, 2);
-    if (single && s.dtype == MINIKV_BF16) hipLaunchKernelGGL((quantize_blk_kernel<1, true>), grid, dim3(256), 0, st, a);
-    else if (single) hipLaunchKernelGGL((quantize_blk_kernel<1, false>), grid, dim3(256), 0, st, a);
-    else if (s.dtype == MINIKV_BF16) hipLaunchKernelGGL((quantize_blk_kernel<16, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((quantize_blk_kernel<16, false>), grid, dim3(256), 0, st, a);
+    // A wave takes about as many tokens as a run has, a request's share of them or a block's worth: one each in a decoding step,
+    // whose runs are single tokens, and few waves without a run of their own for prompts.
+    const int64_t heads = 2 * (int64_t)s.Hkv;
+    const int run = s.block < 64 ? s.block : 64, share = n_tok / s.R;
+    a.chunk = share < 1 ? 1 : share < run ? share : run;
+    fast_div_setup((uint32_t)heads, a.heads_magic, a.heads_shift);
+    const int64_t waves = ((int64_t)n_tok + a.chunk - 1) / a.chunk * heads;
+    if (waves > 0x7fffffff) return MINIKV_EINVAL;
+    const dim3 grid((unsigned)((waves + 3) / 4));
+    const bool bf16 = s.dtype == MINIKV_BF16;
+    if (s.block <= 64 && bf16) hipLaunchKernelGGL((quantize_blk_kernel<64, true>), grid, dim3(256), 0, st, a);
+    else if (s.block <= 64) hipLaunchKernelGGL((quantize_blk_kernel<64, false>), grid, dim3(256), 0, st, a);
+    else if (bf16) hipLaunchKernelGGL((quantize_blk_kernel<128, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((quantize_blk_kernel<128, false>), grid, dim3(256), 0, st, a);
     return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
 }
 
