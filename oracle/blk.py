@@ -1,6 +1,6 @@
 """Plain definitions of the operators over packed prompts and the paged 8-bit cache, in 64 bits and request by request
-(test infrastructure only): written from include/minikv.h, sharing nothing with the library.  Tensors are torch CPU tensors,
-codes are uint8."""
+(test infrastructure only): written from include/minikv.h, sharing nothing with the library.  Codes are uint8; tensors are CPU
+tensors (prompt_attn takes them anywhere)."""
 import math
 
 import torch
@@ -132,13 +132,13 @@ def prompt_attn(Q, K, V, cu, sm):
     """X_O, LSE, A_cumul of packed prompts (LSE and A_cumul laid out prompt by prompt, a row per head), and as above."""
     T, Hq, D = Q.shape
     rep = Hq // K.shape[1]
-    X, mean = torch.zeros(T, Hq, D, dtype=torch.float64), torch.zeros(T, Hq, D, dtype=torch.float64)
-    lse, A, score = torch.zeros(T * Hq, dtype=torch.float64), torch.zeros(T * Hq, dtype=torch.float64), 0.0
+    zeros = lambda *n: torch.zeros(*n, dtype=torch.float64, device=Q.device)  # noqa: E731  (products in 64 bits wherever the inputs are)
+    X, mean, lse, A, score = zeros(T, Hq, D), zeros(T, Hq, D), zeros(T * Hq), zeros(T * Hq), 0.0
     for a, e in zip(cu[:-1], cu[1:]):
         n = e - a
         if n == 0:
             continue
-        later = torch.ones(n, n, dtype=torch.bool).triu(1)
+        later = torch.ones(n, n, dtype=torch.bool, device=Q.device).triu(1)
         for h in range(Hq):
             q, k, v = Q[a:e, h].double(), K[a:e, h // rep].double(), V[a:e, h // rep].double()
             x = (q @ k.t() * sm).masked_fill(later, -math.inf)

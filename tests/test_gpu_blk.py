@@ -70,6 +70,14 @@ def test_assignment_equals_the_definition(api, R, block, width, hi, new, n_slots
             assert got[k] == want[k], k
 
 
+@pytest.mark.parametrize("new", [8, 9])
+def test_assignment_of_few_rows_each_and_of_one_more(api, new):
+    """Up to eight new rows a request are written by the request's own thread, more by a search: the same numbers."""
+    for R, n_slots in ((1, 9), (70, 700), (1500, 20000), (3000, 900)):
+        st = assign_state(R, 16, 20, 200, new, lambda rng, h: rng.choice([0, 1, new]), free=0.9)
+        assert run_assign(api, *st, 16, n_slots) == blk.assign(*st, 16, n_slots)
+
+
 def test_assignment_refuses_by_table_slots_and_pool(api):
     st = ([15, 32, 0, 0, 10], [2, 1, 3, 40, 30], [[0, -1], [1, 2], [-1, -1], [-1, -1], [3, -1]], [7, 8, 9, 4, 5, 6], [4, 3])
     for n_slots in (0, 5, 6, 46, 76, 200):
@@ -244,6 +252,25 @@ def test_long_and_many_requests(api):
     attend(api, [9000, 33], 8, 2, 128, BF16)
     attend(api, [i % 90 for i in range(700)], 2, 1, 16, F16)          # several units a workgroup, empty ones between
     attend(api, [3000] * 9 + [1] * 9, 8, 4, 32, BF16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("Hq,Hkv,block", [(1, 1, 16), (3, 1, 64), (8, 1, 128), (16, 8, 32)])
+def test_the_line_of_work(api, dtype, Hq, Hkv, block):
+    """More units than workgroups: waves with several units, units over many waves and workgroups, merged by the last one."""
+    few = max(300 // Hkv, 40)
+    attend(api, [9000, 5000 // Hkv] + [10, 0, 70] * (few // 3) + [3000 // Hkv], Hq, Hkv, block, dtype)
+    attend(api, [64] * few + [12000 // Hkv, 1], Hq, Hkv, block, dtype, seed=4)
+
+
+@pytest.mark.parametrize("Hq,Hkv,lens,block", [
+    (8, 8, [512], 16), (8, 8, [513], 16), (4, 1, [700, 30], 32), (5, 1, [1100, 1000, 900], 64), (8, 1, [4097], 128), (2, 2, [9000, 100], 16),
+    (7, 1, [16000], 64), (32, 32, [300] * 8, 16),
+])
+def test_workgroups_shared_out_to_units(api, Hq, Hkv, lens, block):
+    """Few units: one workgroup each up to eight tiles, several beyond, whose results meet by ticket."""
+    attend(api, lens, Hq, Hkv, block, F16)
+    attend(api, lens, Hq, Hkv, block, BF16, seed=9)
 
 
 def test_requests_without_tokens_and_wide_tables(api):

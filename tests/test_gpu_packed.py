@@ -52,19 +52,19 @@ def check(api, lens, Hq, Hkv, dtype, scores=True, seed=1, gain=1.0, pad=0, max_l
         for x in (Q, K, V):
             x[cu[-1]:] = float("nan")
     X, lse, A = run(api, Q, K, V, cu, scores, max_len, sm, fill=7.0)
-    X0, lse0, A0, mean, score = blk.prompt_attn(Q.cpu(), K.cpu(), V.cpu(), cu, sm)
+    X0, lse0, A0, mean, score = blk.prompt_attn(Q, K, V, cu, sm)
     n, m = cu[-1], cu[-1] * Hq
     assert bool((X[n:] == 7.0).all()) and bool((lse[m:] == 7.0).all())
     tol = attn_tolerance(X0, mean, score, max(lens), float(V[:n].abs().max()), HALF[dtype], dtype)
-    err = (X.cpu().double() - X0).abs()
+    err = (X.double() - X0).abs()
     assert bool((err <= tol)[:n].all()), (float(err[:n].max()), float((err / tol)[:n].max()))
     ltol = lse_tolerance(lse0, score)
-    err = (lse.cpu().double() - lse0).abs()[:m]
+    err = (lse.double() - lse0).abs()[:m]
     assert bool((err <= ltol[:m]).all()), float((err / ltol[:m]).max())
     if scores:
         # a weight exp(score - LSE): the errors of both, its own rounding, and a half step per addition of up to L of them
         rel = 137 * 2.0 ** -24 * score * 1.01 + float(ltol.max()) + (max(lens) / 64 + 70) * 2.0 ** -24
-        err = (A.cpu().double() - A0).abs()[:m]
+        err = (A.double() - A0).abs()[:m]
         assert bool((A[m:] == 7.0).all()) and bool((err <= (A0 * rel + 1e-30)[:m]).all()), float((err / (A0 * rel + 1e-30)[:m]).max())
     again = run(api, Q, K, V, cu, scores, max_len, sm, fill=7.0)
     assert torch.equal(again[0].view(torch.int16)[:n], X.view(torch.int16)[:n]) and torch.equal(again[1][:m], lse[:m])
@@ -86,6 +86,21 @@ def test_long_prompts(api, dtype):
     check(api, [1500, 40, 2100], 2, 1, dtype)
     check(api, [4200], 2, 2, dtype)
     check(api, [600, 1030, 1, 300], 32, 8, dtype)
+
+
+# One shape for each form of the two passes (the rules go by the longest prompt and the number of blocks): queries per workgroup, sets of
+# waves, buffers, heads of a KV head side by side in 1, 2, 4 and 8.
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("Hq,Hkv,lens,form", [
+    (64, 8, [4100, 70], "256 queries, eight heads side by side"), (72, 24, [4200], "256 queries"), (8, 4, [3000, 3001], "128 queries, two sets"),
+    (16, 16, [1030, 900], "64 queries, two sets, one buffer"), (24, 3, [400, 100, 450], "64 queries, two sets, one buffer, two heads side by side"),
+    (4, 2, [500, 97], "64 queries, two sets, two buffers"), (32, 8, [700, 300, 1, 900, 33], "128 queries, four heads side by side"),
+    (32, 16, [600, 1000, 500], "128 queries, two heads side by side"), (40, 8, [100, 90, 128, 3, 0, 64], "prompts of one block"),
+    (33, 11, [200, 300, 90], "128 queries"),
+])
+def test_every_form(api, dtype, Hq, Hkv, lens, form):
+    check(api, lens, Hq, Hkv, dtype, seed=len(form))
+    check(api, lens, Hq, Hkv, dtype, scores=False, seed=len(form) + 1)
 
 
 def test_many_prompts(api):
