@@ -506,7 +506,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         hand_over();
     }
     if constexpr (WHOLE_ROWS) {
-        constexpr int kPart = WAVES == 8 ? 8 : 16;     // rows at a time
+        constexpr int kPart = 16;                      // rows at a time
         char *stage = (char *)tiles + wave * (kPart * 256);
         hand_over();                                   // (every wave has read the last tile)
         if (g == 0 && query < L) a.lse[stat + query] = lse2 * kLn2;
@@ -860,18 +860,17 @@ static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
         return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
     }
     // Which form, by the rules for prompts of one length (launch_prefill) with the longest prompt as the length and an upper
-    // bound of the blocks, which is what the host knows.
+    // bound of the blocks, which is what the host knows; but never 256 queries a workgroup, which gains nothing where four heads side
+    // by side share the keys and loses elsewhere (8 prompts of 16000 tokens, 32 heads each with keys of its own, 521 against 545 us).
     const int64_t heads = (int64_t)a.B * a.Hq;
     auto blocks = [&](int rows) { return a.Hq * per_head(rows); };
     const bool two_buffers = a.max_len > 96 && 2 * blocks(64) <= (heads <= 20 ? 3 : 2) * kComputeUnits;
     const bool two_sets_64 = two_buffers || (a.max_len > 384 && blocks(64) <= 2 * kComputeUnits);
     const bool two_sets_128 = a.max_len >= 1024 && heads <= 32 && 2 * blocks(128) <= (heads <= 20 ? 4 : 3) * kComputeUnits;
-    const int waves = a.max_len >= 4096 && blocks(256) >= 4 * kComputeUnits ? 8 : two_sets_64 ? 2 : 4;
-    while (a.side < 3 && (2 << a.side) <= waves && a.rep % (2 << a.side) == 0) ++a.side;
+    const int waves = two_sets_64 ? 2 : 4;
+    while ((2 << a.side) <= waves && a.rep % (2 << a.side) == 0) ++a.side;
     const dim3 grid((unsigned)(per_head(32 * waves >> a.side) * (a.Hq >> a.side)));
-    if (waves == 8)
-        hipLaunchKernelGGL((prefill_fwd_kernel<8, 1, 2, false, true, BF16>), grid, dim3(512), fwd_lds_bytes(1, 2), st, a);
-    else if (two_sets_64 && !two_buffers)
+    if (two_sets_64 && !two_buffers)
         hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 1, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 1), st, a);
     else if (two_sets_64)
         hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 2), st, a);

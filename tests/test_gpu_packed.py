@@ -89,10 +89,10 @@ def test_long_prompts(api, dtype):
 
 
 # One shape for each form of the two passes (the rules go by the longest prompt and the number of blocks): queries per workgroup, sets of
-# waves, buffers, heads of a KV head side by side in 1, 2, 4 and 8.
+# waves, buffers, heads of a KV head side by side in 1, 2 and 4.
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("Hq,Hkv,lens,form", [
-    (64, 8, [4100, 70], "256 queries, eight heads side by side"), (72, 24, [4200], "256 queries"), (8, 4, [3000, 3001], "128 queries, two sets"),
+    (64, 8, [4100, 70], "128 queries, four of eight heads side by side"), (72, 24, [4200], "128 queries, many blocks"), (8, 4, [3000, 3001], "128 queries, two sets"),
     (16, 16, [1030, 900], "64 queries, two sets, one buffer"), (24, 3, [400, 100, 450], "64 queries, two sets, one buffer, two heads side by side"),
     (4, 2, [500, 97], "64 queries, two sets, two buffers"), (32, 8, [700, 300, 1, 900, 33], "128 queries, four heads side by side"),
     (32, 16, [600, 1000, 500], "128 queries, two heads side by side"), (40, 8, [100, 90, 128, 3, 0, 64], "prompts of one block"),
