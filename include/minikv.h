@@ -251,7 +251,7 @@ int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, con
  * ([Hq or Hkv][128], contiguous), tokens are `stride` elements apart: a slice of a fused projection is taken as it is.
  * Strides are multiples of 8 elements, at most 2^23, pointers 16-byte aligned.  Inputs must be finite.
  * Shape rules: D == 128; block in {16, 32, 64, 128}; Hq % Hkv == 0 and Hq / Hkv <= 8; 1 <= R <= 8192; Hkv <= 65535;
- * n_blocks * block and R * Hkv * (max_blocks * block / 64 + 1) < 2^31; max_blocks * block <= 2^30. */
+ * n_blocks * block and R * Hkv * (max_blocks * block / 64 + 2) < 2^31; max_blocks * block <= 2^30. */
 typedef enum { MINIKV_F16 = 0, MINIKV_BF16 = 1 } minikv_dtype;
 
 typedef struct minikv_blk_shape {

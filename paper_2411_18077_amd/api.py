@@ -368,11 +368,22 @@ def _stride(x, heads):
     return t if n > 1 else heads * 128                 # (one token: any stride will do)
 
 
-def _need(t, dtype, n, name):
-    """What a raw pointer does not tell the library: the type, and that n elements lie one behind the other."""
-    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
-        raise ValueError("%s: a contiguous tensor of at least %d %s is needed, got %s of %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
+def _home():
+    """The current GPU's index, which is where a call runs; None where no GPU is in use."""
+    return _device() if torch.cuda.is_initialized() else None
+
+
+def _here(t, home, name):
+    if t.get_device() != home:                         # (-1: host memory)
+        raise ValueError("%s is on %s, the call runs on %s" % (name, t.device, "no GPU" if home is None else "cuda:%d" % home))
     return t.data_ptr()
+
+
+def _need(t, dtype, n, name, home):
+    """What a raw pointer does not tell the library: the type, that n elements lie one behind the other, and where."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s: a contiguous tensor of at least %d %s is needed, got %s of %s" % (name, n, dtype, t.dtype, tuple(t.shape)))
+    return _here(t, home, name)
 
 
 def make_blk_shape(R, Hq, Hkv, D, block, n_blocks, max_blocks, dtype):
@@ -392,64 +403,79 @@ class BlkCache:
         if K is not None:
             device = K.device
         rows = (shape.n_blocks, shape.Hkv)
-        e4m3 = torch.float8_e4m3fn
-        self.K = torch.zeros(rows + (shape.block, 128), dtype=torch.uint8, device=device).view(e4m3) if K is None else K
-        self.V = torch.zeros(rows + (shape.block, 128), dtype=torch.uint8, device=device).view(e4m3) if V is None else V
-        self.Ks = torch.zeros(rows, dtype=torch.float32, device=device) if Ks is None else Ks
-        self.Vs = torch.zeros(rows, dtype=torch.float32, device=device) if Vs is None else Vs
-        self._c = MinikvBlkCache(_need(self.K, e4m3, codes, "K"), _need(self.V, e4m3, codes, "V"),
-                                 _need(self.Ks, torch.float32, scales // 4, "Ks"), _need(self.Vs, torch.float32, scales // 4, "Vs"))
+        e4m3, f32 = torch.float8_e4m3fn, torch.float32
+
+        def made(t, size, dtype, n, name):
+            if t is None:
+                return torch.zeros(size, dtype=torch.uint8 if dtype is e4m3 else dtype, device=device).view(dtype)
+            _need(t, dtype, n, name, torch.empty(0, device=device).get_device())
+            return t
+        self._t = (made(K, rows + (shape.block, 128), e4m3, codes, "K"), made(V, rows + (shape.block, 128), e4m3, codes, "V"),
+                   made(Ks, rows, f32, scales // 4, "Ks"), made(Vs, rows, f32, scales // 4, "Vs"))
+        self._c = MinikvBlkCache(*(t.data_ptr() for t in self._t))
         self.workspace = torch.zeros(int(lib().minikv_blk_workspace_bytes(C.byref(shape))), dtype=torch.uint8, device=device)   # zeroed once
+
+    K, V, Ks, Vs = (property(lambda self, i=i: self._t[i]) for i in range(4))          # (not to be replaced: the pointers are kept)
 
     def c(self):
         return self._c
 
 
+def _fits(shape, cache, home):
+    """The cache's buffers are big enough for the shape, and here."""
+    own = cache.shape
+    if own is not shape and (own.n_blocks < shape.n_blocks or own.Hkv != shape.Hkv or own.block != shape.block):
+        raise ValueError("the cache is one of %d blocks of %d tokens and %d heads" % (own.n_blocks, own.block, own.Hkv))
+    _here(cache.K, home, "the cache")
+    return C.byref(cache.c())
+
+
 def kv_assign_blk(shape, q_len, n_new, table, ring, ring_state, q_len_next, ring_state_next, cu, slots, stream=None):
-    i32, R = torch.int32, shape.R
-    _check(lib().kv_assign_blk(C.byref(shape), _need(q_len, i32, R, "q_len"), _need(n_new, i32, R, "n_new"),
-                               _need(table, i32, R * shape.max_blocks, "table"), _need(ring, i32, shape.n_blocks, "ring"),
-                               _need(ring_state, i32, 2, "ring_state"), _need(q_len_next, i32, R, "q_len_next"),
-                               _need(ring_state_next, i32, 2, "ring_state_next"), _need(cu, i32, R + 1, "cu"),
-                               _need(slots, i32, 0, "slots"), slots.numel(), _stream(stream)), "kv_assign_blk")
+    i32, R, home = torch.int32, shape.R, _home()
+    _check(lib().kv_assign_blk(C.byref(shape), _need(q_len, i32, R, "q_len", home), _need(n_new, i32, R, "n_new", home),
+                               _need(table, i32, R * shape.max_blocks, "table", home), _need(ring, i32, shape.n_blocks, "ring", home),
+                               _need(ring_state, i32, 2, "ring_state", home), _need(q_len_next, i32, R, "q_len_next", home),
+                               _need(ring_state_next, i32, 2, "ring_state_next", home), _need(cu, i32, R + 1, "cu", home),
+                               _need(slots, i32, 0, "slots", home), slots.numel(), _stream(stream)), "kv_assign_blk")
 
 
-def _rows(x, dtype, heads, name):
+def _rows(x, dtype, heads, name, home):
     if DTYPES.get(x.dtype) != dtype:
         raise ValueError("%s: got %s" % (name, x.dtype))
-    return x.data_ptr(), _stride(x, heads)
+    return _stride(x, heads), _here(x, home, name)
 
 
 def kv_quantize_blk(shape, K, V, slots, cache, stream=None):
     """K, V: [tokens][Hkv][128], possibly slices of a fused projection; slots: one per token."""
-    n = K.shape[0]
+    n, home = K.shape[0], _home()
     if V.shape[0] != n:
         raise ValueError("K has %d tokens, V %d" % (n, V.shape[0]))
-    (k, ks), (v, vs) = _rows(K, shape.dtype, shape.Hkv, "K"), _rows(V, shape.dtype, shape.Hkv, "V")
-    _check(lib().kv_quantize_blk(C.byref(shape), n, k, ks, v, vs, _need(slots, torch.int32, n, "slots"), C.byref(cache.c()),
+    (ks, k), (vs, v) = _rows(K, shape.dtype, shape.Hkv, "K", home), _rows(V, shape.dtype, shape.Hkv, "V", home)
+    _check(lib().kv_quantize_blk(C.byref(shape), n, k, ks, v, vs, _need(slots, torch.int32, n, "slots", home), _fits(shape, cache, home),
                                  _stream(stream)), "kv_quantize_blk")
 
 
 def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspace=None, stream=None):
     """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous."""
-    (p, qs), ws = _rows(q, shape.dtype, shape.Hq, "q"), cache.workspace if workspace is None else workspace
+    home = _home()
+    (qs, p), ws = _rows(q, shape.dtype, shape.Hq, "q", home), cache.workspace if workspace is None else workspace
     if q.shape[0] < shape.R:
         raise ValueError("q has %d rows, the shape %d requests" % (q.shape[0], shape.R))
-    _check(lib().minikv_decode_attn_blk(C.byref(shape), p, qs, C.byref(cache.c()),
-                                        _need(table, torch.int32, shape.R * shape.max_blocks, "table"),
-                                        _need(q_len, torch.int32, shape.R, "q_len"), float(sm_scale),
-                                        _need(out, q.dtype, shape.R * shape.Hq * 128, "out"), ws.data_ptr(),
+    _check(lib().minikv_decode_attn_blk(C.byref(shape), p, qs, _fits(shape, cache, home),
+                                        _need(table, torch.int32, shape.R * shape.max_blocks, "table", home),
+                                        _need(q_len, torch.int32, shape.R, "q_len", home), float(sm_scale),
+                                        _need(out, q.dtype, shape.R * shape.Hq * 128, "out", home), _here(ws, home, "workspace"),
                                         ws.numel() * ws.element_size(), _stream(stream)), "minikv_decode_attn_blk")
 
 
 def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X_O, lse, A_cumul, stream=None):
     """Q: [T][Hq][128], K, V: [T][Hkv][128], possibly slices of a fused projection; X_O: contiguous; A_cumul may be None."""
-    dtype = DTYPES[Q.dtype]
-    (q, qs), (k, ks), (v, vs) = _rows(Q, dtype, Hq, "Q"), _rows(K, dtype, Hkv, "K"), _rows(V, dtype, Hkv, "V")
+    dtype, home = DTYPES.get(Q.dtype, -1), _home()
+    (qs, q), (ks, k), (vs, v) = _rows(Q, dtype, Hq, "Q", home), _rows(K, dtype, Hkv, "K", home), _rows(V, dtype, Hkv, "V", home)
     if min(Q.shape[0], K.shape[0], V.shape[0]) < T:
         raise ValueError("fewer than %d rows" % T)
     _check(lib().selective_flash_attn_packed(int(B), int(Hq), int(Hkv), int(T), int(max_len), dtype, q, qs, k, ks, v, vs,
-                                             _need(cu, torch.int32, B + 1, "cu"), float(sm_scale),
-                                             _need(X_O, Q.dtype, T * Hq * 128, "X_O"), _need(lse, torch.float32, T * Hq, "lse"),
-                                             None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul"),
+                                             _need(cu, torch.int32, B + 1, "cu", home), float(sm_scale),
+                                             _need(X_O, Q.dtype, T * Hq * 128, "X_O", home), _need(lse, torch.float32, T * Hq, "lse", home),
+                                             None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul", home),
                                              _stream(stream)), "selective_flash_attn_packed")

@@ -60,7 +60,7 @@ static int validate_blk(const minikv_blk_shape *s)
     if (s->n_blocks < 1 || s->max_blocks < 1) return MINIKV_EINVAL;
     const int64_t most = (int64_t)s->max_blocks * s->block;                            // tokens of a request
     if ((int64_t)s->n_blocks * s->block > 0x7fffffff || most > (1 << 30)) return MINIKV_EINVAL;
-    if ((int64_t)s->R * s->Hkv > 0x7fffffff / (most / kBlkTile + 1)) return MINIKV_EINVAL;
+    if ((int64_t)s->R * s->Hkv > 0x7fffffff / (most / kBlkTile + 2)) return MINIKV_EINVAL;
     return MINIKV_OK;
 }
 

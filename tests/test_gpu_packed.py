@@ -255,3 +255,45 @@ def test_a_serving_loop(api, dtype, block):
         want, mean, score = blk.decode_attn(last, Kc, cache.Ks.cpu(), Vc, cache.Vs.cpu(), table.cpu(), q_len.tolist(), SM)
         tol = attn_tolerance(want, mean, score, 300, 6.0, 2.0 ** -11, dtype)
         assert bool(((out.cpu().double() - want).abs() <= tol).all())
+
+
+def test_the_binding_refuses_on_the_gpu(api):
+    """What is checked behind the place of the first tensor: nothing is launched."""
+    Q, K, V = fused(10, 8, 2, BF16, 1)
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    f = torch.zeros(80, device="cuda")
+    good = dict(T=10, Q=Q, K=K, V=V, cu=i([0, 4, 10]), X=Q.contiguous(), lse=f, A=f.clone())
+    for bad in (dict(T=11), dict(Q=Q[:9]), dict(K=K[:9]), dict(V=V.half()), dict(cu=good["cu"][:2]), dict(cu=good["cu"].long()), dict(K=Q[:, ::4]),
+                dict(X=good["X"].half()), dict(X=Q), dict(lse=f[:79]), dict(lse=f.double()), dict(A=f[::2]), dict(V=V.cpu()), dict(A=f.cpu()),
+                dict(cu=good["cu"].cpu())):
+        a = {**good, **bad}
+        with pytest.raises(ValueError):
+            api.selective_flash_attn_packed(2, 8, 2, a["T"], 6, a["Q"], a["K"], a["V"], a["cu"], 0.1, a["X"], a["lse"], a["A"])
+    shape = api.make_blk_shape(4, 8, 2, 128, 32, 10, 5, BF16)
+    cache, n = api.BlkCache(shape), i([0] * 20)
+    x, q = K[:4], Q[:4]
+    for slots, V4, other in ((n[:3], V[:4], cache), (n.long(), V[:4], cache), (n, V[:4].cpu(), cache), (n.cpu(), V[:4], cache), (n, V[:3], cache),
+                             (n, V[:4], api.BlkCache(shape, device="cpu")),
+                             (n, V[:4], api.BlkCache(api.make_blk_shape(4, 8, 2, 128, 32, 9, 5, BF16))),
+                             (n, V[:4], api.BlkCache(api.make_blk_shape(4, 8, 2, 128, 64, 10, 5, BF16)))):
+        with pytest.raises(ValueError):
+            api.kv_quantize_blk(shape, x, V4, slots, other)
+    out = torch.zeros(4, 8, 128, dtype=BF16, device="cuda")
+    for q4, table, lens, o, ws in ((q[:3], n, n, out, None), (q, n[:19], n, out, None), (q, n, n[:3], out, None), (q, n, n, out[:, :4], None),
+                                   (q, n, n, out.half(), None), (q, n, n, out.cpu(), None), (q, n.cpu(), n, out, None), (q.half(), n, n, out, None),
+                                   (q, n, n, torch.zeros(8, 4, 128, dtype=BF16, device="cuda").transpose(0, 1), None),
+                                   (q, n, n, out, cache.workspace.cpu())):
+        with pytest.raises(ValueError):
+            api.minikv_decode_attn_blk(shape, q4, cache, table, lens, SM, o, workspace=ws)
+    with pytest.raises(api.MinikvError):
+        api.minikv_decode_attn_blk(shape, q, cache, n, n, SM, out, workspace=cache.workspace[:1024])
+    with pytest.raises(api.MinikvError):
+        api.kv_quantize_blk(shape, x[:1].expand(4, 2, 128), V[:4], n, cache)         # rows on top of each other
+    i9 = [i([0] * 20) for _ in range(9)]
+    for k in range(9):
+        for bad in (i9[0].long(), i9[0].cpu(), i9[0][::2]):
+            args = list(i9)
+            args[k] = bad
+            with pytest.raises(ValueError):
+                api.kv_assign_blk(shape, *args)
+    assert not bool(out.any()) and not bool(cache.K.view(torch.uint8).any())
