@@ -368,9 +368,12 @@ def _stride(x, heads):
     return t if n > 1 else heads * 128                 # (one token: any stride will do)
 
 
-def _home():
-    """The current GPU's index, which is where a call runs; None where no GPU is in use."""
-    return _device() if torch.cuda.is_initialized() else None
+def _home(stream):
+    """The current GPU's index, which is where a call runs (None where no GPU is in use), and the stream's handle."""
+    if not torch.cuda.is_initialized():
+        return None, 0 if stream is None else _stream(stream)
+    home = _device()
+    return home, _raw_stream(home) if stream is None else _stream(stream)
 
 
 def _here(t, home, name):
@@ -430,13 +433,18 @@ def _fits(shape, cache, home):
     return C.byref(cache.c())
 
 
+_ASSIGN = ("q_len", "n_new", "table", "ring", "ring_state", "q_len_next", "ring_state_next", "cu", "slots")
+
+
 def kv_assign_blk(shape, q_len, n_new, table, ring, ring_state, q_len_next, ring_state_next, cu, slots, stream=None):
-    i32, R, home = torch.int32, shape.R, _home()
-    _check(lib().kv_assign_blk(C.byref(shape), _need(q_len, i32, R, "q_len", home), _need(n_new, i32, R, "n_new", home),
-                               _need(table, i32, R * shape.max_blocks, "table", home), _need(ring, i32, shape.n_blocks, "ring", home),
-                               _need(ring_state, i32, 2, "ring_state", home), _need(q_len_next, i32, R, "q_len_next", home),
-                               _need(ring_state_next, i32, 2, "ring_state_next", home), _need(cu, i32, R + 1, "cu", home),
-                               _need(slots, i32, 0, "slots", home), slots.numel(), _stream(stream)), "kv_assign_blk")
+    i32, R, (home, st) = torch.int32, shape.R, _home(stream)
+    tensors = (q_len, n_new, table, ring, ring_state, q_len_next, ring_state_next, cu, slots)
+    sizes = (R, R, R * shape.max_blocks, shape.n_blocks, 2, R, 2, R + 1, 0)
+    for t, n in zip(tensors, sizes):                   # (_need written out: nine of them are half the call)
+        if t.dtype is not i32 or t.numel() < n or not t.is_contiguous() or t.get_device() != home:
+            for t, n, name in zip(tensors, sizes, _ASSIGN):
+                _need(t, i32, n, name, home)
+    _check(lib().kv_assign_blk(C.byref(shape), *[t.data_ptr() for t in tensors], slots.numel(), st), "kv_assign_blk")
 
 
 def _rows(x, dtype, heads, name, home):
@@ -447,17 +455,17 @@ def _rows(x, dtype, heads, name, home):
 
 def kv_quantize_blk(shape, K, V, slots, cache, stream=None):
     """K, V: [tokens][Hkv][128], possibly slices of a fused projection; slots: one per token."""
-    n, home = K.shape[0], _home()
+    n, (home, st) = K.shape[0], _home(stream)
     if V.shape[0] != n:
         raise ValueError("K has %d tokens, V %d" % (n, V.shape[0]))
     (ks, k), (vs, v) = _rows(K, shape.dtype, shape.Hkv, "K", home), _rows(V, shape.dtype, shape.Hkv, "V", home)
     _check(lib().kv_quantize_blk(C.byref(shape), n, k, ks, v, vs, _need(slots, torch.int32, n, "slots", home), _fits(shape, cache, home),
-                                 _stream(stream)), "kv_quantize_blk")
+                                 st), "kv_quantize_blk")
 
 
 def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspace=None, stream=None):
     """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous."""
-    home = _home()
+    home, st = _home(stream)
     (qs, p), ws = _rows(q, shape.dtype, shape.Hq, "q", home), cache.workspace if workspace is None else workspace
     if q.shape[0] < shape.R:
         raise ValueError("q has %d rows, the shape %d requests" % (q.shape[0], shape.R))
@@ -465,17 +473,17 @@ def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspa
                                         _need(table, torch.int32, shape.R * shape.max_blocks, "table", home),
                                         _need(q_len, torch.int32, shape.R, "q_len", home), float(sm_scale),
                                         _need(out, q.dtype, shape.R * shape.Hq * 128, "out", home), _here(ws, home, "workspace"),
-                                        ws.numel() * ws.element_size(), _stream(stream)), "minikv_decode_attn_blk")
+                                        ws.numel() * ws.element_size(), st), "minikv_decode_attn_blk")
 
 
 def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X_O, lse, A_cumul, stream=None):
     """Q: [T][Hq][128], K, V: [T][Hkv][128], possibly slices of a fused projection; X_O: contiguous; A_cumul may be None."""
-    dtype, home = DTYPES.get(Q.dtype, -1), _home()
+    dtype, (home, st) = DTYPES.get(Q.dtype, -1), _home(stream)
     (qs, q), (ks, k), (vs, v) = _rows(Q, dtype, Hq, "Q", home), _rows(K, dtype, Hkv, "K", home), _rows(V, dtype, Hkv, "V", home)
     if min(Q.shape[0], K.shape[0], V.shape[0]) < T:
         raise ValueError("fewer than %d rows" % T)
     _check(lib().selective_flash_attn_packed(int(B), int(Hq), int(Hkv), int(T), int(max_len), dtype, q, qs, k, ks, v, vs,
                                              _need(cu, torch.int32, B + 1, "cu", home), float(sm_scale),
                                              _need(X_O, Q.dtype, T * Hq * 128, "X_O", home), _need(lse, torch.float32, T * Hq, "lse", home),
-                                             None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul", home),
-                                             _stream(stream)), "selective_flash_attn_packed")
+                                             None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul", home), st),
+           "selective_flash_attn_packed")
