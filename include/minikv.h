@@ -237,7 +237,7 @@ int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, con
  * in 8-bit floating point (e4m3: 4 exponent and 3 mantissa bits, largest value 448) for keys and as many for
  * values, and ONE binary32 scale for each; a row stands for code * scale.  kv_quantize_blk makes every scale a
  * power of two, so that a block whose scale grows later keeps its codes' bits (its rows are only rounded again
- * where they become subnormal codes); the attention takes any finite non-negative scale.
+ * where they become subnormal codes); the attention takes any finite scale that is 0 or at least 2^-126.
  * Request r owns the blocks table[r][0], table[r][1], ...; its token i is row i % block of block
  * table[r][i / block], its SLOT is table[r][i / block] * block + i % block.  A block may stand in several tables
  * (a shared prefix) as long as nothing is filed into it.

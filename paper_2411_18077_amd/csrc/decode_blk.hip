@@ -409,10 +409,10 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
 
     const int units = a.R * a.Hkv;
     const int share = (int)fast_div((uint32_t)wg, a.units_magic, a.units_shift), unit = wg - share * units;      // a unit's workgroups are `units` apart
-    int r = (int)fast_div((uint32_t)unit, a.hkv_magic, a.hkv_shift), h = unit - r * a.Hkv, shares = 1;
+    int r = (int)fast_div((uint32_t)unit, a.hkv_magic, a.hkv_shift), h = unit - r * a.Hkv, log_shares = 0;
     bool by_unit = units <= (int)gridDim.x;
     int unit_len = 0, unit_t0 = 0, unit_t1 = 0, unit_first = 0;
-    if (by_unit) {                                     // (lengths, the table and the queries are requested together, as few units wait for)
+    if (by_unit) {                                     // (lengths and the table are requested together, as few units wait for)
         const int64_t most = (int64_t)a.width * BS;
         auto len_of = [&](int i) { return (int)min((int64_t)max(a.q_len[i], 0), most); };
         const int32_t *row = a.table + (int64_t)r * a.width;
@@ -425,11 +425,12 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
         }
         top = wave_max(top), sum = wave_sum_of(sum) * a.Hkv;
         if (top > kBkWaves)
-            while (shares * 4 < top && 2 * shares * units <= (int)gridDim.x) shares *= 2;
-        by_unit = (top + shares * kBkWaves - 1) / (shares * kBkWaves) <= sum / ((int)gridDim.x * kBkWaves) + kBkUnitTiles;
+            while ((4 << log_shares) < top && (2 * units << log_shares) <= (int)gridDim.x) ++log_shares;
+        by_unit = (top + (kBkWaves << log_shares) - 1) / (kBkWaves << log_shares) <= sum / ((int)gridDim.x * kBkWaves) + kBkUnitTiles;
         if (by_unit) {
-            if (share >= shares) return;               // (the whole workgroup)
-            const int nt = (unit_len + kBlkTile - 1) / kBlkTile, from = nt * share / shares, n = nt * (share + 1) / shares - from;
+            if (share >= 1 << log_shares) return;      // (the whole workgroup)
+            const int64_t nt = (unit_len + kBlkTile - 1) / kBlkTile;
+            const int from = (int)(nt * share >> log_shares), n = (int)(nt * (share + 1) >> log_shares) - from;
             const int each = n / kBkWaves, more = n % kBkWaves;        // (waves 0 .. 3 are on SIMDs of their own)
             unit_t0 = from + wave * each + min(wave, more), unit_t1 = unit_t0 + each + (wave < more);
             const int entry = entry_of(unit_t0);
@@ -485,12 +486,15 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
         len = uniform(lens[r]), c = uniform(before[r + 1] - before[r]), start = uniform(before[r] * a.Hkv) + h * c;
         t0 = max(x - start - kBkUnitCost, 0), t1 = min(end - start, c) - kBkUnitCost;
     };
-    if (!by_unit && x < end) {
+    auto request_at = [&](int x) {                     // the request that place x of the line belongs to (the last one that begins there)
         const int y = (int)fast_div((uint32_t)x, a.hkv_magic, a.hkv_shift);
-        r = 0;
+        int r = 0;
         for (int step = a.R > 1 ? 1 << (31 - __builtin_clz(a.R - 1)) : 0; step; step >>= 1)
             if (r + step < a.R && before[r + step] <= y) r += step;
-        r = uniform(r);
+        return uniform(r);
+    };
+    if (!by_unit && x < end) {
+        r = request_at(x);
         h = uniform((x - before[r] * a.Hkv) / (before[r + 1] - before[r]));
         locate(r, h, len, t0, t1, start, c);
         if (t0 < t1) first = a.table[(int64_t)r * a.width + min(entry_of(t0) + lane, a.width - 1)];
@@ -506,8 +510,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
             if (x < end) {
                 if (h2 == a.Hkv) {
                     h2 = 0, ++r2;
-                    while (before[r2 + 1] == before[r2]) ++r2;         // (x < end: there is one)
-                    r2 = uniform(r2);
+                    if (uniform(before[r2 + 1] - before[r2]) == 0) r2 = request_at(x);          // (requests without tokens between)
                 }
                 locate(r2, h2, len2, from2, to2, start2, c2);
                 if (from2 < to2) first2 = a.table[(int64_t)r2 * a.width + min(lane, a.width - 1)];
@@ -539,16 +542,16 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
     if (by_unit) {
         if (wave >= a.rep) return;                     // a wave per head from here on
         merge_slots(1, 2 * kBkWaves);
-        if (shares > 1) {
+        if (log_shares) {
             float *out = a.partials + (int64_t)2 * wg * kBlkPartial;
             if (lane == 0) st8(out + 2 * wave, M, L);
             st8(out + 2 * kMaxRep + wave * kD + 2 * lane, x0, x1);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // the stores are acknowledged before the ticket is taken
             int *counter = a.tickets + kBlkGroups + unit * kMaxRep + wave, ticket = 0;
             if (lane == 0) ticket = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (uniform(ticket) != shares - 1) return;
+            if (uniform(ticket) != (1 << log_shares) - 1) return;
             if (lane == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            merge_partials(wave, 0, 1, shares, [&](int k) { return 2 * (unit + k * units); });
+            merge_partials(wave, 0, 1, 1 << log_shares, [&](int k) { return 2 * (unit + k * units); });
         }
         write_out(r, h, wave);
         return;

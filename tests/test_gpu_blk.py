@@ -163,6 +163,16 @@ def test_filing_equals_the_definition(api, dtype, block, Hkv, lens, held):
     check_filed(api, Hkv, block, 40, prompt_slots(lens, block, 40, 3, held), dtype, seed=len(lens) + block)
 
 
+def test_filing_nothing(api):
+    shape = api.make_blk_shape(1, 2, 2, 128, 16, 3, 1, F16)
+    cache = api.BlkCache(shape)
+    x = torch.zeros(0, 2, 128, dtype=F16, device="cuda")
+    api.kv_quantize_blk(shape, x, x, torch.zeros(0, dtype=torch.int32, device="cuda"), cache)
+    x = torch.ones(5, 2, 128, dtype=F16, device="cuda")
+    api.kv_quantize_blk(shape, x, x, torch.full((5,), -1, dtype=torch.int32, device="cuda"), cache)          # padding alone
+    assert not bool(cache.K.view(torch.uint8).any()) and not bool(cache.Ks.any()) and not bool(cache.Vs.any())
+
+
 def test_filing_many_tokens_a_wave(api):
     """More tokens than the form of a wave per token takes: waves that begin several runs, runs across waves, padding."""
     slots = prompt_slots([700, 333, 16, 1, 1, 1, 50, 900], 16, 140, 7)
@@ -261,6 +271,7 @@ def test_the_line_of_work(api, dtype, Hq, Hkv, block):
     few = max(300 // Hkv, 40)
     attend(api, [9000, 5000 // Hkv] + [10, 0, 70] * (few // 3) + [3000 // Hkv], Hq, Hkv, block, dtype)
     attend(api, [64] * few + [12000 // Hkv, 1], Hq, Hkv, block, dtype, seed=4)
+    attend(api, [70, 0] + [0] * 2000 + [65, 1, 0, 0, 128], Hq, Hkv, block, dtype, seed=5)         # a padded batch
 
 
 @pytest.mark.parametrize("Hq,Hkv,lens,block", [
