@@ -151,7 +151,8 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
     if (few) {
         for (int64_t t = (int64_t)total[0] + gtid; t < a.n_slots; t += gsize) a.slots[t] = -1;
     } else {
-        for (int t = gtid; t < a.n_slots; t += gsize) {
+        for (int64_t at = gtid; at < a.n_slots; at += gsize) {
+            const int t = (int)at;
             int slot = -1;
             const int r = find(rows, a.R, t);
             if ((uint32_t)t < total[0] && !(need[r] & kRefused)) {

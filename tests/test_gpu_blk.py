@@ -95,6 +95,19 @@ def test_values_out_of_range_stay_inside_the_buffers(api):
     assert got["state"] == [0, 1] and got["q_len"][0] == 0
 
 
+def test_the_largest_slot_map(api):
+    """2^31 - 1 slots: the loop over them steps beyond what 32 bits hold."""
+    R, block, n = 3, 16, 2 ** 31 - 1
+    shape = api.make_blk_shape(R, 1, 1, 128, block, 40, 8, F16)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, ring = torch.zeros(R, 8, dtype=torch.int32, device="cuda"), torch.arange(40, dtype=torch.int32, device="cuda")
+    nxt, state, cu, slots = ints(0, 0, 0), ints(0, 0), ints(0, 0, 0, 0), torch.zeros(n, dtype=torch.int32, device="cuda")
+    api.kv_assign_blk(shape, ints(0, 0, 0), ints(20, 0, 30), table, ring, ints(0, 40), nxt, state, cu, slots)
+    assert nxt.tolist() == [20, 0, 30] and state.tolist() == [4, 36] and cu.tolist() == [0, 20, 20, 50]
+    assert slots[:50].tolist() == list(range(20)) + list(range(32, 62))
+    assert int(slots[50:].max()) == -1 and int(slots[50:].min()) == -1
+
+
 def test_assignment_captured_and_replayed_over_steps(api):
     """A decoding loop whose bookkeeping is one captured launch per parity: blocks go out, come back, and are handed out again."""
     R, block, width, N = 12, 16, 6, 40
