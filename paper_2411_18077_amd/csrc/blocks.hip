@@ -347,9 +347,12 @@ int launch_quantize_blk(const minikv_blk_shape &s, int32_t n_tok, const void *K,
     const int64_t heads = 2 * (int64_t)s.Hkv;
     const int run = s.block < 64 ? s.block : 64, share = n_tok / s.R;
     a.chunk = share < 1 ? 1 : share < run ? share : run;
+    // (a launch holds less than 2^26 waves: more tokens each where there are that many)
+    if (n_tok * heads > 0x7fffffff) return MINIKV_EINVAL;
+    const int least = (int)(n_tok * heads >> 25) + 1;
+    if (a.chunk < least) a.chunk = least < 64 ? least : 64;
     fast_div_setup((uint32_t)heads, a.heads_magic, a.heads_shift);
     const int64_t waves = ((int64_t)n_tok + a.chunk - 1) / a.chunk * heads;
-    if (waves > 0x7fffffff) return MINIKV_EINVAL;
     const dim3 grid((unsigned)((waves + 3) / 4));
     const bool bf16 = s.dtype == MINIKV_BF16;
     if (s.block <= 64 && bf16) hipLaunchKernelGGL((quantize_blk_kernel<64, true>), grid, dim3(256), 0, st, a);

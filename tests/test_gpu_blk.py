@@ -186,6 +186,22 @@ def test_filing_nothing(api):
     assert not bool(cache.K.view(torch.uint8).any()) and not bool(cache.Ks.any()) and not bool(cache.Vs.any())
 
 
+def test_filing_more_rows_than_waves_fit_a_launch(api):
+    """8192 requests' tokens of 4104 heads, K and V: 2^26 rows and more.  The last sixteen have a block."""
+    n, Hkv, block = 8192, 4104, 16
+    x = torch.zeros(n, Hkv, 128, dtype=F16, device="cuda")
+    x[-block:] = torch.randn(block, Hkv, 128, generator=torch.Generator().manual_seed(1)).half().cuda()
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slots[-block:] = torch.arange(block, 2 * block, dtype=torch.int32, device="cuda")
+    many, few = api.make_blk_shape(8192, Hkv, Hkv, 128, block, 2, 1, F16), api.make_blk_shape(1, Hkv, Hkv, 128, block, 2, 1, F16)
+    one, two = api.BlkCache(many), api.BlkCache(few)
+    api.kv_quantize_blk(many, x, x, slots, one)
+    api.kv_quantize_blk(few, x[-block:], x[-block:], slots[-block:], two)
+    assert bool((one.Ks[1] > 0).all()) and not bool(one.Ks[0].any())
+    for a, b in ((one.K, two.K), (one.V, two.V), (one.Ks, two.Ks), (one.Vs, two.Vs)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def test_filing_many_tokens_a_wave(api):
     """More tokens than the form of a wave per token takes: waves that begin several runs, runs across waves, padding."""
     slots = prompt_slots([700, 333, 16, 1, 1, 1, 50, 900], 16, 140, 7)

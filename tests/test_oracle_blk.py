@@ -140,6 +140,7 @@ def test_paged_sizes_and_arguments_are_checked_on_the_host(api):
     assert calls(api, shape, ["assign"], nxt=P(0x1000)) == [-1]                      # lengths read and written at one place
     assert calls(api, shape, ["assign"], n_slots=-1) == [-1] and calls(api, shape, ["file"], n_tok=-1) == [-1]
     assert l.kv_quantize_blk(C.byref(shape), 0, None, 0, None, 0, None, C.byref(api.MinikvBlkCache(*[0x1000] * 4)), None) == 0
+    assert calls(api, shape, ["file"], n_tok=1 << 29) == [-1]                        # 2^30 rows of K and as many of V
 
 
 def test_the_binding_refuses_what_a_pointer_does_not_tell(api):
