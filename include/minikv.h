@@ -329,7 +329,8 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  *   X_O      fp16 / bf16 [T][Hq][128], contiguous                                 (device, written)
  *   lse, A_cumul  fp32 [T * Hq], A_cumul or NULL: the values of prompt b, of length n, are the n * Hq ones from cu[b] * Hq
  *            on, a row of n for each query head -- what kv_select_hh_rw takes for that prompt as it is  (device, written)
- * dtype a minikv_dtype, max_len <= 2^23, T * Hq < 2^31, strides <= 2^23, sm_scale finite and > 0.  T == 0 is no error and
+ * dtype a minikv_dtype, max_len <= 2^23, T * Hq < 2^31, (min(T / 128 + B, T) + 1) * Hq < 2^24, strides <= 2^23, sm_scale finite
+ * and > 0.  T == 0 is no error and
  * writes nothing. */
 int selective_flash_attn_packed(int32_t B, int32_t Hq, int32_t Hkv, int32_t T, int32_t max_len, int32_t dtype,
                                 const void *Q, int64_t q_stride, const void *K, int64_t k_stride, const void *V,

@@ -848,12 +848,13 @@ int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f
 template <bool BF16>
 static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
 {
-    // workgroups of `rows` rows per head, at most: a prompt's last block may be a part of one
+    // workgroups of `rows` rows per head, at most: a prompt's last block may be a part of one, none is empty
     auto per_head = [&](int rows) {
         const int64_t by_rows = a.T / rows + a.B, by_prompt = (int64_t)a.B * ((a.max_len + rows - 1) / rows);
-        return by_rows < by_prompt ? by_rows : by_prompt;
+        const int64_t most = by_rows < by_prompt ? by_rows : by_prompt;
+        return most < a.T ? most : a.T;
     };
-    if (per_head(32) * a.Hq > 0x7fffffff) return MINIKV_EINVAL;
+    if ((per_head(128) + 1) * a.Hq > 0xffffff) return MINIKV_EINVAL;   // (a launch holds less than 2^32 work-items; heads side by side round up once a head)
     if (scores && a.max_len <= 128) {
         hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, true, true, BF16>), dim3((unsigned)(per_head(128) * a.Hq)), dim3(256),
                            fwd_lds_bytes(1, 2, 128), st, a);

@@ -183,6 +183,7 @@ def test_packed_prompt_arguments_are_checked_on_the_host(api):
                 dict(lse=P(0x1001)), dict(A=P(0x1002)), dict(sm=0.0), dict(sm=-1.0), dict(sm=math.nan), dict(sm=math.inf), dict(qs=1020),
                 dict(qs=1016), dict(ks=128), dict(vs=252), dict(vs=-256), dict(qs=(1 << 23) + 8)):
         assert call(**bad) == -1, bad
+    assert call(B=8192, T=8192, max_len=9, Hq=4096, Hkv=4096, qs=4096 * 128, ks=4096 * 128, vs=4096 * 128) == -1      # too large a launch
     assert call(dtype=2) == -2 and call(dtype=-1) == -2
     assert call(T=0, Q=None, K=None, V=None, X=None, lse=None) == 0 and call(max_len=0) == 0                 # no rows
 
