@@ -391,6 +391,8 @@ def _need(t, dtype, n, name, home):
 
 def make_blk_shape(R, Hq, Hkv, D, block, n_blocks, max_blocks, dtype):
     """dtype: torch.float16 or torch.bfloat16, of queries, keys, values and outputs."""
+    if dtype not in DTYPES:
+        raise ValueError("rows are torch.float16 or torch.bfloat16: got %s" % dtype)
     return MinikvBlkShape(R, Hq, Hkv, D, block, n_blocks, max_blocks, DTYPES[dtype])
 
 
@@ -469,6 +471,8 @@ def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspa
     (qs, p), ws = _rows(q, shape.dtype, shape.Hq, "q", home), cache.workspace if workspace is None else workspace
     if q.shape[0] < shape.R:
         raise ValueError("q has %d rows, the shape %d requests" % (q.shape[0], shape.R))
+    if not ws.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor is needed")
     _check(lib().minikv_decode_attn_blk(C.byref(shape), p, qs, _fits(shape, cache, home),
                                         _need(table, torch.int32, shape.R * shape.max_blocks, "table", home),
                                         _need(q_len, torch.int32, shape.R, "q_len", home), float(sm_scale),

@@ -282,7 +282,7 @@ def test_the_binding_refuses_on_the_gpu(api):
     for q4, table, lens, o, ws in ((q[:3], n, n, out, None), (q, n[:19], n, out, None), (q, n, n[:3], out, None), (q, n, n, out[:, :4], None),
                                    (q, n, n, out.half(), None), (q, n, n, out.cpu(), None), (q, n.cpu(), n, out, None), (q.half(), n, n, out, None),
                                    (q, n, n, torch.zeros(8, 4, 128, dtype=BF16, device="cuda").transpose(0, 1), None),
-                                   (q, n, n, out, cache.workspace.cpu())):
+                                   (q, n, n, out, cache.workspace.cpu()), (q, n, n, out, torch.cat([cache.workspace] * 2)[::2])):
         with pytest.raises(ValueError):
             api.minikv_decode_attn_blk(shape, q4, cache, table, lens, SM, o, workspace=ws)
     with pytest.raises(api.MinikvError):

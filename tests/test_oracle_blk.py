@@ -169,6 +169,8 @@ def test_the_binding_refuses_what_a_pointer_does_not_tell(api):
         api.minikv_decode_attn_blk(shape, q, cache, i, i, 0.1, q.clone(), stream=0)
     with pytest.raises(ValueError, match="K: a contiguous"):
         api.BlkCache(shape, K=cache.K[:5], V=cache.V, Ks=cache.Ks, Vs=cache.Vs)
+    with pytest.raises(ValueError, match="float16 or torch.bfloat16"):
+        api.make_blk_shape(4, 8, 2, 128, 32, 10, 5, torch.float32)
     with pytest.raises(ValueError, match="invalid shape"):
         api.BlkCache(api.make_blk_shape(4, 8, 3, 128, 32, 10, 5, torch.float16), device="cpu")
 
