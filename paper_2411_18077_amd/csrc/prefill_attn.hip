@@ -209,9 +209,9 @@ __device__ __forceinline__ half4 read_transposed(const _Float16 *p)
 // scores once more, as S = Q K^T with the Q rows it still holds, so that a lane adds up one key's weights; the waves' sums
 // meet in LDS.  What bounds short prompts is the launch and its two round trips to memory, and a second one repeats them:
 // 8 heads x 48 tokens 9.8 -> 6.7 us, 8 x 128 13.3 -> 10.2, 1024 x 64 26.7 -> 21.4, 2048 x 128 95.6 -> 71.7.
-constexpr unsigned fwd_lds_bytes(int split, int buffers, int scored_queries = 0)
+constexpr unsigned fwd_lds_bytes(int split, int buffers, int scored_queries = 0, int more_tiles = 0)
 {
-    return split * 2 * buffers * kPfTile * sizeof(_Float16) + scored_queries * (1 + scored_queries / 32) * sizeof(float);
+    return (split * 2 * buffers + more_tiles) * kPfTile * sizeof(_Float16) + scored_queries * (1 + scored_queries / 32) * sizeof(float);
 }
 
 template <int WAVES, int SPLIT, int BUF, bool SCORES, bool PACKED = false, bool BF16 = false>
@@ -221,6 +221,7 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     // Many workgroups of packed prompts: outputs go through local memory, a few rows of the wave at a time, so that rows are stored
     // whole.  16 bytes of 32 rows an instruction are 512 requests a wave, and those are what short prompts wait for (64 prompts of up to
     // 320 tokens 52 -> 47 us, 16 of up to 1000 143 -> 136); where a launch is a workgroup or two deep the exchange costs 0.3 us.
+    // The queries come the same way, whole rows straight to local memory with the first tiles (47.9 -> 45.7, 138.5 -> 136.7).
     constexpr bool WHOLE_ROWS = PACKED && SPLIT == 1 && !SCORES;
     extern __shared__ __align__(16) _Float16 tiles[];
 
@@ -254,7 +255,17 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int q0 = qb * rows + (wave >> side) * 32;    // first query of this wave
     const int query = q0 + r;                          // this lane's query column
     half8 qf[8];                                       // B operand of S^T = K Q^T: Q[query][16 ks + 8 g ..]
-    {
+    _Float16 *q_rows = tiles + 3 * kPfTile + wave * 32 * kPfD;         // WHOLE_ROWS: the second V buffer, not in use before step 0, and as much behind it
+    if constexpr (WHOLE_ROWS) {
+        const int row0 = min(q0, L - 1), end = min(L - 1 - row0, 31) * (int)q_pitch + 240;
+        const char *first = (const char *)(Qh + (long)row0 * (q_pitch / 2));
+        const unsigned lds = lds_offset(q_rows);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = 4 * i + (lane >> 4);       // (chunks as in a K tile; rows past the prompt are those of columns that nobody stores)
+            load_to_lds(first, (unsigned)min(row * (int)q_pitch + (((lane & 15) ^ (row & 15)) << 4), end), lds + i * 1024u);
+        }
+    } else {
         const _Float16 *qp = Qh + (long)min(query, L - 1) * (q_pitch / 2) + g * 8;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(qp + ks * 16);
@@ -417,6 +428,10 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     if (BUF == 2) request(Kh, 1, false);
     request(Vh, 0, true);
     hand_over();                                       // (the Q rows have arrived as well)
+    if constexpr (WHOLE_ROWS) {
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(q_rows + k_place[ks]);
+    }
     float16v sa[2], sb[2];
     if (SPLIT == 1 || mytiles > 0) {                   // (the second set may have nothing for the first rows)
 #pragma unroll
@@ -878,7 +893,7 @@ static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
     else if (two_sets_128)
         hipLaunchKernelGGL((prefill_fwd_kernel<4, 2, 2, false, true, BF16>), grid, dim3(512), fwd_lds_bytes(2, 2), st, a);
     else
-        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(1, 2), st, a);
+        hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(1, 2, 0, 1), st, a);
     if (hipGetLastError() != hipSuccess) return MINIKV_ELAUNCH;
     if (!scores) return MINIKV_OK;
     if (blocks(64) <= (heads <= 20 ? 2 : 1) * kComputeUnits)
