@@ -220,9 +220,10 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     constexpr int kRows = kPfN / WAVES, kLoads = kRows / 4;     // rows of a tile one wave loads, four per instruction
     // Many workgroups of packed prompts: outputs go through local memory, a few rows of the wave at a time, so that rows are stored
     // whole.  16 bytes of 32 rows an instruction are 512 requests a wave, and those are what short prompts wait for (64 prompts of up to
-    // 320 tokens 52 -> 47 us, 16 of up to 1000 143 -> 136); where a launch is a workgroup or two deep the exchange costs 0.3 us.
-    // The queries come the same way, whole rows straight to local memory with the first tiles (47.9 -> 45.7, 138.5 -> 136.7).
-    constexpr bool WHOLE_ROWS = PACKED && SPLIT == 1 && !SCORES;
+    // 320 tokens 52 -> 47 us, 16 of up to 1000 143 -> 136); where two sets share the tiles and a launch is a workgroup or two deep the
+    // exchange costs 0.3 us.  The queries come the same way in all forms, whole rows straight to local memory with the first tiles
+    // (47.9 -> 45.7, 138.5 -> 136.7; one prompt of 200 tokens 9.34 -> 8.87, 64 of up to 128 with scores 48.1 -> 46.9).
+    constexpr bool WHOLE_ROWS = PACKED && SPLIT == 1;
     extern __shared__ __align__(16) _Float16 tiles[];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
@@ -255,13 +256,16 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     const int q0 = qb * rows + (wave >> side) * 32;    // first query of this wave
     const int query = q0 + r;                          // this lane's query column
     half8 qf[8];                                       // B operand of S^T = K Q^T: Q[query][16 ks + 8 g ..]
-    _Float16 *q_rows = tiles + 3 * kPfTile + wave * 32 * kPfD;         // WHOLE_ROWS: the second V buffer, not in use before step 0, and as much behind it
-    if constexpr (WHOLE_ROWS) {
-        const int row0 = min(q0, L - 1), end = min(L - 1 - row0, 31) * (int)q_pitch + 240;
+    // Packed prompts: a wave's rows stand in the second V buffer, not in use before step 0, and as much behind it (each set loads half of
+    // them); with single buffers behind those.
+    constexpr int kQRows = 32 / SPLIT;
+    auto q_rows = [&](int set) { return tiles + (BUF == 1 ? 4 : set * 4 + 3) * kPfTile + (BUF == 1 ? set * WAVES + wave : wave) * (kQRows * kPfD); };
+    if constexpr (PACKED) {
+        const int row0 = min(q0 + set * kQRows, L - 1), end = min(L - 1 - row0, kQRows - 1) * (int)q_pitch + 240;
         const char *first = (const char *)(Qh + (long)row0 * (q_pitch / 2));
-        const unsigned lds = lds_offset(q_rows);
+        const unsigned lds = lds_offset(q_rows(set));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kQRows / 4; ++i) {
             const int row = 4 * i + (lane >> 4);       // (chunks as in a K tile; rows past the prompt are those of columns that nobody stores)
             load_to_lds(first, (unsigned)min(row * (int)q_pitch + (((lane & 15) ^ (row & 15)) << 4), end), lds + i * 1024u);
         }
@@ -428,9 +432,10 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
     if (BUF == 2) request(Kh, 1, false);
     request(Vh, 0, true);
     hand_over();                                       // (the Q rows have arrived as well)
-    if constexpr (WHOLE_ROWS) {
+    if constexpr (PACKED) {
+        const _Float16 *mine = q_rows(r / kQRows) - r / kQRows * (kQRows * kPfD);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(q_rows + k_place[ks]);
+        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(mine + k_place[ks]);
     }
     float16v sa[2], sb[2];
     if (SPLIT == 1 || mytiles > 0) {                   // (the second set may have nothing for the first rows)
@@ -521,13 +526,13 @@ __global__ __launch_bounds__(64 * WAVES * SPLIT, 2) void prefill_fwd_kernel(Pref
         hand_over();
     }
     if constexpr (WHOLE_ROWS) {
-        constexpr int kPart = 16;                      // rows at a time
-        char *stage = (char *)tiles + wave * (kPart * 256);
-        hand_over();                                   // (every wave has read the last tile)
+        constexpr int kPart = 16, kCopies = SCORES ? 1 : 2;            // rows at a time; of the code (two cost the scores a private segment)
+        char *stage = (char *)(tiles + 2 * kPfTile) + wave * (kPart * 256);          // (the first V buffer)
+        if (!SCORES) hand_over();                      // (every wave has read the last tile)
         if (g == 0 && query < L) a.lse[stat + query] = lse2 * kLn2;
         const int there = L - q0;                      // rows of the wave that exist
         _Float16 *out = a.XO + (((long)pb.first + q0) * a.Hq + head) * kPfD + (lane & 15) * 8;
-#pragma unroll
+#pragma unroll kCopies
         for (int part = 0; part < 32 / kPart; ++part) {
             if (r / kPart == part) {
 #pragma unroll
@@ -907,7 +912,7 @@ static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
     if ((per_head(128) + 1) * a.Hq > 0xffffff) return MINIKV_EINVAL;   // (a launch holds less than 2^32 work-items; heads side by side round up once a head)
     if (scores && a.max_len <= 128) {
         hipLaunchKernelGGL((prefill_fwd_kernel<4, 1, 2, true, true, BF16>), dim3((unsigned)(per_head(128) * a.Hq)), dim3(256),
-                           fwd_lds_bytes(1, 2, 128), st, a);
+                           fwd_lds_bytes(1, 2, 0, 1), st, a);           // (the query rows' place holds the LSE and sums later on)
         return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
     }
     // Which form, by the rules for prompts of one length (launch_prefill) with the longest prompt as the length and an upper
@@ -922,7 +927,7 @@ static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
     while ((2 << a.side) <= waves && a.rep % (2 << a.side) == 0) ++a.side;
     const dim3 grid((unsigned)(per_head(32 * waves >> a.side) * (a.Hq >> a.side)));
     if (two_sets_64 && !two_buffers)
-        hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 1, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 1), st, a);
+        hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 1, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 1, 0, 1), st, a);
     else if (two_sets_64)
         hipLaunchKernelGGL((prefill_fwd_kernel<2, 2, 2, false, true, BF16>), grid, dim3(256), fwd_lds_bytes(2, 2), st, a);
     else if (two_sets_128)
