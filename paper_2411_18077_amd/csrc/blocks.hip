@@ -251,21 +251,24 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
     const int first = (int)begin, which = of >= (uint32_t)a.Hkv, h = (int)of - (which ? a.Hkv : 0);
     const uint16_t *X = (which ? a.X[1] : a.X[0]) + (int64_t)h * kD + c * 8;
     const int64_t stride = which ? a.stride[1] : a.stride[0];
-    auto block_of = [&](int i) {                       // block of token i, -1: none
-        const int slot = a.slots[i];
-        return (uint32_t)slot < (uint32_t)a.rows ? slot >> a.shift : -1;
-    };
-    bool begins = false;
-    if (lane < a.chunk && first + lane < a.n_tok) {
-        const int b = block_of(first + lane);
-        begins = b >= 0 && (first + lane == 0 || block_of(first + lane - 1) != b);
-    }
+    auto slot_of = [&](int64_t i) { return i >= 0 && i < a.n_tok ? a.slots[i] : -1; };
+    auto block_of = [&](int slot) { return (uint32_t)slot < (uint32_t)a.rows ? slot >> a.shift : -1; };      // -1: none
+    // the slots of the wave's tokens, of the one before, and of as many behind as one look at a run takes: one round trip
+    const int before = slot_of(begin + lane - 1), window[2] = {slot_of(begin + lane), slot_of(begin + 64 + lane)};
+    const bool begins = lane < a.chunk && block_of(window[0]) >= 0 && block_of(before) != block_of(window[0]);
     for (uint64_t todo = __ballot(begins); todo; todo &= todo - 1) {
-        const int i = first + __builtin_ctzll(todo), blk = __builtin_amdgcn_readfirstlane(block_of(i));
+        const int o = __builtin_ctzll(todo), i = first + o, blk = block_of(__builtin_amdgcn_readlane(window[0], o));
         int n = 0;                                     // rows of the run
+        int mine_at = 0;                               // slot of its token `lane`
         bool fresh = false;                            // one of them is the block's first
         for (uint64_t same = ~0ull; same == ~0ull; n += same == ~0ull ? 64 : __builtin_ctzll(~same)) {
-            const int j = i + n + lane, slot = j < a.n_tok ? a.slots[j] : -1;
+            int slot;
+            if (n == 0) {
+                const int lo = __shfl(window[0], (o + lane) & 63, 64), hi = __shfl(window[1], (o + lane) & 63, 64);
+                slot = mine_at = o + lane < 64 ? lo : hi;
+            } else {
+                slot = slot_of((int64_t)i + n + lane);
+            }
             const bool mine = (uint32_t)slot < (uint32_t)a.rows && slot >> a.shift == blk;
             same = __ballot(mine);
             const uint64_t run = same == ~0ull ? ~0ull : (1ull << __builtin_ctzll(~same)) - 1;
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
             if (n > ROWS) load(base);
 #pragma unroll
             for (int k = 0; k < ROWS / 4; ++k) {
-                const int row = base + 4 * k + sub;
+                const int row = base + 4 * k + sub, at = ROWS == 64 ? __shfl(mine_at, row & 63, 64) : 0;      // (in front of the branch: from all lanes)
                 if (base + 4 * k < n && row < n) {
                     int v[2];
 #pragma unroll
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
                         v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(lo & 0xffff) * inv, from16<BF16>(lo >> 16) * inv, 0, false);
                         v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(from16<BF16>(hi & 0xffff) * inv, from16<BF16>(hi >> 16) * inv, v[j], true);
                     }
-                    const int off = a.slots[i + row] & ((1 << a.shift) - 1);
+                    const int off = (ROWS > 64 || base ? a.slots[i + row] : at) & ((1 << a.shift) - 1);
                     *(int2 *)(codes + off * kD + c * 8) = int2{v[0], v[1]};
                 }
             }
