@@ -124,6 +124,22 @@ def test_rows_of_any_pitch(api):
     check(api, [128, 16], 2, 2, F16, tail=1)
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv", [([100, 64], 2, 1), ([150, 60], 4, 1), ([140, 70], 64, 32)])
+def test_the_largest_pitch(api, lens, Hq, Hkv):
+    """Tokens 2^23 elements apart, a tile of rows nearly 2^31 bytes: the same outputs as from rows that stand together."""
+    cu = [0, lens[0], sum(lens)]
+    near = fused(cu[-1], Hq, Hkv, F16, 5)
+    x = torch.full((cu[-1], 1 << 23), float("nan"), dtype=F16, device="cuda")
+    far, at = [], 0
+    for t in near:
+        width = t.shape[1] * 128
+        far.append(x[:, at:at + width].unflatten(1, (t.shape[1], 128)))
+        far[-1].copy_(t)
+        at += width
+    for a, b in zip(run(api, *near, cu, True), run(api, *far, cu, True)):
+        assert torch.equal(a, b)
+
+
 def test_peaked_rows(api):
     check(api, [150, 260], 2, 1, F16, gain=4.0)
     check(api, [150, 260], 2, 1, BF16, gain=4.0)
