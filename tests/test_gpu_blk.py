@@ -416,6 +416,56 @@ def test_offsets_beyond_32_bits(api):
     assert bool(((out.cpu().double() - want).abs() <= attn_tolerance(want, mean, score, 380, 6.0, 2.0 ** -11, F16)).all())
 
 
+def test_filing_captured_and_replayed(api):
+    """Each replay files other rows at other slots; a program's own calls stand between the replays."""
+    shape = api.make_blk_shape(2, 2, 2, 128, 16, 12, 6, F16)
+    one, two = api.BlkCache(shape), api.BlkCache(shape)
+    gen = torch.Generator().manual_seed(4)
+    rows = [torch.randn(20, 2, 128, generator=gen).half().cuda() * 3 ** k for k in range(4)]
+    slots = [torch.tensor([(5 * k + i) % 192 for i in range(20)], dtype=torch.int32, device="cuda") for k in range(4)]
+    x, s = rows[0].clone(), slots[0].clone()
+    api.kv_quantize_blk(shape, x, x, s, two)
+    two.K.view(torch.uint8).zero_(), two.V.view(torch.uint8).zero_(), two.Ks.zero_(), two.Vs.zero_()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        api.kv_quantize_blk(shape, x, x, s, two)
+    for r, n in zip(rows, slots):
+        x.copy_(r), s.copy_(n)
+        g.replay()
+        api.kv_quantize_blk(shape, r, r, n, one)
+        for a, b in ((one.K, two.K), (one.V, two.V), (one.Ks, two.Ks), (one.Vs, two.Vs)):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert bool((one.Ks > 0).any())
+
+
+def test_two_calls_at_once(api):
+    """Attention on two streams with workspaces of their own: the results of one after the other."""
+    lens, block, Hkv, N = [4000, 300, 900], 64, 2, 90
+    shape = api.make_blk_shape(3, 8, Hkv, 128, block, N, 64, BF16)
+    gen = torch.Generator().manual_seed(6)
+    cache = api.BlkCache(shape)
+    t = tables(lens, block, 64, N, 2).cuda()
+    slots = torch.tensor([int(t[r, i // block]) * block + i % block for r, n in enumerate(lens) for i in range(n)], dtype=torch.int32, device="cuda")
+    x = torch.randn(sum(lens), Hkv, 128, generator=gen).bfloat16().cuda()
+    api.kv_quantize_blk(shape, x, x, slots, cache)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = [torch.randn(3, 8, 128, generator=gen).bfloat16().cuda() for _ in range(2)]
+    want = [torch.zeros_like(v) for v in q]
+    for v, o in zip(q, want):
+        api.minikv_decode_attn_blk(shape, v, cache, t, n, SM, o)
+    out = [[torch.zeros_like(v) for _ in range(20)] for v in q]
+    ws = [torch.zeros_like(cache.workspace) for _ in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(20):
+        for v, o, w, st in zip(q, out, ws, streams):
+            api.minikv_decode_attn_blk(shape, v, cache, t, n, SM, o[k], workspace=w, stream=st)
+    torch.cuda.synchronize()
+    for o, w in zip(out, want):
+        assert all(torch.equal(v, w) for v in o)
+
+
 def test_calls_on_a_side_stream(api):
     """The calls go to the stream that is current, or to the one given."""
     lens, block, Hkv = [70, 200], 32, 2
