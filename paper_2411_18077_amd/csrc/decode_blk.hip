@@ -474,7 +474,8 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
         if (total == 0) return;
     }
     // The line: tile t of a unit that begins at `start` on it stands at start + kBkUnitCost + t.
-    const int span = by_unit ? 1 : max((total + (int)gridDim.x * kBkWaves - 1) / ((int)gridDim.x * kBkWaves), kBkUnitCost + 1);
+    // (total is below 2^31, the sum below 2^32)
+    const int span = by_unit ? 1 : max((int)(((uint32_t)total + gridDim.x * kBkWaves - 1) / (gridDim.x * kBkWaves)), kBkUnitCost + 1);
     const int64_t from = (int64_t)(wg * kBkWaves + wave) * span;
     int x = (int)min(from, (int64_t)total);
     const int end = (int)min(from + span, (int64_t)total);
