@@ -309,7 +309,10 @@ int kv_quantize_blk(const minikv_blk_shape *shape, int32_t n_tok, const void *K,
  * hq / (Hq/Hkv), fp32 accumulation; one launch for all requests, whatever their lengths.  A request without tokens gives
  * zeros.  Table entries outside 0 .. n_blocks-1 count as absent: their tokens contribute nothing.  Lengths are clamped
  * to 0 .. max_blocks * block.  What lies behind a request's last token in its last block is not used, whatever it holds.
- * The raw products q . codes are formed in binary32 and must not overflow there.
+ * The raw products q . codes and the sums of exp(score - largest score) times value are formed in binary32 and must not overflow there.
+ * Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is below 2^-17 of the largest such
+ * product of the row by at most 2^-28 of that one, whatever the scales of the row's blocks and whichever of them carry weight (weights below
+ * 2^-126 of the largest weight are 0).
  *   q      fp16 / bf16 [R][Hq][128], requests q_stride elements apart   (device, read)
  *   out    fp16 / bf16 [R][Hq][128]                                     (device, written)
  *   workspace  device scratch of at least minikv_blk_workspace_bytes(shape) bytes, 16-byte aligned, ZERO-FILLED ONCE after

@@ -12,8 +12,12 @@
 //            the second.  Of the 16 x 16 results the two quadrants whose row and column belong to one half count.
 // So every lane of the instruction works, loads are whole rows and neither K, V nor the weights pass through local memory.
 //
-// Weights are rounded to fp16 for the second product (relative 2^-11, to nearest, the sum of weights is kept in fp32 from
-// the unrounded ones), scaled by the block's V scale over the largest one seen so far: at most 1, whatever the scales.
+// Weights are rounded to fp16 for the second product (relative 2^-11, to nearest; the sum of weights is kept in fp32 from
+// the unrounded ones), each with its block's V scale, over a reference that no such product so far exceeds, times 2^15: at most 2^15, and with
+// all 11 bits down to 2^-29 of the reference.  The reference is the largest V scale that the wave has seen of the unit while its scales lie
+// within 2^12 of each other (some token of weight 1 then has a product of 2^-12 or more of it), which costs nothing per tile.
+// From the first tile where they do not on, it is per column the largest product itself, so that neither a large scale without weight nor a large
+// weight without a scale takes the bits of the others: what is lost of a product is at most 2^-28 of the largest one either way.
 #include "decode_common.h"
 
 #include <type_traits>
@@ -31,6 +35,9 @@ constexpr int kBkThreads = 64 * kBkWaves;
 constexpr int kBkRow = kD + 4;                         // floats of a head's state in local memory: m, l, 2 pad, o
 constexpr int kBkEntry = kMaxRep * kBkRow;             // of a part of a unit
 constexpr float kBkNone = -3.0e38f;                    // running maximum before the first token: finite, so that no difference is NaN
+constexpr float kBkHeadroom = 32768.0f;                // fp16 weights run to 65504
+constexpr int kBkFar = 12 << 23;                       // V scales whose bits (of positive floats) differ by more lie more than 2^12 apart
+constexpr float kBkLeast = 0x1p-110f, kBkRange = 0x1p-100f;            // the reference: at least this, and this times the largest V scale (no quotient overflows)
 // What a unit costs a wave besides its tiles (table, scales, queries, output), in tiles on the line of work.
 constexpr int kBkUnitCost = 1;
 // Workgroups of their own for every unit beat the line of work (where there are enough of them) while their waves have at most so
@@ -177,7 +184,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
     const int wg = blockIdx.x;
 
     f4v o[16];                                         // this lane's sums, see the top of the file
-    float m, l, vref;                                  // maximum and sum of weights, largest V scale
+    float m, l, ref;                                   // maximum and sum of weights, reference of the products: o is in units of ref / kBkHeadroom
     auto entry_of = [&](int t) { return t * kIds / kTiles; };
     // What is loaded for: the unit, its table entries batch + lane (block, K factor, V scale), its queries, one tile of codes.
     int ld_h = 0, ld_len = 0, batch = 0, id = -1;
@@ -230,14 +237,19 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
     auto attend = [&](int len, int t0, int t1, bool more, auto next) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
-        m = kBkNone, l = 0.0f, vref = 0.0f;
-        float ivref = 0.0f;
+        m = kBkNone, l = 0.0f, ref = kBkLeast;
+        float iref = kBkHeadroom / kBkLeast;
+        int vmin = 0x7f800000, vmax = 0;               // bits of the V scales seen, smallest and largest
         for (int t = t0; t < t1; ++t) {
             const int e0 = entry_of(t) - batch;
             bool whole = (t + 1) * kBlkTile <= len;
-            float vmax = 0.0f, f[2], vf[2];            // largest V scale; this lane's K factors and V scales (of 16 tokens each)
+            float f[2], vf[2];                         // this lane's K factors and V scales (of 16 tokens each)
 #pragma unroll
-            for (int i = 0; i < kIds; ++i) whole &= lane_value(id, e0 + i) >= 0, vmax = fmaxf(vmax, lane_float(vs, e0 + i));
+            for (int i = 0; i < kIds; ++i) {
+                const int bits = lane_value(__float_as_int(vs), e0 + i);
+                const bool there = lane_value(id, e0 + i) >= 0;
+                whole &= there, vmax = max(vmax, bits), vmin = there ? min(vmin, bits) : vmin;
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int lo = e0 + k * kIds / 4, hi = e0 + (2 + k) * kIds / 4;
@@ -283,15 +295,21 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
                     }
                 }
             }
-            float mx = w[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) mx = fmaxf(mx, w[i]);
-            mx = max_over_g(mx);
-            if (__any(mx > m) || vmax > vref) {
+            const float mx0 = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), mx1 = fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7]));
+            const float mx = max_over_g(fmaxf(mx0, mx1)), largest = __int_as_float(vmax);
+            const bool far = vmax - vmin > kBkFar;
+            if (__any(mx > m || largest > ref) || far) {
                 const float top = fmaxf(mx, m), alpha = __builtin_amdgcn_exp2f(m - top);
                 m = top, l *= alpha;
                 float both = alpha;
-                if (vmax > vref) both *= vref / vmax, vref = vmax, ivref = 1.0f / vmax;
+                if (far) {                             // (o stands for sums relative to the maximum: where that grows, the reference shrinks instead)
+                    const float here = fmaxf(__builtin_amdgcn_exp2f(mx0 - m) * vf[0], __builtin_amdgcn_exp2f(mx1 - m) * vf[1]);
+                    const float old = ref * alpha;
+                    ref = fmaxf(fmaxf(old, max_over_g(here)), fmaxf(largest * kBkRange, kBkLeast)), iref = kBkHeadroom / ref;
+                    both = old / ref;
+                } else if (largest > ref) {
+                    both *= ref / largest, ref = largest, iref = kBkHeadroom / ref;
+                }
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
 #pragma unroll
@@ -302,7 +320,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
             for (int i = 0; i < 8; ++i) {
                 const float e = __builtin_amdgcn_exp2f(w[i] - m);
                 l += e;
-                p[i] = (_Float16)(e * (vf[i >> 2] * ivref));
+                p[i] = (_Float16)(e * (vf[i >> 2] * iref));
             }
 #pragma unroll
             for (int d = 0; d < 4; ++d) {              // channels 16 head + 4 d .. + 3
@@ -326,6 +344,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
     // column belong to one half of the tokens.
     auto leave_halves = [&](int slot) __attribute__((always_inline)) {      // each half to a slot of its own
         l = sum_over_g(l);
+        const float f = ref / kBkHeadroom;
         float *p = parts + (slot + half) * kBkEntry + head * kBkRow;
         if (g == 0) p[0] = m, p[1] = l;
         p += 4 + (g & 1) * 64;
@@ -334,7 +353,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; j += 4)
-                    *(float4 *)(p + i * 16 + j) = float4{o[j][i] * vref, o[j + 1][i] * vref, o[j + 2][i] * vref, o[j + 3][i] * vref};
+                    *(float4 *)(p + i * 16 + j) = float4{o[j][i] * f, o[j + 1][i] * f, o[j + 2][i] * f, o[j + 3][i] * f};
         }
     };
     // both to one slot: the second half's lanes put theirs down, the first half's add theirs
@@ -344,7 +363,7 @@ __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
         l += other_half(l);
         float *p = parts + slot * kBkEntry + head * kBkRow;
         if (lane < 8) p[0] = both, p[1] = l;
-        const float f = mine * vref;
+        const float f = mine * (ref / kBkHeadroom);
         p += 4 + (g & 1) * 64;
         if (half && g >= 2) {
 #pragma unroll

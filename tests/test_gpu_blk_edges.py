@@ -45,3 +45,80 @@ def test_the_longest_line_of_work(api):
     want = value[None, :, None].expand(R, Hkv, 128)
     assert bool(((out.cpu() - want).abs() <= want * (HALF[F16] + 64 * 2.0 ** -24)).all())
     assert not bool(cache.workspace[:5120].any())
+
+
+def coded(x):
+    """Codes and power-of-two scales of rows x [blocks][Hkv][block][128] in 64 bits."""
+    s = torch.tensor([[blk.scale_for(float(a)) for a in row] for row in x.abs().amax(dim=(2, 3))], dtype=torch.float64)
+    return blk.encode(x / torch.where(s > 0, s, 1.0)[:, :, None, None]), s.float()
+
+
+def largest_product(q, Kc, Ks, Vs, table, lens, sm):
+    """Per request and head the largest softmax weight times V scale."""
+    R, Hq, _ = q.shape
+    Hkv, block = Kc.shape[1:3]
+    rep, top = Hq // Hkv, torch.zeros(R, Hq, 1, dtype=torch.float64)
+    for r, n in enumerate(lens):
+        at = [(int(table[r, i // block]), i % block) for i in range(n)]
+        if at:
+            b, o = torch.tensor([p[0] for p in at]), torch.tensor([p[1] for p in at])
+        for h in range(Hkv if at else 0):
+            k = blk.decode_codes(Kc[b, h, o]) * Ks[b, h].double()[:, None]
+            p = torch.softmax(q[r, h * rep:(h + 1) * rep].double() @ k.t() * sm, dim=1)
+            top[r, h * rep:(h + 1) * rep, 0] = (p * Vs[b, h].double()).amax(dim=1)
+    return top
+
+
+SPREADS = {
+    # (V scale, score) of block i of n, r octaves apart
+    "large blocks without weight": lambda i, n, r: (r, -300.0) if i % 3 == 1 else (0, 0.0),
+    "large blocks of little weight": lambda i, n, r: (r, -r * 0.6931) if i % 3 == 1 else (0, 0.0),
+    "large and small blocks of the same weight": lambda i, n, r: (0, 0.0) if i % 3 == 1 else (-r, 0.0),
+    "zeros with the weight": lambda i, n, r: (None, min(r, 40) * 0.6931) if i % 4 == 0 else (0, 0.0),
+    "ever larger": lambda i, n, r: (r * (i + 1) / n, -r * (i + 1) / n * 0.6931),
+    "ever smaller": lambda i, n, r: (r * (n - i) / n, -r * (n - i) / n * 0.6931),
+}
+
+
+@pytest.mark.parametrize("kind", SPREADS)
+@pytest.mark.parametrize("r", [13, 18, 30, 90])
+@pytest.mark.parametrize("Hq,Hkv,block,lens,dtype", [
+    (4, 1, 16, [330], F16), (8, 2, 32, [0, 70, 1000], BF16), (3, 1, 64, [5000, 200], F16), (4, 4, 128, [700, 129, 64], BF16),
+    (2, 1, 16, [60 + i % 40 for i in range(280)] + [4000], BF16), (1, 1, 64, [450] * 258, F16),
+])
+def test_scales_far_apart(api, kind, r, Hq, Hkv, block, lens, dtype):
+    """The V scales of a request's blocks are r octaves apart, with or without weight to go with them.  Per output: each weight's product
+    with its scale is rounded to fp16's 11 bits (half a step 2^-11), or where it is below fp16's normal numbers by at most 2^-28 of the largest
+    such product of the row (see the kernel), times a code of at most 448; scores, sums and the output's own rounding as
+    in attn_tolerance, here with every token's addition counted."""
+    g = torch.Generator().manual_seed(r + block)
+    need = [-(-n // block) for n in lens]
+    N, width = sum(need) + 1, max(need)
+    K, V = (torch.randn(N, Hkv, block, 128, generator=g, dtype=torch.float64) for _ in range(2))
+    q = torch.randn(len(lens), Hq, 128, generator=g)
+    q[:, :, 0] = 16.0
+    q = q.to(dtype)
+    K[..., 0] = 0.0
+    order, table, at = torch.randperm(N, generator=g), torch.full((len(lens), width), -7, dtype=torch.int32), 0
+    for row, n in zip(table, need):
+        for i in range(n):
+            b = int(order[at])
+            row[i], at = b, at + 1
+            octaves, score = SPREADS[kind](i, n, r)
+            V[b] *= 0.0 if octaves is None else 2.0 ** octaves
+            K[b, :, :, 0] = score / (16.0 * SM)
+    (Kc, Ks), (Vc, Vs) = coded(K), coded(V)
+    shape = api.make_blk_shape(len(lens), Hq, Hkv, 128, block, N, width, dtype)
+    cache = api.BlkCache(shape, K=Kc.cuda().view(E4M3), V=Vc.cuda().view(E4M3), Ks=Ks.cuda(), Vs=Vs.cuda())
+    out = torch.full((len(lens), Hq, 128), float("nan"), dtype=dtype, device="cuda")
+    api.minikv_decode_attn_blk(shape, q.cuda(), cache, table.cuda(), ints(*lens), SM, out)
+    want, mean, score = blk.decode_attn(q, Kc, Ks, Vc, Vs, table, lens, SM)
+    n = torch.tensor(lens)[:, None, None]
+    rel = 2.0 ** -11 + 2 * (136 * 2.0 ** -24 * score * 1.01) + (64 + n) * 2.0 ** -24
+    tol = mean * rel + n * 2.0 ** -28 * 448 * largest_product(q, Kc, Ks, Vs, table, lens, SM) + want.abs() * HALF[dtype] * 1.001 + \
+        (2.0 ** -25 if dtype is F16 else 2.0 ** -130)
+    got = out.cpu().double()
+    # (fp16 rounds what is 65520 or more to infinity: the keys' codes miss the intended scores by up to 2^-4 of them, and 200 tokens of
+    # 90 octaves then give outputs of 1.9e7, 3.1e8)
+    err = (got - want).abs().where((got.abs() != float("inf")) | (want * got.sign() + tol < 65520.0), 0.0)
+    assert bool((err <= tol).all()), (float(err.max()), float((err / tol).max()))
