@@ -18,9 +18,9 @@ constexpr int kAsMost = kMaxRequests / kAsThreads;     // requests of a thread, 
 constexpr int kAsFew = 8;                              // rows of a request that its own thread writes the slots of
 constexpr uint32_t kRefused = 0x80000000u;
 
-// Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap < 2^31;
+// Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap <= 2^31;
 // min(a + b, cap) is associative, so a scan in any order gives the same.)
-__device__ inline uint32_t sat_add(uint32_t a, uint32_t b, uint32_t cap) { return min(a + b, cap); }
+__device__ inline uint32_t sat_add(uint32_t a, uint32_t b, uint32_t cap) { return min(__builtin_elementwise_add_sat(a, b), cap); }
 template <int CTRL, int ROWS> __device__ inline uint32_t sat_step(uint32_t v, uint32_t cap)
 {
     return sat_add(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false), cap);
@@ -78,7 +78,8 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
     const int tid = threadIdx.x, gtid = blockIdx.x * kAsThreads + tid, gsize = gridDim.x * kAsThreads;
     const int64_t most = (int64_t)a.width << a.shift;
     const int head = min(max(a.state[0], 0), a.N - 1), n_free = min(max(a.state[1], 0), a.N);
-    const uint32_t kRows = 0x7fffffff, back = a.N - n_free;            // blocks that can come back
+    const uint32_t kRows = 0x80000000, kMostRows = 0x7fffffff;          // where sums of rows saturate (behind any slot), and the largest that is passed on
+    const uint32_t back = a.N - n_free;                // blocks that can come back
     const uint32_t unit = (1u << a.shift) - 1;
 
     auto len_of = [&](int r) { return (int)min((int64_t)max(a.q_len[r], 0), most); };
@@ -119,12 +120,12 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
             take += n;
             const bool ok = !(nd[j] & kRefused) && (n == 0 || take <= (uint32_t)n_free);
             if (ok && n) pop = take;                   // (ascending in the accepted ones)
-            if (!few) rows[r] = row[j], need[r] = first | (ok ? 0u : kRefused);
+            if (!few) rows[r] = min(row[j], kMostRows), need[r] = first | (ok ? 0u : kRefused);
             if (totals[1]) over[r] = give;
             give = sat_add(give, ov[j], back);
             if (blockIdx.x == 0) {
                 a.q_len_next[r] = add[j] < 0 ? 0 : ok ? len[j] + add[j] : len[j];
-                a.cu[r] = (int)row[j];
+                a.cu[r] = (int)min(row[j], kMostRows);
                 if (few) {
                     const int held = (int)blocks(len[j]);
                     int32_t *entry = a.table + (int64_t)r * a.width;
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
     __syncthreads();
     pop = popped;
     if (blockIdx.x == 0 && tid == 0) {
-        a.cu[a.R] = (int)total[0];
+        a.cu[a.R] = (int)min(total[0], kMostRows);
         a.state_next[0] = (int)wrap(head + pop), a.state_next[1] = n_free - (int)pop + (int)totals[1];
     }
     if (few) {

@@ -122,3 +122,27 @@ def test_scales_far_apart(api, kind, r, Hq, Hkv, block, lens, dtype):
     # 90 octaves then give outputs of 1.9e7, 3.1e8)
     err = (got - want).abs().where((got.abs() != float("inf")) | (want * got.sign() + tol < 65520.0), 0.0)
     assert bool((err <= tol).all()), (float(err.max()), float((err / tol).max()))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# kv_assign_blk
+
+@pytest.mark.parametrize("n_new,ok", [((2 ** 31 - 1, 1), (False, False)), ((2 ** 31 - 1, 0, 1), (False, False, False)), ((2 ** 31 - 2, 1), (False, True)),
+                                      ((2 ** 31 - 1, 2 ** 31 - 1, 20), (False, False, False))])
+def test_rows_behind_the_largest_slot_map(api, n_new, ok):
+    """2^31 - 1 slots: a request whose rows begin behind them is refused, although what cu holds of the sum ends at 2^31 - 1."""
+    R, n = len(n_new), 2 ** 31 - 1
+    shape = api.make_blk_shape(R, 1, 1, 128, 16, 40, 8, F16)
+    table, ring = torch.full((R, 8), -1, dtype=torch.int32, device="cuda"), torch.arange(40, dtype=torch.int32, device="cuda")
+    nxt, state, cu, slots = ints(*[-9] * R), ints(-9, -9), ints(*[-9] * (R + 1)), torch.zeros(n, dtype=torch.int32, device="cuda")
+    api.kv_assign_blk(shape, ints(*[0] * R), ints(*n_new), table, ring, ints(0, 40), nxt, state, cu, slots)
+    at = [sum(n_new[:i]) for i in range(R + 1)]
+    want = [k if o else 0 for k, o in zip(n_new, ok)]
+    assert cu.tolist() == [min(a, n) for a in at] and nxt.tolist() == want
+    assert state.tolist() == [sum(ok), 40 - sum(ok)]
+    for r, o in enumerate(ok):
+        assert table[r].tolist() == [0 if o else -1] + [-1] * 7
+        if o:
+            assert slots[at[r]:at[r] + n_new[r]].tolist() == list(range(n_new[r]))
+            slots[at[r]:at[r] + n_new[r]] = -1
+    assert int(slots.max()) == -1 and int(slots.min()) == -1
