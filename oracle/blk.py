@@ -75,7 +75,8 @@ def assign(q_len, n_new, table, ring, state, block, n_slots):
             taken += 1
         for i in range(add):
             pos = q_len[r] + i
-            slots[cu[r] + i] = table[r][pos // block] * block + pos % block
+            b = table[r][pos // block]
+            slots[cu[r] + i] = b * block + pos % block if 0 <= b < N else -1
         length[r] = q_len[r] + add
     for i, b in enumerate(back):
         ring[(head + n_free + i) % N] = b

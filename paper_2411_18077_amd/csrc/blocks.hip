@@ -84,6 +84,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
 
     auto len_of = [&](int r) { return (int)min((int64_t)max(a.q_len[r], 0), most); };
     auto blocks = [&](uint32_t tokens) { return (tokens + unit) >> a.shift; };       // (at most 2^30 + 2^31)
+    auto slot_in = [&](int id, int pos) { return (uint32_t)id < (uint32_t)a.N ? (id << a.shift) + (pos & (int)unit) : -1; };      // (no other block's)
     auto wrap = [&](uint32_t i) { return i >= (uint32_t)a.N ? i - a.N : i; };          // i < 2 N
 
     const int per = (a.R + kAsThreads - 1) / kAsThreads, r0 = min(tid * per, a.R), mine = min(a.R - r0, per);
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
                         if (ok) {
                             const int id = b < held ? entry[b] : a.ring[wrap(head + first + (b - held))];
                             if (b >= held) entry[b] = id;
-                            slot = (id << a.shift) + (pos & (int)unit);
+                            slot = slot_in(id, pos);
                         }
                         if (row[j] + i < (uint32_t)a.n_slots) a.slots[row[j] + i] = slot;
                     }
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
                 const int len = len_of(r), pos = len + (t - (int)rows[r]);
                 const int b = pos >> a.shift, held = (int)blocks(len);
                 const int id = b < held ? a.table[(int64_t)r * a.width + b] : a.ring[wrap(head + need[r] + (b - held))];
-                slot = (id << a.shift) + (pos & (int)unit);
+                slot = slot_in(id, pos);
             }
             a.slots[t] = slot;
         }

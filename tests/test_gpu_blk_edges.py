@@ -146,3 +146,21 @@ def test_rows_behind_the_largest_slot_map(api, n_new, ok):
             assert slots[at[r]:at[r] + n_new[r]].tolist() == list(range(n_new[r]))
             slots[at[r]:at[r] + n_new[r]] = -1
     assert int(slots.max()) == -1 and int(slots.min()) == -1
+
+
+@pytest.mark.parametrize("new", [3, 9])
+def test_blocks_outside_the_pool_have_no_slots(api, new):
+    """A table or a ring that names a block outside the pool: its rows get no slot, whatever the product with the block's size wraps to, in
+    the form for few rows each and in the other one."""
+    block = 16
+    bad = [1 << 28, -(1 << 28), -1, 5, 2 ** 31 - 1]
+    q_len, n_new = [block - 2] * 5 + [0, 0, 0], [new] * 5 + [2, 2, 2]
+    table = [[b, -1] for b in bad] + [[-1, -1]] * 3
+    ring = [0, 1 << 28, 1, -7, 2, 3, 4, 1 << 30, 5, 6]                # (ids outside the pool among the free ones)
+    got = dict(table=ints(*sum(table, [])), ring=ints(*ring), q_len=ints(*[0] * 8), state=ints(0, 0), cu=ints(*[0] * 9), slots=ints(*[7] * 60))
+    shape = api.make_blk_shape(8, 1, 1, 128, block, 10, 2, F16)
+    api.kv_assign_blk(shape, ints(*q_len), ints(*n_new), got["table"], got["ring"], ints(0, 10), got["q_len"], got["state"], got["cu"], got["slots"])
+    want = blk.assign(q_len, n_new, table, ring, [0, 10], block, 60)
+    assert got["table"].view(8, 2).tolist() == want["table"] and got["slots"].tolist() == want["slots"]
+    assert all(got[k].tolist() == want[k] for k in ("ring", "q_len", "state", "cu"))
+    assert got["slots"][:2].tolist() == [-1, -1] and got["slots"][3 * new:3 * new + 2].tolist() == [94, 95]
