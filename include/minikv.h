@@ -240,7 +240,7 @@ int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, con
  * where they become subnormal codes); the attention takes any finite scale that is 0 or at least 2^-126.
  * Request r owns the blocks table[r][0], table[r][1], ...; its token i is row i % block of block
  * table[r][i / block], its SLOT is table[r][i / block] * block + i % block.  A block may stand in several tables
- * (a shared prefix) as long as nothing is filed into it.
+ * (a shared prefix) as long as nothing is filed into it and no request that names it is ended through kv_assign_blk.
  *
  *   K, V    uint8 [n_blocks][Hkv][block][128]     Ks, Vs  float [n_blocks][Hkv]
  *   table   int32 [R][max_blocks]                 q_len   int32 [R]   tokens held by each request
@@ -286,8 +286,12 @@ size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
  *                     the rows of a request that was not accepted, behind cu[R], and of a block outside 0 .. n_blocks-1
  *                     (an absent one: the row is not filed)                        (device, written)
  * The next step takes q_len_next and ring_state_next (swap the pointers: every workgroup reads the old ones).  Lengths
- * outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside 0 .. n_blocks are clamped.  A table
- * entry of a request that is over is put back as it is. */
+ * outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside 0 .. n_blocks are clamped.
+ * A request that is over gives ALL its blocks back, each table entry as it is: the call knows no sharing, so every one of them
+ * has to be a block of the pool that no other table names, else a later step hands it out while another request still reads
+ * it, or hands it out twice.  A request with shared or absent blocks is ended by the program instead, between two steps and in the
+ * arrays that the next one reads: q_len[r] = 0, and those of its blocks that no table names any more go to ring[(head + n_free)
+ * % n_blocks] one by one, n_free counting them. */
 int kv_assign_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *n_new, int32_t *table,
                   int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *ring_state_next, int32_t *cu,
                   int32_t *slots, int32_t n_slots, void *stream);

@@ -164,3 +164,51 @@ def test_blocks_outside_the_pool_have_no_slots(api, new):
     assert got["table"].view(8, 2).tolist() == want["table"] and got["slots"].tolist() == want["slots"]
     assert all(got[k].tolist() == want[k] for k in ("ring", "q_len", "state", "cu"))
     assert got["slots"][:2].tolist() == [-1, -1] and got["slots"][3 * new:3 * new + 2].tolist() == [94, 95]
+
+
+def test_a_shared_prefix_through_the_end_of_its_requests(api):
+    """Two requests name the same first two blocks.  Each is ended by the program (length 0, own blocks behind the last free one), the shared
+    blocks with the second: the other's attention does not change while new requests take what is free, and no block is lost or doubled."""
+    R, block, width, N, Hkv = 3, 16, 6, 12, 2
+    shape = api.make_blk_shape(R, 4, Hkv, 128, block, N, width, F16)
+    cache = api.BlkCache(shape)
+    table, ring, cu, slots = ints(*[-1] * (R * width)).view(R, width), ints(*range(N)), ints(*[0] * (R + 1)), ints(*[0] * 80)
+    s = dict(q=ints(0, 0, 0), q2=ints(0, 0, 0), state=ints(0, N), state2=ints(0, 0))
+    gen = torch.Generator().manual_seed(3)
+
+    def step(*n_new):
+        api.kv_assign_blk(shape, s["q"], ints(*n_new), table, ring, s["state"], s["q2"], s["state2"], cu, slots)
+        s.update(q=s["q2"], q2=s["q"], state=s["state2"], state2=s["state"])
+        x = torch.randn(sum(max(n, 0) for n in n_new), Hkv, 128, generator=gen).half().cuda()
+        api.kv_quantize_blk(shape, x, -x, slots[:len(x)], cache)
+
+    def attend():
+        out = torch.zeros(R, 4, 128, dtype=F16, device="cuda")
+        api.minikv_decode_attn_blk(shape, q, cache, table, s["q"], SM, out)
+        return out
+
+    def end(r, blocks):                                # what the header tells a program to do
+        for b in blocks:
+            head, n_free = s["state"].tolist()
+            ring[(head + n_free) % N] = b
+            s["state"][1] += 1
+        s["q"][r] = 0
+
+    q = torch.randn(R, 4, 128, generator=gen).half().cuda()
+    step(40, 0, 0)                                     # blocks 0, 1, 2
+    table[1, :2], s["q"][1] = table[0, :2], 32         # the second one begins with the first one's 32 tokens
+    step(1, 20, 0)
+    assert table[0, :3].tolist() == [0, 1, 2] and table[1, :4].tolist() == [0, 1, 3, 4] and s["q"].tolist() == [41, 52, 0]
+    before = attend()
+    end(0, [2])
+    for n in (60, 1):
+        step(n, 0, 0)
+        assert torch.equal(attend()[1], before[1])
+    assert not {0, 1, 3, 4} & set(table[0, :4].tolist())
+    step(0, 0, 30)
+    assert torch.equal(attend()[1], before[1]) and not {0, 1, 3, 4} & set(table[2, :2].tolist())
+    end(1, [0, 1, 3, 4])
+    assert not bool(attend()[1].any())
+    step(-1, 0, -1)
+    head, n_free = s["state"].tolist()
+    assert n_free == N and sorted(ring.tolist()) == list(range(N)) and s["q"].tolist() == [0, 0, 0]
