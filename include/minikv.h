@@ -230,8 +230,10 @@ int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, con
 /* ---------------------------------------------------------------------------------------------------------
  * Variant: a paged 8-BIT cache for batches whose requests come and go, and attention of packed prompts of
  * different lengths -- what a serving loop needs around the calls above when its requests do not share one length.
- * Four entry points, used in a row once per step: kv_assign_blk (blocks and slots), selective_flash_attn_packed
- * (new prompts) or minikv_decode_attn_blk (one new token per request), kv_quantize_blk (filing of the new rows).
+ * Four entry points, used in this order in every step: kv_assign_blk (blocks, slots and the lengths after the step), kv_quantize_blk
+ * (filing of the new rows at their slots), then attention: minikv_decode_attn_blk (one new token per request, with the lengths
+ * AFTER the step, so that the token attends to itself as well; its row has to be filed by then) or
+ * selective_flash_attn_packed (new prompts; it reads the rows as they are, not the cache, and may run before the filing).
  *
  * The cache is a pool of n_blocks blocks of `block` tokens.  Block i of KV head h holds `block` rows of 128 codes
  * in 8-bit floating point (e4m3: 4 exponent and 3 mantissa bits, largest value 448) for keys and as many for
@@ -285,7 +287,8 @@ size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
  *   slots             int32 [n_slots]: the slot of row cu[r] + i, that is of token q_len[r] + i of request r; -1 for
  *                     the rows of a request that was not accepted, behind cu[R], and of a block outside 0 .. n_blocks-1
  *                     (an absent one: the row is not filed)                        (device, written)
- * The next step takes q_len_next and ring_state_next (swap the pointers: every workgroup reads the old ones).  Lengths
+ * The attention of this step takes q_len_next, the next step's call q_len_next and ring_state_next (swap the pointers: every
+ * workgroup reads the old ones).  Lengths
  * outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside 0 .. n_blocks are clamped.
  * A request that is over gives ALL its blocks back, each table entry as it is: the call knows no sharing, so every one of them
  * has to be a block of the pool that no other table names, else a later step hands it out while another request still reads
@@ -311,7 +314,8 @@ int kv_quantize_blk(const minikv_blk_shape *shape, int32_t n_tok, const void *K,
                     int64_t v_stride, const int32_t *slots, const minikv_blk_cache *cache, void *stream);
 
 /* out[r][hq] = softmax(sm_scale * q[r][hq] . K^T) . V over the q_len[r] tokens of request r that its table names, KV head
- * hq / (Hq/Hkv), fp32 accumulation; one launch for all requests, whatever their lengths.  A request without tokens gives
+ * hq / (Hq/Hkv), fp32 accumulation; one launch for all requests, whatever their lengths.  All q_len[r] tokens have to be filed: for
+ * a new token q_len is kv_assign_blk's q_len_next, and kv_quantize_blk runs first.  A request without tokens gives
  * zeros.  Table entries outside 0 .. n_blocks-1 count as absent: their tokens contribute nothing.  Lengths are clamped
  * to 0 .. max_blocks * block.  What lies behind a request's last token in its last block is not used, whatever it holds.
  * The raw products q . codes and the sums of exp(score - largest score) times value are formed in binary32 and must not overflow there.

@@ -466,7 +466,8 @@ def kv_quantize_blk(shape, K, V, slots, cache, stream=None):
 
 
 def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspace=None, stream=None):
-    """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous."""
+    """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous.  q_len counts filed tokens: in a step of one new
+    token each it is kv_assign_blk's q_len_next, behind kv_quantize_blk."""
     home, st = _home(stream)
     (qs, p), ws = _rows(q, shape.dtype, shape.Hq, "q", home), cache.workspace if workspace is None else workspace
     if q.shape[0] < shape.R:

@@ -212,3 +212,22 @@ def test_a_shared_prefix_through_the_end_of_its_requests(api):
     step(-1, 0, -1)
     head, n_free = s["state"].tolist()
     assert n_free == N and sorted(ring.tolist()) == list(range(N)) and s["q"].tolist() == [0, 0, 0]
+
+
+def test_a_new_token_sees_itself(api):
+    """The order of a step: assignment, filing, attention with the lengths after the step.  A request's first token gets its own value, the
+    second one, whose score is far larger, as good as its own again."""
+    shape = api.make_blk_shape(2, 2, 1, 128, 16, 4, 2, BF16)
+    cache = api.BlkCache(shape)
+    cache.K.view(torch.uint8).fill_(0x7f), cache.V.view(torch.uint8).fill_(0x7f)      # what a last use left: NaN
+    table, ring, cu, slots = ints(-1, -1, -1, -1), ints(0, 1, 2, 3), ints(0, 0, 0), ints(0, 0)
+    q_len, nxt, state, s_nxt = ints(0, 0), ints(0, 0), ints(0, 4), ints(0, 0)
+    q, out = torch.ones(2, 2, 128, dtype=BF16, device="cuda"), torch.zeros(2, 2, 128, dtype=BF16, device="cuda")
+    for k in range(3):
+        api.kv_assign_blk(shape, q_len, ints(1, 1), table, ring, state, nxt, s_nxt, cu, slots)
+        K = torch.full((2, 1, 128), 8.0 * k, dtype=BF16, device="cuda")
+        V = torch.full((2, 1, 128), 3.0 + k, dtype=BF16, device="cuda")              # (codes hold it exactly)
+        api.kv_quantize_blk(shape, K, V, slots, cache)
+        api.minikv_decode_attn_blk(shape, q, cache, table, nxt, SM, out)
+        assert bool((out == 3.0 + k).all())                                          # (the others weigh e^-90)
+        q_len, nxt, state, s_nxt = nxt, q_len, s_nxt, state
