@@ -308,6 +308,7 @@ int kv_assign_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int
  *   K, V    fp16 / bf16 [n_tok][Hkv][128], tokens k_stride, v_stride elements apart     (device, read)
  *   slots   int32 [n_tok]; rows of one block stand together (as kv_assign_blk gives them); a slot outside
  *           0 .. n_blocks * block - 1 (padding: -1) is skipped                            (device, read)
+ * Both quotients are rounded once, whatever the scale a block came with (one that is no power of two stays until it grows).
  * Two rows of one call with the same slot, or rows of one block with others (or padding) between them, leave that block's
  * contents unspecified.  Nothing else is touched.  n_tok * Hkv < 2^30. */
 int kv_quantize_blk(const minikv_blk_shape *shape, int32_t n_tok, const void *K, int64_t k_stride, const void *V,

@@ -238,6 +238,15 @@ __device__ inline float scale_for(float amax)
     return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
 }
 
+// p is the binary32 number nearest to a value and r that value less p (or 0): of the two numbers next to the value the one whose
+// last bit is set, p itself if it is the value.  Rounded on to fewer bits this gives what the value gives (p could lie on a tie that the value misses).
+__device__ inline float to_odd(float p, float r)
+{
+    const uint32_t b = __float_as_uint(p);
+    if (r == 0.0f || (b & 1)) return p;
+    return __uint_as_float((r > 0.0f) != (b >> 31) ? b + 1 : b - 1);
+}
+
 // A wave takes the runs (consecutive tokens of one block) that begin among its `chunk` tokens, for one head and one of K
 // and V (neighbouring waves take the heads of the same tokens, which lie side by side), so that a block's scale has one
 // owner and no barrier or atomic is needed.  Sixteen lanes hold a row, four rows an instruction; up to ROWS rows, a block,
@@ -305,20 +314,41 @@ __global__ __launch_bounds__(256) void quantize_blk_kernel(FileArgs a)
         if (!fresh) {
             if (old > s) s = old;
             if (s != old) {                            // every row of the block under the new scale
-                const float ratio = old / s;
+                const float ratio = old / s;           // (s is a power of two)
+                auto scaled = [&](float c) { return to_odd(c * ratio, __builtin_fmaf(c, ratio, -(c * ratio))); };
                 for (int k = lane; k < (8 << a.shift); k += 64) {
                     uint4 w = ((const uint4 *)codes)[k];
                     uint32_t *p = &w.x;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8(p[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(p[j], true);
-                        int v = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * ratio, lo[1] * ratio, 0, false);
-                        p[j] = __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * ratio, hi[1] * ratio, v, true);
+                        int v = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(lo[0]), scaled(lo[1]), 0, false);
+                        p[j] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(hi[0]), scaled(hi[1]), v, true);
                     }
                     ((uint4 *)codes)[k] = w;
                 }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // before the new rows go to places among them
             }
+        }
+        if (__builtin_amdgcn_readfirstlane(__float_as_uint(s)) & 0x7fffff) {         // the block came with a scale that is no power of two (filed ones never have it)
+            const float up = s < 1.0f ? 0x1p64f : 1.0f, by = s * up;   // (so that no remainder is subnormal)
+            auto over = [&](uint32_t bits) {
+                const float v = from16<BF16>(bits) * up, p = v / by;
+                return to_odd(p, __builtin_fmaf(-p, by, v));
+            };
+#pragma unroll 1
+            for (int row = sub; row < n; row += 4) {
+                const u4v w = *(const u4v *)(X + (int64_t)(i + row) * stride);
+                int v[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(over(w[2 * j] & 0xffff), over(w[2 * j] >> 16), 0, false);
+                    v[j] = __builtin_amdgcn_cvt_pk_fp8_f32(over(w[2 * j + 1] & 0xffff), over(w[2 * j + 1] >> 16), v[j], true);
+                }
+                *(int2 *)(codes + (a.slots[i + row] & ((1 << a.shift) - 1)) * kD + c * 8) = int2{v[0], v[1]};
+            }
+            if (lane == 0) *scale = s;
+            continue;
         }
         const float inv = s > 0.0f ? 1.0f / s : 0.0f;
         for (int base = 0; base < n; base += ROWS) {

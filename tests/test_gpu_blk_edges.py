@@ -231,3 +231,59 @@ def test_a_new_token_sees_itself(api):
         api.minikv_decode_attn_blk(shape, q, cache, table, nxt, SM, out)
         assert bool((out == 3.0 + k).all())                                          # (the others weigh e^-90)
         q_len, nxt, state, s_nxt = nxt, q_len, s_nxt, state
+
+
+# ---------------------------------------------------------------------------------------------------------
+# kv_quantize_blk
+
+def file_both(api, x, codes, scales, slots, dtype):
+    """Files x as K and -x as V into copies of one pool; checks both against the definition."""
+    N, Hkv, block, _ = codes.shape
+    shape = api.make_blk_shape(1, Hkv, Hkv, 128, block, N, 1, dtype)
+    t = [codes.clone().cuda(), scales.clone().cuda(), codes.clone().cuda(), scales.clone().cuda()]
+    cache = api.BlkCache(shape, K=t[0].view(E4M3), V=t[2].view(E4M3), Ks=t[1], Vs=t[3])
+    api.kv_quantize_blk(shape, x.cuda(), -x.cuda(), ints(*slots), cache)
+    for y, c, s in ((x, t[0], t[1]), (-x, t[2], t[3])):
+        wc, ws = blk.file_rows(y, codes, scales, torch.tensor(slots))
+        assert torch.equal(s.cpu().double(), ws)
+        assert torch.equal(blk.decode_codes(c.cpu()), blk.decode_codes(wc))
+
+
+# halfway between neighbouring codes, ordinary and subnormal ones
+TIES = [(17 + 2 * i) / 16 for i in range(8)] + [2.0 ** -10 * k for k in (1, 3, 5, 13)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("block", [16, 128])
+def test_filing_behind_a_scale_that_is_no_power_of_two(api, dtype, block):
+    """A block's scale from elsewhere: rows next to it are x / s rounded once.  The scales are those nearest to x / tie, so that the
+    quotient in 32 bits lies on the tie where the real one does not."""
+    g = torch.Generator().manual_seed(block)
+    for i, t in enumerate(TIES):
+        x = (1 + torch.rand(1, 8, 128, generator=g)).to(dtype)
+        s = (x[0, :, 0].double() / t).float()          # one x of each head decides; the others are multiples of it
+        x = (x[:, :, :1].float() * 2.0 ** -(torch.arange(128) % 9)).to(dtype).repeat(5, 1, 1)
+        scales = torch.stack([s, s * 2.0 ** -100 if dtype is BF16 else s * 0.37]) + 0.0
+        if dtype is BF16:
+            x[3:] = (x[3:].float() * 2.0 ** -100).to(dtype)
+        codes = torch.randint(0, 127, (2, 8, block, 128), generator=g).to(torch.uint8)
+        file_both(api, x, codes, scales, [5, 6, 7, block + 3, block + 4], dtype)
+
+
+def test_scales_far_below_one_are_divided_by_exactly(api):
+    """bf16 rows of 2^-118 behind scales as small: the remainder of such a quotient is below binary32's numbers."""
+    g = torch.Generator().manual_seed(2)
+    x = ((1 + torch.rand(3, 4, 128, generator=g)) * 2.0 ** -118).to(BF16)
+    for t in TIES[:8]:
+        scales = (x[0, :, 0].double() / t).float()[None]
+        file_both(api, x, torch.zeros(1, 4, 16, 128, dtype=torch.uint8), scales, [3, 4, 5], BF16)
+
+
+@pytest.mark.parametrize("block", [32, 128])
+def test_a_scale_that_is_no_power_of_two_grows(api, block):
+    """A larger row: the block's other rows are code * old / s, rounded once.  The old scales are those nearest to tie / code."""
+    codes = torch.arange(block * 128).reshape(1, 1, block, 128).remainder(127).to(torch.uint8)
+    for code in (9.0, 11.0, 13.0, 15.0):
+        old = torch.tensor([[t / code * 2.0 ** 3 for t in TIES[:8]]], dtype=torch.float64).float()
+        x = torch.full((1, 8, 128), 448.0 * 16).to(F16)
+        file_both(api, x, codes.expand(1, 8, block, 128).contiguous(), old, [1], F16)
