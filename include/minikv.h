@@ -271,7 +271,8 @@ size_t minikv_blk_cache_bytes(const minikv_blk_shape *shape, int which);
 size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
 
 /* Block tables and slot map of one step, from lengths that live on the device.  Request r wants n_new[r] more tokens
- * (0: none; negative: the request is over).  In the order of the requests, those whose new blocks still fit get them:
+ * (0: none; negative: the request is over).  Blocks are handed out in the order of the requests until one finds too few left: it and
+ * all behind it that need a block are refused (what it asked for stays counted), those that need none are not:
  *   need[r] = ceil((q_len[r] + n_new[r]) / block) - ceil(q_len[r] / block) blocks, 0 for a request that is over, that
  *   would need more than max_blocks in all or whose tokens end behind slots[n_slots - 1]; it is ACCEPTED if none of
  *   the last three holds and need[r] is 0 or need[0] + ... + need[r] <= n_free.
@@ -288,8 +289,8 @@ size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
  *                     the rows of a request that was not accepted, behind cu[R], and of a block outside 0 .. n_blocks-1
  *                     (an absent one: the row is not filed)                        (device, written)
  * The attention of this step takes q_len_next, the next step's call q_len_next and ring_state_next (swap the pointers: every
- * workgroup reads the old ones).  Lengths
- * outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside 0 .. n_blocks are clamped.
+ * workgroup reads the old ones).  Lengths outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside
+ * 0 .. n_blocks are clamped.
  * A request that is over gives ALL its blocks back, each table entry as it is: the call knows no sharing, so every one of them
  * has to be a block of the pool that no other table names, else a later step hands it out while another request still reads
  * it, or hands it out twice.  A request with shared or absent blocks is ended by the program instead, between two steps and in the
@@ -304,7 +305,7 @@ int kv_assign_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int
  *   rows already there: if a new row goes to the block's offset 0 the block starts afresh (whatever scale and rows its last
  *   use left do not count), else s becomes at least the block's scale, and where it is larger all the block's other rows are
  *   re-expressed: code = e4m3_rne(code * old scale / s);
- *   new rows: code = e4m3_rne(x / s) (round to nearest, ties to even, subnormal codes included), 0 if s is 0.
+ *   new rows: code = e4m3_rne(x / s) (round to nearest, ties to even, subnormal codes included), 0 of x's sign if s is 0.
  *   K, V    fp16 / bf16 [n_tok][Hkv][128], tokens k_stride, v_stride elements apart     (device, read)
  *   slots   int32 [n_tok]; rows of one block stand together (as kv_assign_blk gives them); a slot outside
  *           0 .. n_blocks * block - 1 (padding: -1) is skipped                            (device, read)

@@ -398,7 +398,8 @@ def make_blk_shape(R, Hq, Hkv, D, block, n_blocks, max_blocks, dtype):
 
 class BlkCache:
     """Caller-owned device buffers of one paged 8-bit cache, sized by minikv_blk_cache_bytes; given ones are taken as they are.
-    K, V: float8_e4m3fn [n_blocks][Hkv][block][128]; Ks, Vs: float32 [n_blocks][Hkv]; and the attention's workspace."""
+    K, V: float8_e4m3fn [n_blocks][Hkv][block][128]; Ks, Vs: float32 [n_blocks][Hkv]; and a workspace of the attention, for calls on
+    one stream at a time."""
 
     def __init__(self, shape, device="cuda", K=None, V=None, Ks=None, Vs=None):
         self.shape = shape
@@ -467,7 +468,8 @@ def kv_quantize_blk(shape, K, V, slots, cache, stream=None):
 
 def minikv_decode_attn_blk(shape, q, cache, table, q_len, sm_scale, out, workspace=None, stream=None):
     """q: [R][Hq][128], possibly a slice of a fused projection; out: contiguous.  q_len counts filed tokens: in a step of one new
-    token each it is kv_assign_blk's q_len_next, behind kv_quantize_blk."""
+    token each it is kv_assign_blk's q_len_next, behind kv_quantize_blk.  workspace: the cache's own if not given; calls on different
+    streams that may overlap need one each (zero-filled once)."""
     home, st = _home(stream)
     (qs, p), ws = _rows(q, shape.dtype, shape.Hq, "q", home), cache.workspace if workspace is None else workspace
     if q.shape[0] < shape.R:
