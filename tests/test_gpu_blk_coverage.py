@@ -24,7 +24,7 @@ def count(api, lens, Hq, Hkv, block, dtype, absent=()):
     the request's tokens in its channel: weights, their products with the scales and sums of up to 2^24 of them are exact, the quotient
     passes two roundings in fp32 and one to its type."""
     need = [-(-n // block) for n in lens]
-    N, width = sum(need) + 1, max(need)
+    N, width = sum(need) + 1, max(max(need), 1)
     t = tables(lens, block, width, N, 3)
     Kc, Ks = rand_cache(N, Hkv, block, 4, 2) if N * Hkv * block < 40000 else (torch.zeros(N, Hkv, block, 128, dtype=torch.uint8), torch.ones(N, Hkv))
     power = torch.arange(N) % 3
@@ -111,3 +111,86 @@ def test_the_prompts_beside_one_that_does_not_fit(api, cu, good):
     assert bool(((got[2][2 * a:2 * e].double() - want[2]).abs() <= want[2] * (rel + float(ltol.max()) + 80 * 2.0 ** -24) + 1e-30).all())
     for x, f in ((got[0], 1), (got[1], 2), (got[2], 2)):
         assert bool((x[:a * f] == 7.0).all()) and bool((x[e * f:] == 7.0).all())
+
+
+def test_the_largest_batches(api):
+    """8192 requests, most of local memory taken by their lengths; 8192 prompts, whose counts take a tile of the second pass."""
+    count(api, [(i * 7) % 50 if i % 3 else 0 for i in range(8191)] + [5000], 2, 1, 16, F16)
+    count(api, [0] * 8192, 1, 1, 128, BF16)
+    count(api, [0] * 8191 + [1], 8, 8, 64, BF16)
+    for lens in ([i % 2 for i in range(8192)], [0] * 8000 + [300] + [0] * 190 + [170]):
+        cu = [0] + torch.tensor(lens).cumsum(0).tolist()
+        Q, K, V = fused(cu[-1], 2, 1, BF16, 3)
+        for scores in (True, False):
+            X, lse, A = run(api, Q, K, V, cu, scores)
+            want = blk.prompt_attn(Q, K, V, [c for i, c in enumerate(cu) if i == 0 or c > cu[i - 1]], SM)
+            tol = attn_tolerance(want[0], want[3], want[4], max(lens), float(V.abs().max()), HALF[BF16], BF16)
+            assert bool(((X.double() - want[0]).abs() <= tol).all())
+            rel = 137 * 2.0 ** -24 * want[4] * 1.01
+            ltol = rel + 4 * 2.0 ** -24 * (want[1].abs() + want[4] + 1)
+            assert bool(((lse.double() - want[1]).abs() <= ltol).all())
+            if scores:
+                assert bool(((A.double() - want[2]).abs() <= want[2] * (rel + float(ltol.max()) + 80 * 2.0 ** -24) + 1e-30).all())
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 1), (24, 2), (10, 1)])
+def test_more_than_eight_query_heads_of_a_kv_head(api, Hq, Hkv):
+    """The packed prompts have no bound of their own on the heads that share keys."""
+    for lens in ([100, 28], [333, 1, 90], [1200]):
+        cu = [0] + torch.tensor(lens).cumsum(0).tolist()
+        Q, K, V = fused(cu[-1], Hq, Hkv, F16, 4)
+        X, lse, A = run(api, Q, K, V, cu, True)
+        want = blk.prompt_attn(Q, K, V, cu, SM)
+        tol = attn_tolerance(want[0], want[3], want[4], max(lens), float(V.abs().max()), HALF[F16], F16)
+        assert bool(((X.double() - want[0]).abs() <= tol).all())
+        rel = 137 * 2.0 ** -24 * want[4] * 1.01
+        ltol = rel + 4 * 2.0 ** -24 * (want[1].abs() + want[4] + 1)
+        assert bool(((lse.double() - want[1]).abs() <= ltol).all())
+        assert bool(((A.double() - want[2]).abs() <= want[2] * (rel + float(ltol.max()) + (max(lens) / 64 + 80) * 2.0 ** -24) + 1e-30).all())
+
+
+def test_attention_captured_and_replayed_with_other_lengths(api):
+    """One captured call whose requests grow, shrink and end between replays: a workgroup per unit, several, the line of work, nothing."""
+    R, Hq, Hkv, block, width = 40, 16, 8, 32, 300
+    N = R * width
+    gen = torch.Generator().manual_seed(8)
+    shape = api.make_blk_shape(R, Hq, Hkv, 128, block, N, width, BF16)
+    codes = [torch.randint(0, 120, (N, Hkv, block, 128), generator=gen, dtype=torch.uint8).cuda() for _ in range(2)]
+    ones = torch.full((N, Hkv), 2.0 ** -8, device="cuda")
+    cache = api.BlkCache(shape, K=codes[0].view(E4M3), V=codes[1].view(E4M3), Ks=ones, Vs=ones.clone())
+    table = torch.arange(N, dtype=torch.int32).view(R, width).cuda()
+    q = torch.randn(R, Hq, 128, generator=gen).bfloat16().cuda()
+    n, out, want = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros_like(q), torch.zeros_like(q)
+    own = torch.zeros_like(cache.workspace)
+    api.minikv_decode_attn_blk(shape, q, cache, table, n, SM, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        api.minikv_decode_attn_blk(shape, q, cache, table, n, SM, out)
+    for lens in ([0] * R, [40] * R, [9600] * 3 + [1] * 37, [0] * 39 + [9000], [i * 200 for i in range(R)], [9600] * R, [0] * R, [5] + [0] * 39):
+        n.copy_(torch.tensor(lens, dtype=torch.int32))
+        out.fill_(float("nan"))
+        g.replay()
+        api.minikv_decode_attn_blk(shape, q, cache, table, n, SM, want, workspace=own)
+        assert torch.equal(out, want)
+        for r in (0, R - 1):                           # (against the definition: two requests of each)
+            k = (lens[r] + block - 1) // block
+            some = [c[r * width:r * width + max(k, 1)].cpu() for c in codes]
+            s = torch.full((max(k, 1), Hkv), 2.0 ** -8)
+            exact, mean, score = blk.decode_attn(q[r:r + 1].cpu(), some[0], s, some[1], s, torch.arange(max(k, 1)).view(1, -1), [lens[r]], SM)
+            tol = attn_tolerance(exact, mean, score, max(lens[r], 1), 448 * 2.0 ** -8, 2.0 ** -11, BF16)
+            assert bool(((out[r:r + 1].cpu().double() - exact).abs() <= tol).all())
+
+
+def test_keys_and_values_of_different_strides(api):
+    """Keys as a slice of a projection, values standing alone, and the other way round."""
+    g = torch.Generator().manual_seed(5)
+    shape = api.make_blk_shape(3, 2, 2, 128, 32, 6, 2, F16)
+    wide, alone = torch.randn(70, 7, 128, generator=g).half().cuda(), torch.randn(70, 2, 128, generator=g).half().cuda()
+    slots = torch.arange(96, 166, dtype=torch.int32, device="cuda")
+    for K, V in ((wide[:, 3:5], alone), (alone, wide[:, 5:])):
+        cache = api.BlkCache(shape)
+        api.kv_quantize_blk(shape, K, V, slots, cache)
+        for x, c, s in ((K, cache.K, cache.Ks), (V, cache.V, cache.Vs)):
+            wc, ws = blk.file_rows(x.cpu(), torch.zeros(6, 2, 32, 128, dtype=torch.uint8), torch.zeros(6, 2), slots.cpu())
+            assert torch.equal(s.cpu().double(), ws) and torch.equal(blk.decode_codes(c.view(torch.uint8).cpu()), blk.decode_codes(wc))
