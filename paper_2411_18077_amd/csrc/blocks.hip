@@ -15,7 +15,7 @@ struct AssignArgs {
 
 constexpr int kAsThreads = 1024;
 constexpr int kAsMost = kMaxRequests / kAsThreads;     // requests of a thread, consecutive ones
-constexpr int kAsFew = 8;                              // rows of a request that its own thread writes the slots of
+constexpr int kAsFew = 3;                              // rows of all its requests that a thread writes the slots of itself
 constexpr uint32_t kRefused = 0x80000000u;
 
 // Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap <= 2^31;
@@ -64,12 +64,13 @@ __device__ inline int find(const uint32_t *v, int n, uint32_t x)
 }
 
 // Every workgroup scans all the requests (two scans: rows first, because a request whose rows do not fit asks for no blocks).
-// Where no request has more than kAsFew new rows, a decoding step, its thread writes its slots and table entries; else three
-// prefix sums in local memory make slots, table entries and returned blocks three flat loops over the grid, each element
-// finding its request by bisection.  New slots are computed from the ring, not from the table entries that another
+// Where no thread has more than kAsFew new rows in all (at most so many each of its one to eight requests), a decoding step, it writes
+// their slots and table entries itself; else three prefix sums in local memory make slots, table entries and returned blocks three
+// flat loops over the grid, each element finding its request by bisection.  Us, own thread / loops: 256 requests of 1 row 3.9 / 5.2,
+// of 3 4.8 / 5.4, of 4 5.2 / 5.5, of 8 7.5 / 6.0; 1024 of 3 6.3 / 6.5, of 4 7.6 / 6.7; 1500 of 1 5.5 / 6.5, of 2 7.1 / 6.8; 3000 of 1 7.5 /
+// 7.8; 8192 of 1 27.8 / 20.9, of 8 103 / 22.  New slots are computed from the ring, not from the table entries that another
 // workgroup may not have written yet, so one launch does it all and nothing waits for anything.  What bounds it is latency, two
-// dependent loads and the scans: 4.2 us for a step of 256 requests (9.0 by bisection, with scans through local memory), 7 for 64
-// prompts of 131072 tokens, 9 for 1000 of 100000.
+// dependent loads and the scans: 4.2 us for a step of 256 requests, 6.4 for 64 prompts of 131072 tokens, 9 for 1000 of 100000.
 __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
 {
     extern __shared__ uint32_t lds[];
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
             sum[0] = sat_add(sum[0], max(add[j], 0), kRows), largest = max(largest, (uint32_t)max(add[j], 0));
         }
     block_scan(sum, {kRows}, part, total);
-    if (largest > kAsFew) many = 1;
+    if (largest > kAsFew || largest * per > kAsFew) many = 1;
     uint32_t row[kAsMost], nd[kAsMost], ov[kAsMost], at = sum[0];
 #pragma unroll
     for (int j = 0; j < kAsMost; ++j)                  // (need <= new rows <= n_slots in all: no overflow)

@@ -287,3 +287,26 @@ def test_a_scale_that_is_no_power_of_two_grows(api, block):
         old = torch.tensor([[t / code * 2.0 ** 3 for t in TIES[:8]]], dtype=torch.float64).float()
         x = torch.full((1, 8, 128), 448.0 * 16).to(F16)
         file_both(api, x, codes.expand(1, 8, block, 128).contiguous(), old, [1], F16)
+
+
+@pytest.mark.parametrize("R", [1, 5, 1024, 1025, 2048, 2049, 3500, 8192])
+@pytest.mark.parametrize("new", [0, 1, 2, 3, 4])
+def test_assignment_on_both_sides_of_its_rule(api, R, new):
+    """Threads with one to eight requests, of no more rows each than they write themselves and of one more: the definition's numbers."""
+    block, width, N = 16, 3, 2 * R + 7
+    q_len = [(7 * r) % 33 for r in range(R)]
+    n_new = [-1 if r % 11 == 3 else new if r % 5 else min(new, 1) for r in range(R)]
+    ids = iter(torch.randperm(N, generator=torch.Generator().manual_seed(R)).tolist())
+    table = [[next(ids) if 16 * b < n else -1 for b in range(width)] for n in q_len]
+    ring = list(ids)
+    n_free = min(len(ring), R // 3 + 1)
+    ring += [-1] * (N - len(ring))
+    n_slots = sum(max(n, 0) for n in n_new) + 3
+    want = blk.assign(q_len, n_new, table, ring, [0, n_free], block, n_slots)
+    t, g, q, s = ints(*sum(table, [])), ints(*ring), ints(*[-9] * R), ints(-9, -9)
+    cu, slots = ints(*[-9] * (R + 1)), ints(*[-9] * n_slots)
+    shape = api.make_blk_shape(R, 1, 1, 128, block, N, width, F16)
+    api.kv_assign_blk(shape, ints(*q_len), ints(*n_new), t, g, ints(0, n_free), q, s, cu, slots)
+    got = dict(table=t.view(R, width).tolist(), ring=g.tolist(), q_len=q.tolist(), state=s.tolist(), cu=cu.tolist(), slots=slots.tolist())
+    for k in want:
+        assert got[k] == want[k], k
