@@ -18,9 +18,9 @@ constexpr int kAsMost = kMaxRequests / kAsThreads;     // requests of a thread, 
 constexpr int kAsFew = 3;                              // rows of all its requests that a thread writes the slots of itself
 constexpr uint32_t kRefused = 0x80000000u;
 
-// Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap <= 2^31;
+// Sums saturate: lengths come from the device and may be anything, what is indexed with them may not.  (a, b <= cap < 2^31;
 // min(a + b, cap) is associative, so a scan in any order gives the same.)
-__device__ inline uint32_t sat_add(uint32_t a, uint32_t b, uint32_t cap) { return min(__builtin_elementwise_add_sat(a, b), cap); }
+__device__ inline uint32_t sat_add(uint32_t a, uint32_t b, uint32_t cap) { return min(a + b, cap); }
 template <int CTRL, int ROWS> __device__ inline uint32_t sat_step(uint32_t v, uint32_t cap)
 {
     return sat_add(v, (uint32_t)__builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false), cap);
@@ -79,8 +79,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
     const int tid = threadIdx.x, gtid = blockIdx.x * kAsThreads + tid, gsize = gridDim.x * kAsThreads;
     const int64_t most = (int64_t)a.width << a.shift;
     const int head = min(max(a.state[0], 0), a.N - 1), n_free = min(max(a.state[1], 0), a.N);
-    const uint32_t kRows = 0x80000000, kMostRows = 0x7fffffff;          // where sums of rows saturate (behind any slot), and the largest that is passed on
-    const uint32_t back = a.N - n_free;                // blocks that can come back
+    const uint32_t kRows = 0x7fffffff, back = a.N - n_free;            // blocks that can come back
     const uint32_t unit = (1u << a.shift) - 1;
 
     auto len_of = [&](int r) { return (int)min((int64_t)max(a.q_len[r], 0), most); };
@@ -100,13 +99,18 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
         }
     block_scan(sum, {kRows}, part, total);
     if (largest > kAsFew || largest * per > kAsFew) many = 1;
+    int end = a.R;                                     // requests from here on lie behind the slots although the saturated sum does not tell
+    if (total[0] == kRows && (uint32_t)a.n_slots == kRows) {
+        int64_t exact = 0;
+        for (end = 0; end < a.R && (exact += max(a.n_new[end], 0)) <= kRows; ++end);
+    }
     uint32_t row[kAsMost], nd[kAsMost], ov[kAsMost], at = sum[0];
 #pragma unroll
     for (int j = 0; j < kAsMost; ++j)                  // (need <= new rows <= n_slots in all: no overflow)
         if (j < mine) {
             const uint32_t more = max(add[j], 0), after = blocks((uint32_t)len[j] + more), held = blocks(len[j]);
             row[j] = at, at = sat_add(at, more, kRows);
-            const bool fits = add[j] >= 0 && after <= (uint32_t)a.width && at <= (uint32_t)a.n_slots;
+            const bool fits = add[j] >= 0 && after <= (uint32_t)a.width && at <= (uint32_t)a.n_slots && r0 + j < end;
             nd[j] = fits ? after - held : kRefused;
             ov[j] = add[j] < 0 ? min(held, back) : 0;
             sums[0] += nd[j] & ~kRefused, sums[1] = sat_add(sums[1], ov[j], back);
@@ -122,12 +126,12 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
             take += n;
             const bool ok = !(nd[j] & kRefused) && (n == 0 || take <= (uint32_t)n_free);
             if (ok && n) pop = take;                   // (ascending in the accepted ones)
-            if (!few) rows[r] = min(row[j], kMostRows), need[r] = first | (ok ? 0u : kRefused);
+            if (!few) rows[r] = row[j], need[r] = first | (ok ? 0u : kRefused);
             if (totals[1]) over[r] = give;
             give = sat_add(give, ov[j], back);
             if (blockIdx.x == 0) {
                 a.q_len_next[r] = add[j] < 0 ? 0 : ok ? len[j] + add[j] : len[j];
-                a.cu[r] = (int)min(row[j], kMostRows);
+                a.cu[r] = (int)row[j];
                 if (few) {
                     const int held = (int)blocks(len[j]);
                     int32_t *entry = a.table + (int64_t)r * a.width;
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
     __syncthreads();
     pop = popped;
     if (blockIdx.x == 0 && tid == 0) {
-        a.cu[a.R] = (int)min(total[0], kMostRows);
+        a.cu[a.R] = (int)total[0];
         a.state_next[0] = (int)wrap(head + pop), a.state_next[1] = n_free - (int)pop + (int)totals[1];
     }
     if (few) {
