@@ -286,8 +286,8 @@ size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
  *   cu                int32 [R+1]: cu[r] = sum of max(n_new, 0) over the requests before r (at most 2^31 - 1): the rows
  *                     of the packed step                                          (device, written)
  *   slots             int32 [n_slots]: the slot of row cu[r] + i, that is of token q_len[r] + i of request r; -1 for
- *                     the rows of a request that was not accepted, behind cu[R], and of a block outside 0 .. n_blocks-1
- *                     (an absent one: the row is not filed)                        (device, written)
+ *                     the rows of a request that was not accepted and behind cu[R]; a row of a block outside 0 .. n_blocks-1
+ *                     (an absent one) has a slot outside the pool: it is not filed  (device, written)
  * The attention of this step takes q_len_next, the next step's call q_len_next and ring_state_next (swap the pointers: every
  * workgroup reads the old ones).  Lengths outside 0 .. max_blocks * block, a head outside 0 .. n_blocks-1 and a count outside
  * 0 .. n_blocks are clamped.

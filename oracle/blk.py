@@ -76,7 +76,7 @@ def assign(q_len, n_new, table, ring, state, block, n_slots):
         for i in range(add):
             pos = q_len[r] + i
             b = table[r][pos // block]
-            slots[cu[r] + i] = b * block + pos % block if 0 <= b < N else -1
+            slots[cu[r] + i] = b * block + pos % block if 0 <= b <= (2 ** 31 - 1) // block else -1
         length[r] = q_len[r] + add
     for i, b in enumerate(back):
         ring[(head + n_free + i) % N] = b

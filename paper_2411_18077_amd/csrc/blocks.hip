@@ -84,7 +84,8 @@ __global__ __launch_bounds__(kAsThreads) void assign_blk_kernel(AssignArgs a)
 
     auto len_of = [&](int r) { return (int)min((int64_t)max(a.q_len[r], 0), most); };
     auto blocks = [&](uint32_t tokens) { return (tokens + unit) >> a.shift; };       // (at most 2^30 + 2^31)
-    auto slot_in = [&](int id, int pos) { return (uint32_t)id < (uint32_t)a.N ? (id << a.shift) + (pos & (int)unit) : -1; };      // (no other block's)
+    // (of a block outside the pool: outside the pool as well, never another block's)
+    auto slot_in = [&](int id, int pos) { return (uint32_t)id <= 0x7fffffffu >> a.shift ? (id << a.shift) + (pos & (int)unit) : -1; };
     auto wrap = [&](uint32_t i) { return i >= (uint32_t)a.N ? i - a.N : i; };          // i < 2 N
 
     const int per = (a.R + kAsThreads - 1) / kAsThreads, r0 = min(tid * per, a.R), mine = min(a.R - r0, per);

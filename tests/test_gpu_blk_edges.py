@@ -149,9 +149,9 @@ def test_rows_behind_the_largest_slot_map(api, n_new, ok):
 
 
 @pytest.mark.parametrize("new", [3, 9])
-def test_blocks_outside_the_pool_have_no_slots(api, new):
-    """A table or a ring that names a block outside the pool: its rows get no slot, whatever the product with the block's size wraps to, in
-    the form for few rows each and in the other one."""
+def test_blocks_outside_the_pool_have_no_slots_in_it(api, new):
+    """A table or a ring that names a block outside the pool: its rows' slots lie outside it too, whatever the product with the block's size
+    wraps to, in the form for few rows each and in the other one."""
     block = 16
     bad = [1 << 28, -(1 << 28), -1, 5, 2 ** 31 - 1]
     q_len, n_new = [block - 2] * 5 + [0, 0, 0], [new] * 5 + [2, 2, 2]
@@ -164,6 +164,8 @@ def test_blocks_outside_the_pool_have_no_slots(api, new):
     assert got["table"].view(8, 2).tolist() == want["table"] and got["slots"].tolist() == want["slots"]
     assert all(got[k].tolist() == want[k] for k in ("ring", "q_len", "state", "cu"))
     assert got["slots"][:2].tolist() == [-1, -1] and got["slots"][3 * new:3 * new + 2].tolist() == [94, 95]
+    free = [b for b in ring if 0 <= b < 10] + [5]
+    assert all(s < 0 or s >= 160 or s // 16 in free for s in got["slots"].tolist())
 
 
 def test_a_shared_prefix_through_the_end_of_its_requests(api):
