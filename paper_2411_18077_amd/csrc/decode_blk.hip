@@ -38,10 +38,13 @@ constexpr float kBkNone = -3.0e38f;                    // running maximum before
 constexpr float kBkHeadroom = 32768.0f;                // fp16 weights run to 65504
 constexpr int kBkFar = 12 << 23;                       // V scales whose bits (of positive floats) differ by more lie more than 2^12 apart
 constexpr float kBkLeast = 0x1p-110f, kBkRange = 0x1p-100f;            // the reference: at least this, and this times the largest V scale (no quotient overflows)
-// What a unit costs a wave besides its tiles (table, scales, queries, output), in tiles on the line of work.
+// What a unit costs a wave besides its tiles (table, scales, queries, output), in tiles on the line of work.  Us with 0 / 1 / 2, 8 KV heads: 1000
+// requests of 1 to 300 tokens 53.0 / 52.0 / 56.1, 48 of 1 to 16000 57.4 / 48.7 / 48.4, 200 of 120 16.6 each, 100 of 1 to 2000 25.7 / 27.2 / 26.7;
+// 400 of 700, one KV head, 32.1 / 24.3 / 28.4.
 constexpr int kBkUnitCost = 1;
 // Workgroups of their own for every unit beat the line of work (where there are enough of them) while their waves have at most so
-// many tiles more than the line's.
+// many tiles more than the line's.  Us with 1 / 3 / 6 / 12, 8 KV heads: 32 requests of 1 to 2000 tokens 22.8 / 14.3 / 14.3 / 14.3, of 1 to 4000 23.1 /
+// 23.1 / 22.2 / 22.2, of 1 to 8000 23.5 / 23.5 / 23.5 / 36.0; 16 of 1 to 5000 21.6 / 21.6 / 25.6 / 25.5; 24 of 1 to 8000 23.8 / 23.8 / 23.8 / 41.0.
 constexpr int kBkUnitTiles = 3;
 
 struct BlkArgs {
@@ -71,7 +74,9 @@ __device__ inline float lo8(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ inline float hi8(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
 
 // Codes are read once a call, and a program's other layers have caches of their own before this one's turn comes again: loaded
-// with the streaming hint (16 requests of 32768 tokens 195 -> 178 us, 6.0 TB/s; one of 131072 59 -> 56).
+// with the streaming hint (without -> with: 16 requests of 32768 tokens 185 -> 166 us, one of 131072 56.0 -> 50.9, 48 of 1 to 16000 51.2 -> 48.7, 1000
+// of 1 to 300 50.6 -> 51.8).  Where requests share their blocks, which a call cannot tell, it costs: 64 requests of 100 tokens behind one
+// prefix of 8192 104 -> 151, behind one of 2048 40 -> 55, 32 of 4096 behind one of 4096 59 -> 67.
 __device__ inline uint4 load_codes(const uint8_t *p)
 {
     typedef uint32_t u4v __attribute__((ext_vector_type(4)));
@@ -165,10 +170,10 @@ template <bool BF16> __device__ inline uint32_t pack2(float a, float b)
 //   power of two of them with about four tiles each, so that every SIMD has one.  (A wave's tile is 2800 cycles of one SIMD, most of them
 //   conversions, and merging between workgroups 4000.)
 // What bounds it: memory, where there is much to read (16 requests of 32768 tokens, 8 KV heads, 1.07 GB: 166 us, 6.5 TB/s, a plain
-// streaming read reaches 6.0; one of 131072 tokens 51 us, 5.3 TB/s; 48 of 1 to 16000 tokens 48 us, 4.2 TB/s); round trips and the
-// first pass through the code where there is little (8 heads of 1024 tokens 7.7 us); the conversions and what a unit costs besides
-// its tiles where there are many short ones (1000 requests of 1 to 300 tokens 47 us).  With a workgroup's four waves on the same unit
-// and a barrier for each, the 48 took 130 us, the 1024 tokens 9.1; on the line alone the 16 took 178 and the 1024 tokens 11.4.
+// streaming read reaches 6.0; one of 131072 tokens 50.3 us, 5.3 TB/s; 48 of 1 to 16000 tokens 48.6 us, 4.2 TB/s); round trips and the
+// first pass through the code where there is little (8 heads of 1024 tokens 7.6 us); the conversions and what a unit costs besides
+// its tiles where there are many short ones (1000 requests of 1 to 300 tokens 52 us).  Earlier forms: a workgroup of four waves on one
+// unit at a time, with a barrier for each, 130 us for the 48 and 9.1 for the 1024 tokens; the line alone 178 for the 16, 11.4 for the 1024 tokens.
 template <int BS, bool BF16>
 __global__ __launch_bounds__(kBkThreads, 2) void decode_blk_kernel(BlkArgs a)
 {

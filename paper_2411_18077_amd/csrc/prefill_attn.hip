@@ -45,7 +45,8 @@ struct PrefillArgs {
     unsigned q_pitch, k_pitch, v_pitch;
 };
 
-// 16-bit operands are kept as halves whatever they are; BF16 instances differ in the product and in the two roundings.
+// 16-bit operands are kept as halves whatever they are; BF16 instances differ in the product and in the two roundings (a product's operands
+// are of one type, and bf16 values leave fp16's range, so the weights have bf16's 8 bits there).
 typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
 
 template <bool BF16 = false>
@@ -918,6 +919,10 @@ static int launch_packed(PrefillArgs a, bool scores, hipStream_t st)
     // Which form, by the rules for prompts of one length (launch_prefill) with the longest prompt as the length and an upper
     // bound of the blocks, which is what the host knows; but never 256 queries a workgroup, which gains nothing where four heads side
     // by side share the keys and loses elsewhere (8 prompts of 16000 tokens, 32 heads each with keys of its own, 521 against 545 us).
+    // On uneven batches, outputs only, us by the rules / in the best of the four forms: 15 prompts of 30 tokens beside one of 2000, 8 heads
+    // 28.7 / 28.2, 32 heads on 8 KV heads 49.2 / 49.2; 1000 + 200 + 60 16.2 / 15.8, 24.4 / 23.7; 500 + 30 x 20 11.2 / 11.2, 15.5 / 15.5; 777 + 100 14.5 / 14.4,
+    // 17.8 / 17.8; bounds of eight times the longest prompt the same.  Of 8 heads the many blocks of short prompts beside a long one mislead
+    // them: 6000 + 7 x 50 111 / 98, 3000 + 8 x 200 51.8 / 40.8.
     const int64_t heads = (int64_t)a.B * a.Hq;
     auto blocks = [&](int rows) { return a.Hq * per_head(rows); };
     const bool two_buffers = a.max_len > 96 && 2 * blocks(64) <= (heads <= 20 ? 3 : 2) * kComputeUnits;
