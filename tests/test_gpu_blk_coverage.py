@@ -194,3 +194,39 @@ def test_keys_and_values_of_different_strides(api):
         for x, c, s in ((K, cache.K, cache.Ks), (V, cache.V, cache.Vs)):
             wc, ws = blk.file_rows(x.cpu(), torch.zeros(6, 2, 32, 128, dtype=torch.uint8), torch.zeros(6, 2), slots.cpu())
             assert torch.equal(s.cpu().double(), ws) and torch.equal(blk.decode_codes(c.view(torch.uint8).cpu()), blk.decode_codes(wc))
+
+
+def test_a_step_of_prompts_and_decoding_requests(api):
+    """One step in which requests begin, go on and end, on what kv_assign_blk left on the device: the packed call takes its cu as it is (requests
+    that go on are prompts of one token there), the cache gets all rows, and the decoding requests attend with the lengths after the step."""
+    R, Hq, Hkv, block, width, N, T = 6, 8, 2, 32, 8, 40, 300
+    shape = api.make_blk_shape(R, Hq, Hkv, 128, block, N, width, F16)
+    cache = api.BlkCache(shape)
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, ring, cu, slots = i([-1] * (R * width)), i(list(range(N))), i([0] * (R + 1)), i([0] * T)
+    now, nxt, state, s_nxt = i([0] * R), i([0] * R), i([0, N]), i([0, 0])
+    for k, plan in enumerate(([70, 0, 33, 1, 0, 20], [1, 90, 1, 1, 0, -1], [1, 1, 64, -1, 5, 130])):        # (request 2 gets 64 more: filed only)
+        api.kv_assign_blk(shape, now, i(plan), table, ring, state, nxt, s_nxt, cu, slots)
+        now, nxt, state, s_nxt = nxt, now, s_nxt, state
+        Q, K, V = fused(T, Hq, Hkv, F16, 20 + k)       # (rows of no request behind the step's)
+        X, lse = torch.full((T, Hq, 128), 7.0, dtype=F16, device="cuda"), torch.full((T * Hq,), 7.0, device="cuda")
+        api.selective_flash_attn_packed(R, Hq, Hkv, T, max(plan), Q, K, V, cu, SM, X, lse, None)
+        api.kv_quantize_blk(shape, K, V, slots, cache)
+        at = [sum(max(n, 0) for n in plan[:r]) for r in range(R + 1)]
+        assert cu.tolist() == at
+        rows = [a for j, a in enumerate(at) if j == 0 or a > at[j - 1]]
+        want = blk.prompt_attn(Q[:at[-1]], K[:at[-1]], V[:at[-1]], rows, SM)
+        tol = attn_tolerance(want[0], want[3], want[4], max(plan), float(V.abs().max()), HALF[F16], F16)
+        assert bool(((X[:at[-1]].double() - want[0]).abs() <= tol).all()) and bool((X[at[-1]:] == 7.0).all())
+        assert bool((lse[at[-1] * Hq:] == 7.0).all())
+        for r, n in enumerate(plan):                   # a single token's own value
+            if n == 1:
+                assert torch.equal(X[at[r]], V[at[r]].repeat_interleave(Hq // Hkv, 0))
+        q = torch.randn(R, Hq, 128, generator=torch.Generator().manual_seed(k)).half()
+        out = torch.full((R, Hq, 128), float("nan"), dtype=F16, device="cuda")
+        api.minikv_decode_attn_blk(shape, q.cuda(), cache, table, now, SM, out)
+        codes = [c.view(torch.uint8).cpu() for c in (cache.K, cache.V)]
+        exact, mean, score = blk.decode_attn(q, codes[0], cache.Ks.cpu(), codes[1], cache.Vs.cpu(), table.view(R, width).cpu(), now.tolist(), SM)
+        tol = attn_tolerance(exact, mean, score, 300, 6.0, 2.0 ** -11, F16)
+        assert bool(((out.cpu().double() - exact).abs() <= tol).all())
+    assert now.tolist() == [72, 91, 98, 0, 5, 130]
