@@ -230,10 +230,14 @@ int minikv_decode_attn_pt(const minikv_pt_shape *shape, const minikv_f16 *q, con
 /* ---------------------------------------------------------------------------------------------------------
  * Variant: a paged 8-BIT cache for batches whose requests come and go, and attention of packed prompts of
  * different lengths -- what a serving loop needs around the calls above when its requests do not share one length.
- * Four entry points, used in this order in every step: kv_assign_blk (blocks, slots and the lengths after the step), kv_quantize_blk
+ * Entry points, used in this order in every step: kv_assign_blk (blocks, slots and the lengths after the step), minikv_norm_rope (norms
+ * and position rotation of queries and keys, where the model has them), kv_quantize_blk
  * (filing of the new rows at their slots), then attention: minikv_decode_attn_blk (one new token per request, with the lengths
- * AFTER the step, so that the token attends to itself as well; its row has to be filed by then) or
- * selective_flash_attn_packed (new prompts; it reads the rows as they are, not the cache, and may run before the filing).
+ * AFTER the step, so that the token attends to itself as well; its row has to be filed by then), minikv_prompt_attn_blk (any number of new
+ * tokens per request behind what it holds, a step of prompts and decoding requests together; the same lengths, the rows filed as well) or
+ * selective_flash_attn_packed (new prompts alone; it reads the rows as they are, not the cache, and may run before the filing).
+ * Between steps: kv_fork_blk and kv_copy_blk (requests that begin with what another one holds), kv_free_blk (blocks of requests that
+ * are over, where blocks are shared), kv_compact_blk and kv_copy_blk (the used blocks moved to the front of the pool).
  *
  * The cache is a pool of n_blocks blocks of `block` tokens.  Block i of KV head h holds `block` rows of 128 codes
  * in 8-bit floating point (e4m3: 4 exponent and 3 mantissa bits, largest value 448) for keys and as many for
@@ -295,7 +299,7 @@ size_t minikv_blk_workspace_bytes(const minikv_blk_shape *shape);
  * has to be a block of the pool that no other table names, else a later step hands it out while another request still reads
  * it, or hands it out twice.  A request with shared or absent blocks is ended by the program instead, between two steps and in the
  * arrays that the next one reads: q_len[r] = 0, and those of its blocks that no table names any more go to ring[(head + n_free)
- * % n_blocks] one by one, n_free counting them. */
+ * % n_blocks] one by one, n_free counting them, or all at once by kv_free_blk. */
 int kv_assign_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *n_new, int32_t *table,
                   int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *ring_state_next, int32_t *cu,
                   int32_t *slots, int32_t n_slots, void *stream);
@@ -332,6 +336,100 @@ int kv_quantize_blk(const minikv_blk_shape *shape, int32_t n_tok, const void *K,
 int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t q_stride, const minikv_blk_cache *cache,
                            const int32_t *table, const int32_t *q_len, float sm_scale, void *out, void *workspace,
                            size_t workspace_bytes, void *stream);
+
+/* Attention from several new tokens per request over its tokens in the paged cache: prompts in parts, the next turn of a conversation,
+ * a prompt behind a shared prefix, drafted tokens, and decoding requests among them.  The n = cu[r+1] - cu[r] new tokens of request r are
+ * its last ones, and rows cu[r] .. cu[r+1]-1 of q: row cu[r] + i is token p = q_len[r] - n + i, and sees tokens 0 .. p, itself among them:
+ *   out[cu[r]+i][hq] = softmax_j(sm_scale * q[cu[r]+i][hq] . K[j]) . V over j <= p, KV head hq / (Hq/Hkv)
+ *   lse[cu[r]+i][hq] = log sum_j exp(sm_scale * q . K[j])                      (natural logarithm)
+ * All q_len[r] tokens have to be filed: after kv_assign_blk cu is its cu, q_len its q_len_next, and kv_quantize_blk runs first.  (The rows
+ * of a request that was refused there have no filed tokens: they are taken for its last ones, their outputs are of no use.)
+ * A row without tokens (n > q_len[r], or all of them absent) gives zeros and -infinity.  Table entries outside 0 .. n_blocks-1 count as absent:
+ * their tokens contribute nothing.  Lengths are clamped to 0 .. max_blocks * block; a request whose rows do not lie inside 0 .. T-1 is
+ * left alone, as are the rows of no request.  What lies behind a request's last token in its last block is not used, whatever it holds.
+ * Scales are finite, 0 or at least 2^-126.  The raw products q . codes and the sums of exp(score - largest score) times value are formed in
+ * binary32 and must not overflow there.  Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is
+ * below 2^-29 of the largest such product of the row by at most 2^-40 of that one.  Values of a block whose V scale is below 2^-60 of one in
+ * front of it in the request's head may count as 0.
+ *   T       rows of q, out and lse (a host-side bound of cu[R])
+ *   q       fp16 / bf16 [T][Hq][128], tokens q_stride elements apart            (device, read)
+ *   cu      int32 [R+1], non-decreasing                                         (device, read)
+ *   out     fp16 / bf16 [T][Hq][128], contiguous; lse fp32 [T][Hq] or NULL      (device, written)
+ *   workspace  device scratch of at least minikv_prompt_blk_workspace_bytes(shape, T) bytes, 16-byte aligned, no initial state.  Two
+ *              calls that share one must be ordered (same stream).
+ * T * Hq < 2^31, (T * Hq / 128 / Hkv + min(R, T)) * Hkv < 2^23 - 512, sm_scale finite and > 0.  T == 0 is no error and writes nothing. */
+size_t minikv_prompt_blk_workspace_bytes(const minikv_blk_shape *shape, int32_t T);
+int minikv_prompt_attn_blk(const minikv_blk_shape *shape, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache *cache,
+                           const int32_t *table, const int32_t *q_len, const int32_t *cu, float sm_scale, void *out, float *lse,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* Norms of queries and keys for each head, and the rotation by position, in one pass.  For token t with p = pos[t] >= 0, a row x of 128 of Q
+ * (weights w = w_q) or K (w = w_k):
+ *   y = x * w / sqrt(mean(x^2) + eps), y = x where the weights are NULL;
+ *   pair i < rot_dim / 2 of y, channels i and rot_dim/2 + i, or 2i and 2i+1 if `adjacent`: (u, v) becomes
+ *   (u cos a - v sin a, v cos a + u sin a), a = p * inv_freq[i]; channels from rot_dim on stay.
+ * In binary32 (the angle is right to 2^-20 of a radian whatever the position), rounded once.  A token with pos[t] < 0 (padding) is left alone.
+ *   Q, K    fp16 / bf16 [T][Hq or Hkv][128], tokens q_stride, k_stride elements apart              (device, read)
+ *   w_q, w_k   fp16 / bf16 [128], or NULL                                        (device, read)
+ *   inv_freq   fp32 [rot_dim / 2], finite, or NULL if rot_dim == 0               (device, read)
+ *   pos     int32 [T]                                                            (device, read)
+ *   Q_out, K_out  as Q and K, tokens q_out_stride, k_out_stride elements apart; they may be Q and K themselves with the same strides, and
+ *           must not overlap them otherwise                                      (device, written)
+ * dtype a minikv_dtype; rot_dim a multiple of 16, 0 .. 128; eps finite and >= 0; strides as above, multiples of 8, at most 2^23;
+ * T <= 2^25.  Squares are formed in binary32 and must not overflow there.  T == 0 is no error. */
+int minikv_norm_rope(int32_t Hq, int32_t Hkv, int32_t T, int32_t dtype, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                     const void *w_q, const void *w_k, float eps, const float *inv_freq, int32_t rot_dim, int32_t adjacent,
+                     const int32_t *pos, void *Q_out, int64_t q_out_stride, void *K_out, int64_t k_out_stride, void *stream);
+
+/* Requests that begin with what another one holds (shared prefixes, beams, several answers to one prompt).  Request r of the next step is made from
+ * request p = parent[r] of this one (r itself stays where parent[r] == r; a parent outside 0 .. R-1: r is empty) and keeps its first
+ * k = min(n_keep[r], q_len[p]) tokens: whole blocks are shared, table_next[r] names them.  A partly filled last block (k % block != 0) will get rows
+ * of its own and cannot be shared: it is inherited by ONE request that keeps all of p's tokens, by p itself if it stays whole, else by
+ * the lowest such request; every other request that needs one gets a fresh block, the next one of the ring in the order of the requests, and
+ * (src[r], dst[r]) says which block's contents kv_copy_blk has to copy into it, in every layer's cache, before it is used.
+ * Where the ring has no more blocks the request keeps its whole blocks only, q_len_next[r] = k - k % block.  An absent last block (an entry outside
+ * 0 .. n_blocks-1) stays one.
+ *   q_len, parent, n_keep  int32 [R]; table int32 [R][max_blocks]; ring, ring_state as above       (device, read)
+ *   q_len_next   int32 [R]: k, or less as said                                   (device, written)
+ *   table_next   int32 [R][max_blocks]: the ceil(q_len_next[r] / block) first entries of each row  (device, written)
+ *   ring_state_next  int32 [2]                                                   (device, written)
+ *   src, dst     int32 [R]: the pair of request r, or -1 and -1                  (device, written)
+ * What is written must not overlap what is read.  Blocks that only a parent's old row named are in no table then: kv_free_blk finds them.  Lengths
+ * outside 0 .. max_blocks * block are clamped, as are negative n_keep, the ring's head and count. */
+int kv_fork_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *parent, const int32_t *n_keep, const int32_t *table,
+                const int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *table_next, int32_t *ring_state_next,
+                int32_t *src, int32_t *dst, void *stream);
+
+/* Copies blocks: block dst[i] of every one of n_caches caches (a program's layers, all of this shape) becomes what block src[i] is, codes and
+ * scales of all KV heads.  A pair with an index outside 0 .. n_blocks-1 is skipped (kv_fork_blk and kv_compact_blk fill theirs with -1).  A
+ * block that is the destination of one pair must be neither end of another.
+ *   caches    minikv_blk_cache [n_caches]                                        (HOST, read before the call returns; buffers written)
+ *   src, dst  int32 [n_pairs]                                                    (device, read) */
+int kv_copy_blk(const minikv_blk_shape *shape, int32_t n_caches, const minikv_blk_cache *caches, int32_t n_pairs, const int32_t *src,
+                const int32_t *dst, void *stream);
+
+/* Takes back every block that no request holds: the ring becomes the blocks that no table row names among its first
+ * ceil(q_len[r] / block) entries, ascending from ring[0] on, ring_state = {0, their number}.  However many tables name a block, it stays as long as one
+ * does, so this ends requests that share blocks: set q_len[r] = 0, then call.  (A prefix that no request holds at the moment is kept
+ * by a row of its own.)  Lengths are clamped, entries outside the pool name nothing.
+ *   q_len int32 [R], table int32 [R][max_blocks]                                 (device, read)
+ *   ring int32 [n_blocks], ring_state int32 [2]; only the free blocks' entries   (device, written)
+ *   workspace  device scratch of at least kv_free_workspace_bytes(shape) bytes, 16-byte aligned, ZERO-FILLED ONCE after allocation (every
+ *              call leaves it ready for the next, of the same n_blocks; for another n_blocks zero it again).  Two calls that share one
+ *              must be ordered (same stream). */
+size_t kv_free_workspace_bytes(const minikv_blk_shape *shape);
+int kv_free_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *table, int32_t *ring, int32_t *ring_state,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/* kv_free_blk that also moves used blocks to the front of the pool, at most n_pairs of them: with U blocks used, those from U on move, the
+ * highest one first, each to the lowest free block that no other one moves to.
+ *   table_next   int32 [R][max_blocks]: the ceil(q_len[r] / block) first entries of each row, with the blocks' new places (entries
+ *                outside the pool as they are)                                   (device, written; not table)
+ *   ring, ring_state  the free blocks after the moves, as above                  (device, written)
+ *   src, dst     int32 [n_pairs]: what moved and where to, -1 behind the last move (device, written)
+ * kv_copy_blk has to move the contents, in every layer's cache, before table_next is used; ring's blocks may be handed out after that. */
+int kv_compact_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring,
+                   int32_t *ring_state, int32_t n_pairs, int32_t *src, int32_t *dst, void *workspace, size_t workspace_bytes, void *stream);
 
 /* selective_flash_attn (below) for a batch of prompts of different lengths, packed one behind the other: prompt b is rows
  * cu[b] .. cu[b+1]-1 of Q, K, V and X_O, and each attends to itself alone, causally.

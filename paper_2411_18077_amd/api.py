@@ -129,6 +129,23 @@ def lib():
         l.selective_flash_attn_packed.restype = C.c_int
         l.selective_flash_attn_packed.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, P, C.c_int64,
                                                   P, C.c_int64, P, C.c_int64, P, C.c_float, P, P, P, P]
+        l.minikv_prompt_blk_workspace_bytes.restype = C.c_size_t
+        l.minikv_prompt_blk_workspace_bytes.argtypes = [S, C.c_int32]
+        l.minikv_prompt_attn_blk.restype = C.c_int
+        l.minikv_prompt_attn_blk.argtypes = [S, C.c_int32, P, C.c_int64, C.POINTER(MinikvBlkCache), P, P, P, C.c_float, P, P, P, C.c_size_t, P]
+        l.minikv_norm_rope.restype = C.c_int
+        l.minikv_norm_rope.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, P, C.c_int64, P, P, C.c_float, P, C.c_int32,
+                                       C.c_int32, P, P, C.c_int64, P, C.c_int64, P]
+        l.kv_fork_blk.restype = C.c_int
+        l.kv_fork_blk.argtypes = [S] + [P] * 12
+        l.kv_copy_blk.restype = C.c_int
+        l.kv_copy_blk.argtypes = [S, C.c_int32, C.POINTER(MinikvBlkCache), C.c_int32, P, P, P]
+        l.kv_free_workspace_bytes.restype = C.c_size_t
+        l.kv_free_workspace_bytes.argtypes = [S]
+        l.kv_free_blk.restype = C.c_int
+        l.kv_free_blk.argtypes = [S, P, P, P, P, P, C.c_size_t, P]
+        l.kv_compact_blk.restype = C.c_int
+        l.kv_compact_blk.argtypes = [S, P, P, P, P, P, C.c_int32, P, P, P, C.c_size_t, P]
         l.minikv_diag_redo_count.restype = C.c_int
         l.minikv_diag_redo_count.argtypes = [C.POINTER(MinikvShape), P, C.POINTER(C.c_int32)]
         l.minikv_stream_read_probe.restype = C.c_int
@@ -494,3 +511,112 @@ def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X
                                              _need(X_O, Q.dtype, T * Hq * 128, "X_O", home), _need(lse, torch.float32, T * Hq, "lse", home),
                                              None if A_cumul is None else _need(A_cumul, torch.float32, T * Hq, "A_cumul", home), st),
            "selective_flash_attn_packed")
+
+
+def minikv_prompt_blk_workspace_bytes(shape, T):
+    return int(lib().minikv_prompt_blk_workspace_bytes(C.byref(shape), int(T)))
+
+
+def _space(ws, home):
+    if not ws.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor is needed")
+    return _here(ws, home, "workspace"), ws.numel() * ws.element_size()
+
+
+def minikv_prompt_attn_blk(shape, T, q, cache, table, q_len, cu, sm_scale, out, lse, workspace, stream=None):
+    """q: [T][Hq][128], possibly a slice of a fused projection; out: contiguous; lse: [T][Hq] or None.  cu and q_len are kv_assign_blk's cu
+    and q_len_next, behind kv_quantize_blk."""
+    home, st = _home(stream)
+    (qs, p), (ws, n) = _rows(q, shape.dtype, shape.Hq, "q", home), _space(workspace, home)
+    if q.shape[0] < T:
+        raise ValueError("q has %d rows, fewer than %d" % (q.shape[0], T))
+    _check(lib().minikv_prompt_attn_blk(C.byref(shape), int(T), p, qs, _fits(shape, cache, home),
+                                        _need(table, torch.int32, shape.R * shape.max_blocks, "table", home),
+                                        _need(q_len, torch.int32, shape.R, "q_len", home), _need(cu, torch.int32, shape.R + 1, "cu", home),
+                                        float(sm_scale), _need(out, q.dtype, T * shape.Hq * 128, "out", home),
+                                        None if lse is None else _need(lse, torch.float32, T * shape.Hq, "lse", home), ws, n, st),
+           "minikv_prompt_attn_blk")
+
+
+def minikv_norm_rope(Hq, Hkv, T, Q, K, w_q, w_k, eps, inv_freq, rot_dim, adjacent, pos, Q_out, K_out, stream=None):
+    """Q, Q_out: [T][Hq][128], K, K_out: [T][Hkv][128], possibly slices of a fused projection; Q_out and K_out may be Q and K.  w_q, w_k:
+    [128] of the rows' type, or None; inv_freq: float32 [rot_dim / 2]."""
+    dtype, (home, st) = DTYPES.get(Q.dtype, -1), _home(stream)
+    (qs, q), (ks, k) = _rows(Q, dtype, Hq, "Q", home), _rows(K, dtype, Hkv, "K", home)
+    (qos, qo), (kos, ko) = _rows(Q_out, dtype, Hq, "Q_out", home), _rows(K_out, dtype, Hkv, "K_out", home)
+    if min(Q.shape[0], K.shape[0], Q_out.shape[0], K_out.shape[0]) < T:
+        raise ValueError("fewer than %d rows" % T)
+    if T == 1:                                         # (one row has no stride of its own)
+        qos, kos = qs if qo == q else qos, ks if ko == k else kos
+    _check(lib().minikv_norm_rope(int(Hq), int(Hkv), int(T), dtype, q, qs, k, ks,
+                                  None if w_q is None else _need(w_q, Q.dtype, 128, "w_q", home),
+                                  None if w_k is None else _need(w_k, Q.dtype, 128, "w_k", home), float(eps),
+                                  _need(inv_freq, torch.float32, rot_dim // 2, "inv_freq", home) if rot_dim else None, int(rot_dim),
+                                  int(bool(adjacent)), _need(pos, torch.int32, T, "pos", home), qo, qos, ko, kos, st), "minikv_norm_rope")
+
+
+class BlkCaches:
+    """The caches of a program's layers, all of one shape, for kv_copy_blk: BlkCache objects, or dicts of their buffers K, V, Ks, Vs."""
+
+    def __init__(self, shape, layers):
+        self.shape = shape
+        self._t = []
+        for x in layers:
+            t = x._t if isinstance(x, BlkCache) else (x["K"], x["V"], x["Ks"], x["Vs"])
+            home = t[0].get_device() if not self._t else self._t[0][0].get_device()
+            codes, scales = int(lib().minikv_blk_cache_bytes(C.byref(shape), 0)), int(lib().minikv_blk_cache_bytes(C.byref(shape), 1)) // 4
+            if not codes:
+                raise ValueError("invalid shape")
+            for y, dtype, n, name in zip(t, (torch.float8_e4m3fn,) * 2 + (torch.float32,) * 2, (codes, codes, scales, scales), ("K", "V", "Ks", "Vs")):
+                _need(y, dtype, n, name, home)
+            self._t.append(t)
+        self._c = (MinikvBlkCache * max(len(self._t), 1))(*(MinikvBlkCache(*(y.data_ptr() for y in t)) for t in self._t))
+
+    def __len__(self):
+        return len(self._t)
+
+
+def kv_fork_blk(shape, q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst, stream=None):
+    i32, R, (home, st) = torch.int32, shape.R, _home(stream)
+    rows = R * shape.max_blocks
+    p = [_need(t, i32, n, name, home) for t, n, name in (
+        (q_len, R, "q_len"), (parent, R, "parent"), (n_keep, R, "n_keep"), (table, rows, "table"), (ring, shape.n_blocks, "ring"),
+        (ring_state, 2, "ring_state"), (q_len_next, R, "q_len_next"), (table_next, rows, "table_next"), (ring_state_next, 2, "ring_state_next"),
+        (src, R, "src"), (dst, R, "dst"))]
+    _check(lib().kv_fork_blk(C.byref(shape), *p, st), "kv_fork_blk")
+
+
+def kv_copy_blk(shape, caches, src, dst, stream=None):
+    """caches: BlkCaches; src, dst: a pair per element."""
+    home, st = _home(stream)
+    own, n = caches.shape, src.numel()
+    if dst.numel() != n:
+        raise ValueError("%d sources, %d destinations" % (n, dst.numel()))
+    if own is not shape and (own.n_blocks < shape.n_blocks or own.Hkv != shape.Hkv or own.block != shape.block):
+        raise ValueError("the caches are ones of %d blocks of %d tokens and %d heads" % (own.n_blocks, own.block, own.Hkv))
+    if len(caches):
+        _here(caches._t[0][0], home, "the caches")
+    _check(lib().kv_copy_blk(C.byref(shape), len(caches), caches._c, n, _need(src, torch.int32, n, "src", home),
+                             _need(dst, torch.int32, n, "dst", home), st), "kv_copy_blk")
+
+
+def kv_free_workspace_bytes(shape):
+    return int(lib().kv_free_workspace_bytes(C.byref(shape)))
+
+
+def kv_free_blk(shape, q_len, table, ring, ring_state, workspace, stream=None):
+    i32, (home, st) = torch.int32, _home(stream)
+    ws, n = _space(workspace, home)
+    _check(lib().kv_free_blk(C.byref(shape), _need(q_len, i32, shape.R, "q_len", home), _need(table, i32, shape.R * shape.max_blocks, "table", home),
+                             _need(ring, i32, shape.n_blocks, "ring", home), _need(ring_state, i32, 2, "ring_state", home), ws, n, st),
+           "kv_free_blk")
+
+
+def kv_compact_blk(shape, q_len, table, table_next, ring, ring_state, src, dst, workspace, stream=None):
+    """At most src.numel() blocks move."""
+    i32, (home, st) = torch.int32, _home(stream)
+    (ws, n), pairs, rows = _space(workspace, home), src.numel(), shape.R * shape.max_blocks
+    _check(lib().kv_compact_blk(C.byref(shape), _need(q_len, i32, shape.R, "q_len", home), _need(table, i32, rows, "table", home),
+                                _need(table_next, i32, rows, "table_next", home), _need(ring, i32, shape.n_blocks, "ring", home),
+                                _need(ring_state, i32, 2, "ring_state", home), pairs, _need(src, i32, pairs, "src", home),
+                                _need(dst, i32, pairs, "dst", home), ws, n, st), "kv_compact_blk")

@@ -16,7 +16,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libminikv.so")
 
 SOURCES = ["api.hip", "quantize.hip", "decode_scalar.hip", "decode_tiled.hip", "decode_static.hip", "select.hip",
-           "prefill_attn.hip", "pt.hip", "blocks.hip", "decode_blk.hip"]
+           "prefill_attn.hip", "pt.hip", "blocks.hip", "decode_blk.hip", "prompt_blk.hip", "norm_rope.hip", "pages.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -30,7 +30,7 @@ FLAGS = [
 # the packed fp16 min / max need no NaN canonicalisation (-fno-honor-nans drops one instruction of three there)
 EXTRA = {"quantize.hip": ["-ffp-contract=off", "-fno-honor-nans"], "pt.hip": ["-ffp-contract=off"],
          # finite inputs by contract: the running maximum needs no NaN canonicalisation (an instruction per score)
-         "prefill_attn.hip": ["-fno-honor-nans"]}
+         "prefill_attn.hip": ["-fno-honor-nans"], "prompt_blk.hip": ["-fno-honor-nans"]}
 
 
 def hipcc():

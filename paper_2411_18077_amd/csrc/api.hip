@@ -274,6 +274,104 @@ int minikv_decode_attn_blk(const minikv_blk_shape *s, const void *q, int64_t q_s
     return launch_decode_blk(*s, q, q_stride, *c, table, q_len, sm_scale, out, workspace, (hipStream_t)stream);
 }
 
+size_t minikv_prompt_blk_workspace_bytes(const minikv_blk_shape *s, int32_t T)
+{
+    return validate_blk(s) == MINIKV_OK && T >= 0 && (int64_t)T * s->Hq <= 0x7fffffff ? prompt_blk_workspace_bytes(*s, T) : 0;
+}
+
+int minikv_prompt_attn_blk(const minikv_blk_shape *s, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache *c,
+                           const int32_t *table, const int32_t *q_len, const int32_t *cu, float sm_scale, void *out, float *lse,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (T < 0 || (int64_t)T * s->Hq > 0x7fffffff) return MINIKV_EINVAL;
+    if (!valid_blk_cache(c) || !valid_stride(q_stride, s->Hq) || !aligned4(table) || !aligned4(q_len) || !aligned4(cu)) return MINIKV_EINVAL;
+    if (!(sm_scale > 0.0f) || sm_scale - sm_scale != 0.0f) return MINIKV_EINVAL;       // positive and finite
+    if (T == 0) return MINIKV_OK;                                                      // (a null pointer is one of an empty tensor)
+    if (!aligned16(q) || !aligned16(out) || (lse && !aligned4(lse)) || !aligned16(workspace)) return MINIKV_EINVAL;
+    if (workspace_bytes < prompt_blk_workspace_bytes(*s, T)) return MINIKV_EWORKSPACE;
+    return launch_prompt_blk(*s, T, q, q_stride, *c, table, q_len, cu, sm_scale, out, lse, workspace, (hipStream_t)stream);
+}
+
+int minikv_norm_rope(int32_t Hq, int32_t Hkv, int32_t T, int32_t dtype, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                     const void *w_q, const void *w_k, float eps, const float *inv_freq, int32_t rot_dim, int32_t adjacent,
+                     const int32_t *pos, void *Q_out, int64_t q_out_stride, void *K_out, int64_t k_out_stride, void *stream)
+{
+    if (Hq <= 0 || Hkv <= 0 || T < 0 || T > (1 << 25)) return MINIKV_EINVAL;
+    if (dtype != MINIKV_F16 && dtype != MINIKV_BF16) return MINIKV_EUNSUPPORTED;
+    if (rot_dim < 0 || rot_dim > kD || rot_dim % 16 || !(eps >= 0.0f) || eps - eps != 0.0f) return MINIKV_EINVAL;
+    if (!valid_stride(q_stride, Hq) || !valid_stride(k_stride, Hkv) || !valid_stride(q_out_stride, Hq) || !valid_stride(k_out_stride, Hkv))
+        return MINIKV_EINVAL;
+    if ((w_q && !aligned16(w_q)) || (w_k && !aligned16(w_k)) || (rot_dim && !aligned4(inv_freq))) return MINIKV_EINVAL;
+    if (T == 0) return MINIKV_OK;                                                      // (a null pointer is one of an empty tensor)
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out) || !aligned4(pos)) return MINIKV_EINVAL;
+    if ((Q_out == Q && q_out_stride != q_stride) || (K_out == K && k_out_stride != k_stride)) return MINIKV_EINVAL;
+    return launch_norm_rope(Hq, Hkv, T, dtype, Q, q_stride, K, k_stride, w_q, w_k, eps, inv_freq, rot_dim, adjacent, pos, Q_out, q_out_stride,
+                            K_out, k_out_stride, (hipStream_t)stream);
+}
+
+int kv_fork_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *parent, const int32_t *n_keep, const int32_t *table,
+                const int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *table_next, int32_t *ring_state_next,
+                int32_t *src, int32_t *dst, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    const int32_t *in[] = {q_len, parent, n_keep, table, ring, ring_state};
+    const int32_t *out[] = {q_len_next, table_next, ring_state_next, src, dst};
+    for (const int32_t *p : in)
+        if (!aligned4(p)) return MINIKV_EINVAL;
+    for (int i = 0; i < 5; ++i) {
+        if (!aligned4(out[i])) return MINIKV_EINVAL;
+        for (const int32_t *p : in)
+            if (p == out[i]) return MINIKV_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (out[j] == out[i]) return MINIKV_EINVAL;
+    }
+    return launch_fork_blk(*s, q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst,
+                           (hipStream_t)stream);
+}
+
+int kv_copy_blk(const minikv_blk_shape *s, int32_t n_caches, const minikv_blk_cache *caches, int32_t n_pairs, const int32_t *src,
+                const int32_t *dst, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (n_caches < 0 || n_pairs < 0 || (n_caches && !caches)) return MINIKV_EINVAL;
+    for (int32_t i = 0; i < n_caches; ++i)
+        if (!valid_blk_cache(caches + i)) return MINIKV_EINVAL;
+    if (n_caches == 0 || n_pairs == 0) return MINIKV_OK;
+    if (!aligned4(src) || !aligned4(dst) || src == dst) return MINIKV_EINVAL;
+    return launch_copy_blk(*s, n_caches, caches, n_pairs, src, dst, (hipStream_t)stream);
+}
+
+size_t kv_free_workspace_bytes(const minikv_blk_shape *s)
+{
+    return validate_blk(s) == MINIKV_OK ? pool_workspace_bytes(*s) : 0;
+}
+
+int kv_free_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *table, int32_t *ring, int32_t *ring_state,
+                void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (!aligned4(q_len) || !aligned4(table) || !aligned4(ring) || !aligned4(ring_state) || !aligned16(workspace)) return MINIKV_EINVAL;
+    if (workspace_bytes < pool_workspace_bytes(*s)) return MINIKV_EWORKSPACE;
+    return launch_pool_blk(*s, q_len, table, nullptr, ring, ring_state, 0, nullptr, nullptr, workspace, (hipStream_t)stream);
+}
+
+int kv_compact_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring,
+                   int32_t *ring_state, int32_t n_pairs, int32_t *src, int32_t *dst, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_blk(s);
+    if (rc) return rc;
+    if (!aligned4(q_len) || !aligned4(table) || !aligned4(table_next) || !aligned4(ring) || !aligned4(ring_state) || !aligned16(workspace))
+        return MINIKV_EINVAL;
+    if (n_pairs < 0 || (n_pairs && (!aligned4(src) || !aligned4(dst) || src == dst)) || table_next == table) return MINIKV_EINVAL;
+    if (workspace_bytes < pool_workspace_bytes(*s)) return MINIKV_EWORKSPACE;
+    return launch_pool_blk(*s, q_len, table, table_next, ring, ring_state, n_pairs, src, dst, workspace, (hipStream_t)stream);
+}
+
 size_t selective_flash_attn_workspace_bytes(int32_t B, int32_t Hkv, int64_t L)
 {
     if (B <= 0 || Hkv <= 0 || L < 1) return 0;

@@ -110,6 +110,20 @@ int launch_quantize_blk(const minikv_blk_shape &s, int32_t n_tok, const void *K,
                         int64_t v_stride, const int32_t *slots, const minikv_blk_cache &c, hipStream_t st);
 int launch_decode_blk(const minikv_blk_shape &s, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
                       const int32_t *q_len, float sm_scale, void *out, void *workspace, hipStream_t st);
+size_t prompt_blk_workspace_bytes(const minikv_blk_shape &s, int32_t T);
+int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
+                      const int32_t *q_len, const int32_t *cu, float sm_scale, void *out, float *lse, void *workspace, hipStream_t st);
+int launch_norm_rope(int32_t Hq, int32_t Hkv, int32_t T, int32_t dtype, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
+                     const void *w_q, const void *w_k, float eps, const float *inv_freq, int32_t rot, int32_t adjacent, const int32_t *pos,
+                     void *Q_out, int64_t q_out_stride, void *K_out, int64_t k_out_stride, hipStream_t st);
+int launch_fork_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *parent, const int32_t *n_keep, const int32_t *table,
+                    const int32_t *ring, const int32_t *state, int32_t *q_len_next, int32_t *table_next, int32_t *state_next, int32_t *src,
+                    int32_t *dst, hipStream_t st);
+int launch_copy_blk(const minikv_blk_shape &s, int32_t n_caches, const minikv_blk_cache *caches, int32_t n_pairs, const int32_t *src,
+                    const int32_t *dst, hipStream_t st);
+size_t pool_workspace_bytes(const minikv_blk_shape &s);
+int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring, int32_t *state,
+                    int32_t n_pairs, int32_t *src, int32_t *dst, void *workspace, hipStream_t st);       // table_next NULL: nothing moves
 
 int launch_prefill(int32_t B, int32_t Hq, int32_t Hkv, int64_t L, const minikv_f16 *Q, const minikv_f16 *K,
                    const minikv_f16 *V, float sm_scale, minikv_f16 *XO, float *lse, float *A_cumul, hipStream_t st);

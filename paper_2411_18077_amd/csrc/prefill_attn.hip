@@ -15,21 +15,13 @@
 //                          recomputes S = Q K^T, normalises with the saved LSE and adds the weights of its key column
 //                          in the lane: no atomics, one exchange at the end.
 // A prompt of at most 128 tokens is one row block: its workgroup of the first kernel forms the column sums as well.
-#include "common.h"
+#include "attn_tile.h"
 
 #include <type_traits>
 
 namespace minikv {
 
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef float float16v __attribute__((ext_vector_type(16)));
-
-constexpr int kPfD = 128;            // head dimension
-constexpr int kPfN = 64;             // keys (forward) / queries (column sums) per LDS tile
 constexpr int kWaitVm0 = 0x0F70;      // s_waitcnt vmcnt(0), other counters untouched
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 struct PrefillArgs {
     const _Float16 *Q, *K, *V;
@@ -44,25 +36,6 @@ struct PrefillArgs {
     int side;                        // log2 of the query heads (of one KV head) that a workgroup of the first pass takes side by side
     unsigned q_pitch, k_pitch, v_pitch;
 };
-
-// 16-bit operands are kept as halves whatever they are; BF16 instances differ in the product and in the two roundings (a product's operands
-// are of one type, and bf16 values leave fp16's range, so the weights have bf16's 8 bits there).
-typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
-
-template <bool BF16 = false>
-__device__ __forceinline__ float16v mfma32(half8 a, half8 b, float16v c)
-{
-    if constexpr (BF16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bfloat8, a), __builtin_bit_cast(bfloat8, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-template <bool BF16>
-__device__ __forceinline__ _Float16 to16(float v)
-{
-    if constexpr (BF16) return __builtin_bit_cast(_Float16, (__bf16)v);
-    else return (_Float16)v;
-}
 
 // Packed prompts: which row block of which prompt a workgroup takes.  The blocks of all prompts are dealt in the order of
 // what they cost (HEAVY_LAST: row blocks, whose last ones see the most keys; else column blocks, whose first ones are
@@ -137,9 +110,6 @@ __device__ __forceinline__ PackedBlock packed_block(const PrefillArgs &a, const 
     return p;
 }
 
-// Row of accumulator element i (0..15) inside a 32x32 result tile, for a lane of half-wave g.
-__device__ __forceinline__ int acc_row(int i, int g) { return (i >> 2) * 8 + g * 4 + (i & 3); }
-
 // 64 lanes x 16 bytes from base + off (per lane) straight to LDS at lds + 16 * lane: no registers and no LDS store
 // instructions in between.  The compiler does not count this load: wait with s_waitcnt vmcnt before the barrier that
 // hands the data over.  (m0, which it sets, is a register the compiler reserves and holds no value in from one statement to
@@ -155,10 +125,6 @@ __device__ __forceinline__ unsigned lds_offset(const void *p)
 {
     return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
 }
-// Tiles loaded this way have unpadded rows of 256 bytes; chunk k (16 bytes) of row r sits at place k ^ (r & 15), so
-// that the fragment reads of 32 consecutive rows use all banks evenly.
-__device__ __forceinline__ int tile_place(int row, int chunk) { return row * kPfD + ((chunk ^ (row & 15)) << 3); }
-
 // Local memory that one wave writes and reads: its operations are done in order, the compiler is told to keep them so.
 __device__ __forceinline__ void wave_order()
 {
@@ -183,18 +149,6 @@ __device__ __forceinline__ void wave_order()
 // 16384^3 reaches 1.29 on this card), 2 x 32 x 4096 364 -> 320 us, 32 x 777 26.7 -> 19.9 us.  Letting the reference of the
 // weights lag behind the running maximum (fewer rescales) is another 2-3 %, but then the key that dominates a row no
 // longer has the weight 1 that fp16 holds exactly, and the error grows by 1 %.
-constexpr int kPfTile = kPfN * kPfD;                    // halves of one unpadded tile in LDS
-
-// Place (in halves) of 16-byte chunk k of row `key` in a V tile: the rows 4j .. 4j+3 that one transposing read takes
-// fall on different banks.
-__device__ __forceinline__ int v_swizzle(int key) { return 4 * (key & 3) + 2 * ((key >> 1) & 1); }
-
-typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
-__device__ __forceinline__ half4 read_transposed(const _Float16 *p)
-{
-    return (half4)__builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4 *)p);
-}
-
 // SPLIT == 2: two sets of WAVES waves take the even and the odd tiles of the same queries, each through LDS buffers of
 // its own, and meet at the end; for launches that leave a compute unit a single set.  The launch gives the LDS: where the
 // compiler knows that 128 KB leave room for one workgroup, it spreads two sets of two waves over the registers of two
