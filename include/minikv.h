@@ -355,9 +355,10 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  *   q       fp16 / bf16 [T][Hq][128], tokens q_stride elements apart            (device, read)
  *   cu      int32 [R+1], non-decreasing                                         (device, read)
  *   out     fp16 / bf16 [T][Hq][128], contiguous; lse fp32 [T][Hq] or NULL      (device, written)
- *   workspace  device scratch of at least minikv_prompt_blk_workspace_bytes(shape, T) bytes, 16-byte aligned, no initial state.  Two
- *              calls that share one must be ordered (same stream).
- * T * Hq < 2^31, (T * Hq / 128 / Hkv + min(R, T)) * Hkv < 2^23 - 512, sm_scale finite and > 0.  T == 0 is no error and writes nothing. */
+ *   workspace  device scratch of at least minikv_prompt_blk_workspace_bytes(shape, T) bytes, 16-byte aligned, ZERO-FILLED ONCE after
+ *              allocation (every call returns its ticket counters to zero).  Calls of any shapes may take turns on one workspace of
+ *              sufficient size; two calls that share a workspace must be ordered (same stream).
+ * T * Hq < 2^31, (T * Hq / 128 / Hkv + 2 min(R, T)) * Hkv < 2^23 - 512, sm_scale finite and > 0.  T == 0 is no error and writes nothing. */
 size_t minikv_prompt_blk_workspace_bytes(const minikv_blk_shape *shape, int32_t T);
 int minikv_prompt_attn_blk(const minikv_blk_shape *shape, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache *cache,
                            const int32_t *table, const int32_t *q_len, const int32_t *cu, float sm_scale, void *out, float *lse,

@@ -1,26 +1,37 @@
 // Attention of several new tokens of each request over its tokens in the paged 8-bit cache (minikv_prompt_attn_blk).
 //
-// The rows of one KV head of a request are its new tokens times the query heads of that head: row i * rep + h.  A workgroup of four waves
-// takes 128 of them, 32 a wave, and walks the request's tokens in tiles of 64, all it sees or a part of them.  A tile's codes go from
-// memory through registers to local memory as 16-bit operands, every code once per workgroup (keys in the queries' type, values in fp16: e4m3 is
-// exact in both).  Scores are computed transposed, S^T = K Q^T on the 32x32x16 instruction, so that a lane holds one row: maximum and
-// sum of the softmax are the lane's own, and its weights are the B operand of O^T = V^T P^T as they are.
+// The rows of one KV head of a request are its new tokens times the query heads of that head: row i * rep + h.  Scores are computed
+// transposed, S^T = K Q^T on the 32x32x16 instruction, so that a lane holds one row: maximum and sum of the softmax are the lane's own, and its
+// weights are the B operand of O^T = V^T P^T as they are.  A workgroup of four waves takes
+//   wide    128 rows, 32 a wave, and walks the tokens in tiles of 64: a tile's codes go from memory through registers to local memory as 16-bit
+//           operands, every code once per workgroup (keys in the queries' type, values in fp16: e4m3 is exact in both);
+//   narrow  the last up to 64 rows of a request, 32 of them: all waves hold the same rows and take every fourth 32 tokens each, keys from memory to
+//           registers, values through a wave's own local memory, and no barrier; their results meet at the end.
 //
 // The scales of a block are factors of whole keys and values: that of K is part of the factor that takes a score to a power of two, that
 // of V becomes part of the weight, as its logarithm in the exponent: w = 2^(s c Ks + log2 Vs - m'), m' the largest such exponent of the row so far.  So
 // the second product takes codes as they are, and no weight loses bits to a large scale without weight.  w, times 2^15, is rounded to fp16:
 // 11 bits down to 2^-29 of the row's largest.  The sum of the weights without Vs is kept over a reference of its own, the largest score.
+//
+// Long walks are made in parts, by as many workgroups as the card holds (see find_item); the parts of a block's rows are joined by the last
+// workgroup of each eight to arrive, the results of eight of those by the last of them, and so on, always summed in the parts' order.
 #include "decode_common.h"
 #include "attn_tile.h"
 
 namespace minikv {
 
-constexpr int kPbRows = 128;                           // rows of a workgroup
+constexpr int kPbNarrow = 32;                          // rows of a narrow block
+constexpr int kPbRows = 128;                           // rows of a wide one
+constexpr int kPbTail = 64;                            // most rows behind the last wide block that narrow ones take
 constexpr int kPbThreads = 256;
 constexpr float kPbNone = -3.0e38f;                    // references before the first token: finite, so that no difference is NaN
 constexpr float kPbHead = 15.0f;                       // log2 of the largest weight
 constexpr float kPbRange = 60.0f;                      // V scales further below the largest one, as powers of two, count as 0
-constexpr int kPbLeast = 2;                            // tiles that a part of a walk has at least
+constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens for a wide block, 1 for a narrow one
+constexpr int kPbLeast = 4;                            // least cost of a part of a walk
+constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
+constexpr int kPbJoin = 8;                             // parts joined at once
+constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
 
 struct PromptBlkArgs {
     const uint16_t *q;
@@ -30,58 +41,77 @@ struct PromptBlkArgs {
     const int32_t *table, *q_len, *cu;
     uint16_t *out;
     float *lse;
-    int *header;                                       // parts of walks in this call
-    int4 *parts;                                       // of each: first row of q, rows of the request, first row | KV head, parts (0: not a first one)
+    int *tickets;                                      // [3][2 * kPbSlots], of the first part of each eight, 64, 512
     float *ml, *o;                                     // [part][row] (m, l) and [part][row][128]
     int part_rows;
     float c;                                           // sm_scale * log2(e)
-    int R, T, Hq, Hkv, rep, n_blocks, width, shift, slots;
+    int R, T, Hq, Hkv, rep, n_blocks, width, shift;
     uint32_t hkv_magic, hkv_shift, rep_magic, rep_shift;
 };
 
 // What a workgroup works on.
 struct PromptItem {
     int r, at, n, L;                                   // request, its first row of q, new tokens, tokens held
-    int block, part, parts, slot;                      // row block; which part of the walk, of how many; its place in the workspace (part 0's for parts > 1)
+    int row0, narrow;                                  // first row of the block, and its kind
+    int part, parts, slot;                             // which part of the walk, of how many; part 0's place in the workspace, for parts > 1
     int chunk;                                         // tiles of a part
 };
 
-// The requests' rows in blocks of 128, each block's walk in parts of about as many tiles as there are for a slot (of workgroups at
-// once).  A block has ceil(tiles / chunk) parts, tiles the request's, chunk = ceil(all tiles of all blocks / slots): at most slots more
-// than there are blocks, and at most twice slots where there are two or more.  Every workgroup counts all that for itself.
+__device__ inline uint64_t pb_load(const float *p)     // device scope: other dies wrote it in this launch
+{
+    return __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline void pb_store(float *p, float a, float b)
+{
+    __hip_atomic_store((uint64_t *)p, (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float2 pb_pair(uint64_t v) { return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))}; }
+
+// The requests' rows in blocks, each block's walk in parts of about the cost that there is for a slot (of workgroups at once).  A
+// block has ceil(cost / chunk) parts, chunk = ceil(all blocks' cost / slots): at most slots more than there are blocks, and at most twice slots where
+// there are two or more.  The longest walks come first: a request's narrow blocks, then its wide ones from the last on.  Every workgroup
+// counts all that for itself.
 __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t *lds, PromptItem &it)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (a.R + kPbThreads - 1) / kPbThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-    auto request = [&](int r, int &at, int &n, int &L) {
-        at = a.cu[r];
-        const int end = a.cu[r + 1];
-        n = at >= 0 && end > at && end <= a.T ? end - at : 0;
-        L = (int)min((int64_t)max(a.q_len[r], 0), (int64_t)a.width << a.shift);
+    struct Request {
+        int at, n, L;
+        uint32_t wide, narrow, tiles;
     };
-    auto blocks = [&](int n) { return (uint32_t)((n * a.rep + kPbRows - 1) / kPbRows); };
-    auto tiles = [&](int L) { return (uint32_t)max((L + 63) >> 6, 1); };
+    auto request = [&](int r) {
+        Request q;
+        q.at = a.cu[r];
+        const int end = a.cu[r + 1];
+        q.n = q.at >= 0 && end > q.at && end <= a.T ? end - q.at : 0;
+        q.L = (int)min((int64_t)max(a.q_len[r], 0), (int64_t)a.width << a.shift);
+        const uint32_t M = (uint32_t)q.n * a.rep, rest = M % kPbRows;
+        q.wide = M / kPbRows + (rest > kPbTail), q.narrow = rest > kPbTail ? 0 : (rest + kPbNarrow - 1) / kPbNarrow;
+        q.tiles = (uint32_t)max((q.L + 63) >> 6, 1);
+        return q;
+    };
     uint32_t *sums = (uint32_t *)(lds + 1);            // [2][4] of the waves
     PromptItem *found = (PromptItem *)(lds + 8);
     if (tid == 0) lds[0] = 0, found->r = -1;
     __syncthreads();
     uint64_t all = 0;
-    int at, n, L;
     for (int r = r0; r < r1; ++r) {
-        request(r, at, n, L);
-        all += (uint64_t)blocks(n) * tiles(L);
+        const Request q = request(r);
+        all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles;
     }
     if (all) atomicAdd((unsigned long long *)lds, (unsigned long long)all);
     __syncthreads();
     all = lds[0] * a.Hkv;
-    const uint32_t chunk = max((uint32_t)((all + a.slots - 1) / a.slots), (uint32_t)kPbLeast);
-    uint32_t items = 0, split = 0;
+    const uint32_t chunk = max((uint32_t)((all + kPbSlots - 1) / kPbSlots), (uint32_t)kPbLeast);
+    auto wide_parts = [&](const Request &q) { return min((q.tiles * kPbWideCost + chunk - 1) / chunk, (uint32_t)kPbMost); };
+    auto narrow_parts = [&](const Request &q) { return min((q.tiles + chunk - 1) / chunk, (uint32_t)kPbMost); };
+    uint32_t v[2] = {0, 0};                            // items, and those of walks in two or more parts
     for (int r = r0; r < r1; ++r) {
-        request(r, at, n, L);
-        const uint32_t b = blocks(n), p = (tiles(L) + chunk - 1) / chunk;
-        items += b * p, split += p > 1 ? b * p : 0;
+        const Request q = request(r);
+        const uint32_t w = wide_parts(q), n = narrow_parts(q);
+        v[0] += q.wide * w + q.narrow * n, v[1] += (w > 1 ? q.wide * w : 0) + (n > 1 ? q.narrow * n : 0);
     }
-    uint32_t v[2] = {items, split};
+    const uint32_t items = v[0], split = v[1];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -94,26 +124,28 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
     __syncthreads();
     uint32_t first = v[0] - items, slot = v[1] - split;
     for (int w = 0; w < wave; ++w) first += sums[w], slot += sums[4 + w];
-    if (blockIdx.x == 0 && tid == 0) a.header[0] = (int)((sums[4] + sums[5] + sums[6] + sums[7]) * a.Hkv);
     if (idx >= first && idx - first < items)
         for (int r = r0; r < r1; ++r) {
-            request(r, at, n, L);
-            const uint32_t b = blocks(n), p = (tiles(L) + chunk - 1) / chunk;
-            if (idx - first < b * p) {
-                const uint32_t k = (idx - first) / p;
-                found->at = at, found->n = n, found->L = L, found->r = r;
-                found->block = (int)(b - 1 - k), found->part = (int)(idx - first - k * p), found->parts = (int)p;      // the longest walks first
-                found->slot = (int)(slot + k * p), found->chunk = (int)chunk;
+            const Request q = request(r);
+            const uint32_t w = wide_parts(q), n = narrow_parts(q), at = idx - first, narrow = q.narrow * n, wide = q.wide * w;
+            if (at < narrow + wide) {
+                const bool is_narrow = at < narrow;
+                const uint32_t p = is_narrow ? n : w, i = is_narrow ? at : at - narrow, k = i / p;
+                found->at = q.at, found->n = q.n, found->L = q.L, found->r = r;
+                found->narrow = is_narrow;
+                found->row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
+                found->part = (int)(i - k * p), found->parts = (int)p, found->chunk = (int)((q.tiles + p - 1) / p);
+                found->slot = (int)(slot + (is_narrow ? 0 : n > 1 ? narrow : 0) + k * p);
                 break;
             }
-            first += b * p, slot += p > 1 ? b * p : 0;
+            first += narrow + wide, slot += (n > 1 ? narrow : 0) + (w > 1 ? wide : 0);
         }
     __syncthreads();
     it = *found;
     __syncthreads();
-    it.r = __builtin_amdgcn_readfirstlane(it.r), it.at = __builtin_amdgcn_readfirstlane(it.at), it.n = __builtin_amdgcn_readfirstlane(it.n);
-    it.L = __builtin_amdgcn_readfirstlane(it.L), it.block = __builtin_amdgcn_readfirstlane(it.block), it.part = __builtin_amdgcn_readfirstlane(it.part);
-    it.parts = __builtin_amdgcn_readfirstlane(it.parts), it.slot = __builtin_amdgcn_readfirstlane(it.slot), it.chunk = __builtin_amdgcn_readfirstlane(it.chunk);
+    int *p = (int *)&it;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(it) / sizeof(int)); ++i) p[i] = __builtin_amdgcn_readfirstlane(p[i]);
     return it.r >= 0;
 }
 
@@ -144,89 +176,163 @@ __device__ __forceinline__ float log2_scale(float s)
     return (float)((int)(b >> 23) - 127) + __builtin_amdgcn_logf(__uint_as_float((b & 0x7fffff) | 0x3f800000));
 }
 
+// Where a lane reads the transposed fragments of a tile of values: rows 4 g + 0..3 and 8 more, channels 32 db + r
+__device__ __forceinline__ void value_places(int (&v_place)[4])
+{
+    const int lane = threadIdx.x & 63, i = lane & 15, row = 4 * (lane >> 5) + (i >> 2), c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) v_place[db] = row * kPfD + (((4 * db + c0) ^ v_swizzle(row)) << 3) + (i & 1) * 4;
+}
+
+// A block's scales as the softmax takes them: ck takes a score to a power of two, lv = log2 Vs, add what is added (lv, or -inf where the block is
+// absent); `most`: the largest lv so far.  zero: its values count as 0.
+struct BlockScale {
+    float ck, lv, add;
+    bool zero;
+};
+__device__ __forceinline__ BlockScale block_scale(float ks, float vs, bool there, float c, float most)
+{
+    BlockScale b;
+    const float l = vs > 0.0f ? log2_scale(vs) : kPbNone;
+    b.zero = !(l >= most - kPbRange) || !there;
+    b.lv = !b.zero ? l : most > -1.0e29f ? most : 0.0f;
+    b.add = there ? b.lv : -INFINITY;
+    b.ck = fmaxf(ks, 0x1p-126f) * c;                   // (not 0: a masked score is -inf)
+    return b;
+}
+
+// Per lane: a row's references of the weights with and without Vs, the sum of those without (of this half's keys), and O^T:
+// o[db][i] = out[row][32 db + acc_row(i, g)].
+struct RowState {
+    float mv, m, l;
+    float16v o[4];
+    __device__ void clear()
+    {
+        mv = m = kPbNone, l = 0.0f;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+    }
+    __device__ float by() const { return __builtin_amdgcn_exp2f(mv - m - kPbHead); }         // of o, to the weights over m
+};
+
+// 32 TILES scores a row (16 TILES a lane) of NG blocks to weights
+template <int TILES, int NG>
+__device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockScale (&b)[NG], RowState &st, half8 (&wb)[2 * TILES])
+{
+    constexpr int kOf = 16 * TILES / NG;               // scores of a block
+    float top = -INFINITY, top_v = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = k * kOf; e < (k + 1) * kOf; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
+        top_v = fmaxf(top_v, __builtin_fmaf(mx, b[k].ck, b[k].add));
+        top = fmaxf(top, __builtin_fmaf(mx, b[k].ck, b[k].add - b[k].lv));
+    }
+    auto both = [&](float v) {                         // (the other half-wave holds the row's other keys)
+        const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+    };
+    top = both(top), top_v = both(top_v);
+    if (__any(top > st.m)) {
+        const float to = fmaxf(top, st.m);
+        st.l *= __builtin_amdgcn_exp2f(st.m - to), st.m = to;
+    }
+    if (__any(top_v > st.mv)) {
+        const float to = fmaxf(top_v, st.mv), alpha = __builtin_amdgcn_exp2f(st.mv - to);
+        st.mv = to;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[db][i] *= alpha;
+    }
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+        const float off = b[k].add - st.mv + kPbHead;
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = k * kOf; e < (k + 1) * kOf; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], b[k].ck, off));
+            sum += w, wb[e >> 3][e & 7] = (_Float16)w;
+        }
+        st.l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(st.mv - st.m - b[k].lv - kPbHead), st.l);
+    }
+}
+
+// 16 KEYS tokens' weights times their values, in a tile of local memory
+template <int KEYS>
+__device__ __forceinline__ void add_values(const _Float16 *Vt, const int (&v_place)[4], const half8 (&wb)[KEYS], RowState &st)
+{
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+            const _Float16 *p = Vt + k * 16 * kPfD + v_place[db];
+            const half4 lo = read_transposed(p), hi = read_transposed(p + 8 * kPfD);
+            st.o[db] = mfma32<false>(half8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, wb[k], st.o[db]);
+        }
+}
+
+// The requests' blocks as a walk sees them
+struct Pages {
+    const uint8_t *K, *V;
+    const float *Ks, *Vs;
+    const int32_t *table;                              // the request's row
+    int entries, n_blocks, Hkv, kvh, shift, L;
+    __device__ __forceinline__ int id(int token) const { return __builtin_amdgcn_readfirstlane(table[min(token >> shift, entries - 1)]); }
+    __device__ __forceinline__ bool there(int id) const { return (uint32_t)id < (uint32_t)n_blocks; }
+    __device__ __forceinline__ int64_t head(int id) const { return (int64_t)(there(id) ? id : 0) * Hkv + kvh; }
+};
+
 // NG: blocks that a tile of 64 tokens may hold (4, 2, 1 of 16, 32, 64 and 128 tokens).
 template <bool BF16, int NG>
-__global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs a)
+__device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &pg, _Float16 *tiles, int t0, int t1, int wt1, int full, int last, const half8 (&qf)[8],
+                                          RowState &st)
 {
-    __shared__ __align__(16) _Float16 tiles[2][2][kPfTile];            // [buffer][K, V]
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t idx = fast_div(blockIdx.x, a.hkv_magic, a.hkv_shift);
-    const int kvh = (int)(blockIdx.x - idx * a.Hkv);                   // (neighbours on a die walk through the same head)
-    PromptItem it;
-    if (!find_item(a, idx, (uint64_t *)tiles, it)) return;
-
-    const int M = it.n * a.rep, row0 = it.block * kPbRows, rows = min(M - row0, kPbRows), base = it.L - it.n;        // token of the first new one
-    auto token_of = [&](int row) { return base + (int)fast_div(row, a.rep_magic, a.rep_shift); };
-    const int seen = (token_of(row0 + rows - 1) + 64) >> 6;            // tiles that the block's last row sees (0 where it has no token)
-    const int parts = it.parts > 1 ? min(max((seen + it.chunk - 1) / it.chunk, 1), it.parts) : 1;
-    const int share = (seen + parts - 1) / parts, t0 = it.part * share, t1 = min(t0 + share, seen);
-    const int slot = (it.slot + it.part) * a.Hkv + kvh;
-    if (it.parts > 1 && tid == 0)
-        a.parts[slot] = int4{it.at, M, row0, it.part == 0 && parts > 1 ? kvh | parts << 16 : 0};
-    if (it.part >= parts) return;
-
-    const int w0 = row0 + 32 * wave;                   // the wave's first row; a lane's own (behind the last one: that again, not stored)
-    const bool works = w0 < M;
-    const int row = min(w0 + r, M - 1), query = (int)fast_div(row, a.rep_magic, a.rep_shift), head = kvh * a.rep + row - query * a.rep;
-    const int last = base + query;                     // the last token that the row sees
-    const int wt1 = works ? min(t1, (token_of(min(w0 + 31, M - 1)) + 64) >> 6) : t0, full = (token_of(min(w0, M - 1)) + 1) >> 6;     // tiles the wave sees, and whole
-    half8 qf[8];
-    {
-        const uint16_t *qp = a.q + (int64_t)(it.at + query) * a.q_stride + head * kD + g * 8;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const half8 *)(qp + ks * 16);
-    }
-
     // tile loads: thread tid has 16 channels of tokens tid / 8 and tid / 8 + 32
-    const int32_t *table = a.table + (int64_t)it.r * a.width;
-    const int entries = (it.L + (1 << a.shift) - 1) >> a.shift, key0 = tid >> 3, chunk = tid & 7, in_block = (1 << a.shift) - 1;
+    const int key0 = tid >> 3, chunk = tid & 7, in_block = (1 << pg.shift) - 1;
     int ids[NG];
-    float ks[NG], vs[NG];                              // of the tile whose codes are on the way
+    float ks[NG], vs[NG];                              // of the tile whose codes are on the way (negative: absent)
     u4b kraw[2], vraw[2];
     auto load_ids = [&](int n) {
 #pragma unroll
-        for (int b = 0; b < NG; ++b) ids[b] = __builtin_amdgcn_readfirstlane(table[min((n * 64 + b * (64 / NG)) >> a.shift, entries - 1)]);
+        for (int b = 0; b < NG; ++b) ids[b] = pg.id(n * 64 + b * (64 / NG));
     };
     // what belongs to the block of the thread's token j (the same for the whole wave)
     auto of_token = [&](const auto &v, int j) { return NG == 4 ? (wave >> 1 ? v[(2 * j + 1) % NG] : v[2 * j % NG]) : v[j % NG]; };
     auto load = [&](int n) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int id = of_token(ids, j);
-            const int64_t at = ((int64_t)((uint32_t)id < (uint32_t)a.n_blocks ? id : 0) * a.Hkv + kvh) << a.shift;
-            const int64_t off = (at + ((n * 64 + key0 + 32 * j) & in_block)) * kD + chunk * 16;
-            kraw[j] = *(const u4b *)(a.K + off), vraw[j] = *(const u4b *)(a.V + off);
+            const int64_t off = ((pg.head(of_token(ids, j)) << pg.shift) + ((n * 64 + key0 + 32 * j) & in_block)) * kD + chunk * 16;
+            kraw[j] = *(const u4b *)(pg.K + off), vraw[j] = *(const u4b *)(pg.V + off);
         }
 #pragma unroll
         for (int b = 0; b < NG; ++b) {
-            const bool there = (uint32_t)ids[b] < (uint32_t)a.n_blocks;
-            const int64_t at = (int64_t)(there ? ids[b] : 0) * a.Hkv + kvh;
-            ks[b] = there ? a.Ks[at] : -1.0f, vs[b] = there ? a.Vs[at] : -1.0f;
+            const int64_t at = pg.head(ids[b]);
+            const bool there = pg.there(ids[b]);
+            ks[b] = there ? pg.Ks[at] : -1.0f, vs[b] = there ? pg.Vs[at] : -1.0f;
         }
     };
-    float ck[NG], lv[NG], add[NG];                     // of the tile in local memory: score to power of two, log2 Vs, and what is added (-inf: absent)
-    float most = -1.0e30f;                             // the largest log2 Vs so far
+    BlockScale scale[NG];                              // of the tile in local memory
+    float most = -1.0e30f;
     auto store = [&](int n) {
-        bool zero[NG];
+        bool none[NG], zero[NG];
 #pragma unroll
         for (int b = 0; b < NG; ++b)
             if (vs[b] > 0.0f) most = fmaxf(most, log2_scale(vs[b]));
 #pragma unroll
-        for (int b = 0; b < NG; ++b) {
-            const float l = vs[b] > 0.0f ? log2_scale(vs[b]) : kPbNone;
-            zero[b] = !(l >= most - kPbRange);
-            lv[b] = !zero[b] ? l : most > -1.0e29f ? most : 0.0f;
-            add[b] = vs[b] < 0.0f ? -INFINITY : lv[b];
-            ck[b] = fmaxf(ks[b], 0x1p-126f) * a.c;     // (not 0: a masked score is -inf)
-        }
+        for (int b = 0; b < NG; ++b) scale[b] = block_scale(ks[b], vs[b], vs[b] >= 0.0f, a.c, most), none[b] = vs[b] < 0.0f, zero[b] = scale[b].zero;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = key0 + 32 * j;
-            const bool in = n * 64 + key < it.L, none = of_token(vs, j) < 0.0f, nil = of_token(zero, j);
+            const bool in = n * 64 + key < pg.L, no_key = of_token(none, j), no_value = of_token(zero, j);
             u4b k = kraw[j], v = vraw[j], x[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = in && !none ? k[e] : 0, v[e] = in && !nil ? v[e] : 0;
-            _Float16 *Kt = tiles[n & 1][0] + key * kPfD, *Vt = tiles[n & 1][1] + key * kPfD;
+            for (int e = 0; e < 4; ++e) k[e] = in && !no_key ? k[e] : 0, v[e] = in && !no_value ? v[e] : 0;
+            _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile + key * kPfD, *Vt = Kt + kPfTile;
             widen<BF16>(k, x);
 #pragma unroll
             for (int e = 0; e < 2; ++e) *(u4b *)(Kt + (((2 * chunk + e) ^ (key & 15)) << 3)) = x[e];
@@ -235,191 +341,273 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
             for (int e = 0; e < 2; ++e) *(u4b *)(Vt + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = x[e];
         }
     };
-
-    // fragment places
     int k_place[8], v_place[4];
 #pragma unroll
     for (int s = 0; s < 8; ++s) k_place[s] = tile_place(r, 2 * s + g);
-    {
-        const int i = lane & 15, row = 4 * g + (i >> 2), c0 = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-#pragma unroll
-        for (int db = 0; db < 4; ++db) v_place[db] = row * kPfD + (((4 * db + c0) ^ v_swizzle(row)) << 3) + (i & 1) * 4;
-    }
+    value_places(v_place);
 
-    float16v o[4];                                     // O^T: o[db][i] = out[row][32 db + acc_row(i, g)]
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-    float mv = kPbNone, m = kPbNone, l = 0.0f;         // references of the weights with and without Vs; sum of the weights without, of this half's keys
-
-    auto compute = [&](int n) {
-        const _Float16 *Kt = tiles[n & 1][0], *Vt = tiles[n & 1][1];
-        float16v s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s[t] = mfma32<BF16>(*(const half8 *)(Kt + t * 32 * kPfD + k_place[k]), qf[k], s[t]);
+    load_ids(t0);
+    load(t0);
+    if (t0 + 1 < t1) load_ids(t0 + 1);
+    store(t0);
+    __syncthreads();
+    for (int n = t0; n < t1; ++n) {
+        if (n + 1 < t1) {
+            load(n + 1);
+            if (n + 2 < t1) load_ids(n + 2);
         }
-        if (n >= full) {
-            const int rel = last - n * 64 - 4 * g;
+        if (n < wt1) {
+            const _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile, *Vt = Kt + kPfTile;
+            float16v s[2];
+            half8 wb[4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (t * 32 + acc_row(i, 0) > rel) s[t][i] = -INFINITY;
-        }
-        constexpr int kOf = 32 / NG;                   // scores of a block
-        float top = -INFINITY, top_v = -INFINITY;
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-        for (int b = 0; b < NG; ++b) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int e = b * kOf; e < (b + 1) * kOf; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
-            top_v = fmaxf(top_v, __builtin_fmaf(mx, ck[b], add[b]));
-            top = fmaxf(top, __builtin_fmaf(mx, ck[b], add[b] - lv[b]));
-        }
-        auto both = [&](float v) {                     // (the other half-wave holds the row's other keys)
-            const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-            return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-        };
-        top = both(top), top_v = both(top_v);
-        if (__any(top > m)) {
-            const float to = fmaxf(top, m);
-            l *= __builtin_amdgcn_exp2f(m - to), m = to;
-        }
-        if (__any(top_v > mv)) {
-            const float to = fmaxf(top_v, mv), alpha = __builtin_amdgcn_exp2f(mv - to);
-            mv = to;
-#pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-        }
-        half8 wb[4];
-#pragma unroll
-        for (int b = 0; b < NG; ++b) {
-            const float off = add[b] - mv + kPbHead;
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = b * kOf; e < (b + 1) * kOf; ++e) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], ck[b], off));
-                sum += w, wb[e >> 3][e & 7] = (_Float16)w;
+                for (int k = 0; k < 8; ++k) s[t] = mfma32<BF16>(*(const half8 *)(Kt + t * 32 * kPfD + k_place[k]), qf[k], s[t]);
             }
-            l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(mv - m - lv[b] - kPbHead), l);
-        }
+            if (n >= full) {
+                const int rel = last - n * 64 - 4 * g;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int db = 0; db < 4; ++db) {
-                const _Float16 *p = Vt + k * 16 * kPfD + v_place[db];
-                const half4 lo = read_transposed(p), hi = read_transposed(p + 8 * kPfD);
-                o[db] = mfma32<false>(half8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, wb[k], o[db]);
+                    for (int i = 0; i < 16; ++i)
+                        if (t * 32 + acc_row(i, 0) > rel) s[t][i] = -INFINITY;
             }
-    };
-
-    if (t0 < t1) {
-        load_ids(t0);
-        load(t0);
-        if (t0 + 1 < t1) load_ids(t0 + 1);
-        store(t0);
+            softmax_step<2, NG>(s, scale, st, wb);
+            add_values<4>(Vt, v_place, wb, st);
+        }
+        if (n + 1 < t1) store(n + 1);
         __syncthreads();
-        for (int n = t0; n < t1; ++n) {
-            if (n + 1 < t1) {
-                load(n + 1);
-                if (n + 2 < t1) load_ids(n + 2);
-            }
-            if (n < wt1) compute(n);
-            if (n + 1 < t1) store(n + 1);
-            __syncthreads();
-        }
     }
-    if (w0 + r >= M) return;
+}
 
-    {
-        const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-        l = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+// A wave's 32 tokens on their way: a lane has channels 64 g .. 64 g + 63 of key r, and 16 channels of the values of tokens lane / 8 + 8 j
+template <int NG> struct Unit {
+    u4b k[4], v[4];
+    float ks[NG], vs[NG];
+    int ids[NG];                                       // of the unit after it
+};
+
+// Units of 32 tokens u0, u0 + 4, ... below u1.  qf: Q[row][64 g + 8 s ..], the channels in the order in which a lane has the keys'.  NG: 2 blocks of 16 tokens, or 1.
+template <bool BF16, int NG>
+__device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages &pg, _Float16 *Vt, int u0, int u1, int full, int last, const half8 (&qf)[8],
+                                            RowState &st)
+{
+    const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5, key0 = lane >> 3, chunk = lane & 7, in_block = (1 << pg.shift) - 1;
+    int v_place[4];
+    value_places(v_place);
+    float most = -1.0e30f;
+    auto load_ids = [&](Unit<NG> &x, int u) {
+#pragma unroll
+        for (int b = 0; b < NG; ++b) x.ids[b] = pg.id(u * 32 + b * 16);
+    };
+    auto load = [&](Unit<NG> &x, int u) {
+        const int of_key = NG == 1 ? x.ids[0] : r & 16 ? x.ids[NG - 1] : x.ids[0];
+        const uint8_t *K = pg.K + ((pg.head(of_key) << pg.shift) + ((u * 32 + r) & in_block)) * kD + 64 * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.k[j] = *(const u4b *)(K + 16 * j);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            x.v[j] = *(const u4b *)(pg.V + ((pg.head(x.ids[j * NG / 4]) << pg.shift) + ((u * 32 + key0 + 8 * j) & in_block)) * kD + chunk * 16);
+#pragma unroll
+        for (int b = 0; b < NG; ++b) {
+            const int64_t at = pg.head(x.ids[b]);
+            const bool there = pg.there(x.ids[b]);
+            x.ks[b] = there ? pg.Ks[at] : -1.0f, x.vs[b] = there ? pg.Vs[at] : -1.0f;
+        }
+    };
+    auto step = [&](Unit<NG> &x, int u) {
+        BlockScale scale[NG];
+#pragma unroll
+        for (int b = 0; b < NG; ++b)
+            if (x.vs[b] > 0.0f) most = fmaxf(most, log2_scale(x.vs[b]));
+#pragma unroll
+        for (int b = 0; b < NG; ++b) scale[b] = block_scale(x.ks[b], x.vs[b], x.vs[b] >= 0.0f, a.c, most);
+        float16v s[1];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
+        const bool tail = u * 32 + 32 > pg.L;
+        const bool no_key = (tail && u * 32 + r >= pg.L) || (NG == 1 ? x.vs[0] < 0.0f : r & 16 ? x.vs[NG - 1] < 0.0f : x.vs[0] < 0.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u4b k = x.k[j], w[2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = no_key ? 0 : k[e];
+            widen<BF16>(k, w);
+            s[0] = mfma32<BF16>(__builtin_bit_cast(half8, w[0]), qf[2 * j], s[0]);
+            s[0] = mfma32<BF16>(__builtin_bit_cast(half8, w[1]), qf[2 * j + 1], s[0]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 8 * j;
+            const bool no_value = (tail && u * 32 + key >= pg.L) || scale[j * NG / 4].zero;
+            u4b v = x.v[j], w[2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = no_value ? 0 : v[e];
+            widen<false>(v, w);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) *(u4b *)(Vt + key * kPfD + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = w[e];
+        }
+        if (u + 8 < u1) {                              // what was in the registers has been taken
+            load(x, u + 8);
+            if (u + 16 < u1) load_ids(x, u + 16);
+        }
+        if (u >= full) {
+            const int rel = last - u * 32 - 4 * g;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (acc_row(i, 0) > rel) s[0][i] = -INFINITY;
+        }
+        half8 wb[2];
+        softmax_step<1, NG>(s, scale, st, wb);
+        add_values<2>(Vt, v_place, wb, st);
+    };
+    Unit<NG> x, y;
+    if (u0 < u1) load_ids(x, u0);
+    if (u0 + 4 < u1) load_ids(y, u0 + 4);
+    if (u0 < u1) {
+        load(x, u0);
+        if (u0 + 8 < u1) load_ids(x, u0 + 8);
     }
-    const float by = __builtin_amdgcn_exp2f(mv - m - kPbHead);         // of o, to the weights over m
-    if (parts > 1) {
-        const int64_t at = (int64_t)slot * a.part_rows + (row - row0);
-        if (g == 0) *(float2 *)(a.ml + at * 2) = float2{m, l};
-        float *p = a.o + at * kD + g * 4;
+    if (u0 + 4 < u1) {
+        load(y, u0 + 4);
+        if (u0 + 12 < u1) load_ids(y, u0 + 12);
+    }
+    for (int u = u0; u < u1; u += 8) {
+        step(x, u);
+        if (u + 4 < u1) step(y, u + 4);
+    }
+}
+
+template <bool BF16, int NG>
+__global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs a)
+{
+    // tiles [buffer][K, V] of a wide block, or each wave's values of a narrow one; at the end the waves' rows
+    __shared__ __align__(16) _Float16 tiles[4 * kPfTile];
+    __shared__ float2 wave_ml[4][32];
+    __shared__ int ticket;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t idx = fast_div(blockIdx.x, a.hkv_magic, a.hkv_shift);
+    const int kvh = (int)(blockIdx.x - idx * a.Hkv);                   // (neighbours on a die walk through the same head)
+    PromptItem it;
+    if (!find_item(a, idx, (uint64_t *)tiles, it)) return;
+
+    const int M = it.n * a.rep, rows = min(M - it.row0, it.narrow ? kPbNarrow : kPbRows), base = it.L - it.n;        // rows of the block; token of the first new one
+    auto query_of = [&](int row) { return (int)fast_div(row, a.rep_magic, a.rep_shift); };
+    const int seen = (base + query_of(it.row0 + rows - 1) + 64) >> 6;  // tiles that the block's last row sees (0 or less where it has no token)
+    const int parts = it.parts > 1 ? min(max((seen + it.chunk - 1) / it.chunk, 1), it.parts) : 1;
+    if (it.part >= parts) return;
+    const int share = (seen + parts - 1) / parts, t0 = it.part * share, t1 = min(t0 + share, seen);
+
+    const int w0 = it.row0 + (it.narrow ? 0 : 32 * wave);              // the wave's first row; a lane's own (behind the last one: that again, not stored)
+    const int row = min(w0 + r, M - 1), query = query_of(row), last = base + query;              // the last token that the row sees
+    const int low = base + query_of(min(w0, M - 1)), high = base + query_of(min(w0 + 31, M - 1));       // of the wave's first and last row
+    half8 qf[8];
+    {
+        const uint16_t *qp = a.q + (int64_t)(it.at + query) * a.q_stride + (kvh * a.rep + row - query * a.rep) * kD;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) qf[s] = *(const half8 *)(qp + (it.narrow ? 64 * g + 8 * s : 16 * s + 8 * g));
+    }
+    const Pages pg{a.K, a.V, a.Ks, a.Vs, a.table + (int64_t)it.r * a.width, (it.L + (1 << a.shift) - 1) >> a.shift, a.n_blocks, a.Hkv, kvh, a.shift, it.L};
+    RowState st;
+    st.clear();
+    if (it.narrow)
+        walk_narrow<BF16, NG == 4 ? 2 : 1>(a, pg, tiles + wave * kPfTile / 2, 2 * t0 + wave, 2 * t1, (low + 1) >> 5, last, qf, st);
+    else if (t0 < t1)
+        walk_wide<BF16, NG>(a, pg, tiles, t0, t1, w0 < M ? min(t1, (high + 64) >> 6) : t0, (low + 1) >> 6, last, qf, st);
+
+    // the waves' rows in local memory, 16 bytes of channels at place (channels / 4) ^ row, so that writes of 32 rows and reads of one use all banks
+    float *rows_of = (float *)tiles;
+    __syncthreads();
+    {
+        const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
+        if (g == 0) wave_ml[wave][r] = float2{st.m, __uint_as_float(h[0]) + __uint_as_float(h[1])};
+        const float by = st.by();
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *(float4 *)(p + db * 32 + (i >> 2) * 8) = float4{o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
-        return;
+                *(float4 *)(rows_of + (wave * 32 + r) * kD + (((db * 8 + (i >> 1) + g) ^ r) << 2)) =
+                    float4{st.o[db][i] * by, st.o[db][i + 1] * by, st.o[db][i + 2] * by, st.o[db][i + 3] * by};
     }
-    const float inv = l > 0.0f ? by / l : 0.0f;
-    const int64_t to = (int64_t)(it.at + query) * a.Hq + head;
-    if (a.lse && g == 0) a.lse[to] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-    uint16_t *p = a.out + to * kD + g * 4;
+    __syncthreads();
+    const int quad = tid & 31;                         // a thread's four channels, of rows tid / 32 + 8 k
+    auto finish = [&](int i, float m, float l, float4 o) {
+        const int row = it.row0 + i, query = query_of(row);
+        const int64_t to = (int64_t)(it.at + query) * a.Hq + kvh * a.rep + row - query * a.rep;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        *(half4 *)(a.out + to * kD + quad * 4) = half4{to16<BF16>(o.x * inv), to16<BF16>(o.y * inv), to16<BF16>(o.z * inv), to16<BF16>(o.w * inv)};
+        if (a.lse && quad == 0) a.lse[to] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    };
+    auto keep = [&](int slot, int i, float m, float l, float4 o) {
+        const int64_t at = (int64_t)slot * a.part_rows + i;
+        if (quad == 0) pb_store(a.ml + at * 2, m, l);
+        pb_store(a.o + at * kD + quad * 4, o.x, o.y), pb_store(a.o + at * kD + quad * 4 + 2, o.z, o.w);
+    };
+    auto slot_of = [&](int part) { return (it.slot + part) * a.Hkv + kvh; };
+    for (int i = tid >> 5; i < rows; i += 8) {
+        float m, l;
+        float4 o;
+        if (it.narrow) {
+            float2 ml[4];
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+            for (int w = 0; w < 4; ++w) ml[w] = wave_ml[w][i];
+            m = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), l = 0.0f, o = float4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            half4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = to16<BF16>(o[db][i + e] * inv);
-            *(half4 *)(p + db * 32 + (i >> 2) * 8) = v;
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f(ml[w].x - m);
+                const float4 v = *(const float4 *)(rows_of + (w * 32 + i) * kD + ((quad ^ i) << 2));
+                l = __builtin_fmaf(ml[w].y, f, l);
+                o.x = __builtin_fmaf(v.x, f, o.x), o.y = __builtin_fmaf(v.y, f, o.y), o.z = __builtin_fmaf(v.z, f, o.z), o.w = __builtin_fmaf(v.w, f, o.w);
+            }
+        } else {
+            const float2 ml = wave_ml[i >> 5][i & 31];
+            m = ml.x, l = ml.y, o = *(const float4 *)(rows_of + i * kD + ((quad ^ (i & 31)) << 2));
         }
-}
-
-// The rows whose walk was made in parts: a wave a row, two channels a lane.
-constexpr int kPbJoinRows = 16;                        // of a workgroup
-
-template <bool BF16>
-__global__ __launch_bounds__(kPbThreads) void prompt_join_kernel(PromptBlkArgs a, int groups)
-{
-    const int slot = (int)blockIdx.x / groups, group = (int)blockIdx.x % groups, lane = threadIdx.x & 63;
-    if (slot >= a.header[0]) return;
-    const int4 d = a.parts[slot];
-    const int parts = d.w >> 16, kvh = d.w & 0xffff, M = d.y, row0 = d.z;
-    // (a call whose cu is not what it has to be may leave parts without a description of their own)
-    if (parts < 2 || kvh >= a.Hkv || (int64_t)slot + (int64_t)(parts - 1) * a.Hkv >= a.header[0] || d.x < 0 || row0 < 0) return;
-    const int end = min(M - row0, min((group + 1) * kPbJoinRows, a.part_rows));
-    for (int i = group * kPbJoinRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < end; i += 4) {
-        auto at = [&](int j) { return ((int64_t)slot + (int64_t)j * a.Hkv) * a.part_rows + i; };
-        float m = kPbNone, l = 0.0f, x = 0.0f, y = 0.0f;
-        for (int j0 = 0; j0 < parts; j0 += 64) {
-            float2 ml = float2{kPbNone, 0.0f};
-            if (j0 + lane < parts) ml = *(const float2 *)(a.ml + at(j0 + lane) * 2);
-            float top = ml.x;
+        if (parts == 1) finish(i, m, l, o);
+        else keep(slot_of(it.part), i, m, l, o);
+    }
+    // joins: step is how many parts each of up to eight results stands for
+    for (int step = 1, level = 0; step < parts; step *= kPbJoin, ++level) {
+        const int first = it.part / (step * kPbJoin) * (step * kPbJoin), n = min((parts - first + step - 1) / step, kPbJoin);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wave's results are where every die sees them
+        __syncthreads();
+        if (n > 1) {
+            if (tid == 0) {
+                int *t = a.tickets + level * 2 * kPbSlots + slot_of(first);
+                ticket = __hip_atomic_fetch_add(t, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (ticket == n - 1) __hip_atomic_store(t, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // ready for the next call
+            }
+            __syncthreads();
+            if (ticket != n - 1) return;
+            const bool done = step * kPbJoin >= parts;
+            for (int i = tid >> 5; i < rows; i += 8) {
+                float2 ml[kPbJoin], lo[kPbJoin], hi[kPbJoin];
 #pragma unroll
-            for (int s = 32; s; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
-            top = fmaxf(top, m);
-            const float old = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
-            float sum = ml.y * f;
-#pragma unroll
-            for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s, 64);
-            m = top, l = l * old + sum, x *= old, y *= old;
-            const int n = min(parts - j0, 64);
-            for (int j = 0; j < n; j += 8) {
-                float2 v[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = *(const float2 *)(a.o + at(j0 + min(j + k, n - 1)) * kD + lane * 2);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float w = j + k < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(j + k, n - 1))) : 0.0f;
-                    x = __builtin_fmaf(v[k].x, w, x), y = __builtin_fmaf(v[k].y, w, y);
+                for (int j = 0; j < kPbJoin; ++j) {
+                    const int64_t at = (int64_t)slot_of(first + min(j, n - 1) * step) * a.part_rows + i;
+                    ml[j] = pb_pair(pb_load(a.ml + at * 2)), lo[j] = pb_pair(pb_load(a.o + at * kD + quad * 4));
+                    hi[j] = pb_pair(pb_load(a.o + at * kD + quad * 4 + 2));
                 }
+                float m = kPbNone, l = 0.0f;
+                float4 o = float4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < kPbJoin; ++j) m = fmaxf(m, ml[j].x);
+#pragma unroll
+                for (int j = 0; j < kPbJoin; ++j) {
+                    const float f = j < n ? __builtin_amdgcn_exp2f(ml[j].x - m) : 0.0f;
+                    l = __builtin_fmaf(ml[j].y, f, l);
+                    o.x = __builtin_fmaf(lo[j].x, f, o.x), o.y = __builtin_fmaf(lo[j].y, f, o.y);
+                    o.z = __builtin_fmaf(hi[j].x, f, o.z), o.w = __builtin_fmaf(hi[j].y, f, o.w);
+                }
+                if (done) finish(i, m, l, o);
+                else keep(slot_of(first), i, m, l, o);
             }
         }
-        const int row = row0 + i, query = (int)fast_div(row, a.rep_magic, a.rep_shift);
-        if (query >= a.T - d.x) return;
-        const int64_t to = (int64_t)(d.x + query) * a.Hq + kvh * a.rep + row - query * a.rep;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        const _Float16 p = to16<BF16>(x * inv), q = to16<BF16>(y * inv);
-        *(half2p *)(a.out + to * kD + lane * 2) = half2p{p, q};
-        if (a.lse && lane == 0) a.lse[to] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
 }
-
-constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
 
 static int part_rows(const minikv_blk_shape &s, int32_t T)
 {
@@ -427,10 +615,10 @@ static int part_rows(const minikv_blk_shape &s, int32_t T)
     return (int)(rows < kPbRows ? rows : kPbRows);
 }
 
-// [header][parts][(m, l) of the parts' rows][their outputs]
+// [tickets][(m, l) of the parts' rows][their outputs]
 size_t prompt_blk_workspace_bytes(const minikv_blk_shape &s, int32_t T)
 {
-    return 64 + (size_t)2 * kPbSlots * (sizeof(int4) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
+    return (size_t)2 * kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
 }
 
 int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
@@ -440,12 +628,12 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
     a.q = (const uint16_t *)q, a.q_stride = q_stride, a.K = c.K, a.V = c.V, a.Ks = c.Ks, a.Vs = c.Vs;
     a.table = table, a.q_len = q_len, a.cu = cu, a.out = (uint16_t *)out, a.lse = lse;
     a.R = s.R, a.T = T, a.Hq = s.Hq, a.Hkv = s.Hkv, a.rep = s.Hq / s.Hkv, a.n_blocks = s.n_blocks, a.width = s.max_blocks;
-    a.shift = __builtin_ctz(s.block), a.c = sm_scale * kLog2e, a.slots = kPbSlots, a.part_rows = part_rows(s, T);
-    a.header = (int *)workspace, a.parts = (int4 *)((char *)workspace + 64);
-    a.ml = (float *)(a.parts + 2 * kPbSlots), a.o = a.ml + (size_t)2 * kPbSlots * a.part_rows * 2;
+    a.shift = __builtin_ctz(s.block), a.c = sm_scale * kLog2e, a.part_rows = part_rows(s, T);
+    a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * 2 * kPbSlots), a.o = a.ml + (size_t)2 * kPbSlots * a.part_rows * 2;
     fast_div_setup((uint32_t)s.Hkv, a.hkv_magic, a.hkv_shift);
     fast_div_setup((uint32_t)a.rep, a.rep_magic, a.rep_shift);
-    const int64_t blocks = (int64_t)T * a.rep / kPbRows + (s.R < T ? s.R : T), items = blocks * s.Hkv + kPbSlots;
+    // row blocks: 128 rows each, and up to two for the rest of each request that has rows
+    const int64_t blocks = (int64_t)T * a.rep / kPbRows + 2 * (int64_t)(s.R < T ? s.R : T), items = blocks * s.Hkv + kPbSlots;
     if (items > 0x7fffff) return MINIKV_EINVAL;
     const dim3 grid((unsigned)items), threads(kPbThreads);
     const bool bf16 = s.dtype == MINIKV_BF16;
@@ -460,10 +648,6 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
         LAUNCH(1);
     }
 #undef LAUNCH
-    const int groups = (a.part_rows + kPbJoinRows - 1) / kPbJoinRows;
-    const dim3 join(2 * kPbSlots * groups);
-    if (bf16) hipLaunchKernelGGL((prompt_join_kernel<true>), join, threads, 0, st, a, groups);
-    else hipLaunchKernelGGL((prompt_join_kernel<false>), join, threads, 0, st, a, groups);
     return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
 }
 

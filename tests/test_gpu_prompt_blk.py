@@ -40,7 +40,7 @@ class Case:
         self.out = torch.full((self.T, self.Hq, 128), 7.0, dtype=self.dtype, device="cuda")
         self.lse = torch.full((self.T, self.Hq), 7.0, device="cuda")
         if ws is None:
-            ws = torch.full((api.minikv_prompt_blk_workspace_bytes(self.shape, T),), 0xab, dtype=torch.uint8, device="cuda")
+            ws = torch.zeros(api.minikv_prompt_blk_workspace_bytes(self.shape, T), dtype=torch.uint8, device="cuda")
         self.ws = ws
         self.args = (self.shape, T, self.q_dev, self.cache, self.table.cuda(), self.q_len.cuda(), self.cu.cuda(), SM, self.out,
                      self.lse if lse else None, ws)

@@ -52,7 +52,7 @@ class Program:
             api.minikv_norm_rope(self.Hq, self.Hkv, T, q, k, self.w[0], self.w[1], 1e-6, self.inv, 128, False, pos, q, k)
             api.kv_quantize_blk(self.shape, k, v, slots, cache)
             out, lse = torch.full((T, self.Hq, 128), 7.0, dtype=self.dtype, device="cuda"), torch.full((T, self.Hq), 7.0, device="cuda")
-            ws = torch.empty(api.minikv_prompt_blk_workspace_bytes(self.shape, T), dtype=torch.uint8, device="cuda")
+            ws = torch.zeros(api.minikv_prompt_blk_workspace_bytes(self.shape, T), dtype=torch.uint8, device="cuda")
             api.minikv_prompt_attn_blk(self.shape, T, q, cache, self.table, self.q_len_next, self.cu, SM, out, lse, ws)
             raw = [x.view(torch.uint8).cpu() if x.element_size() == 1 else x.cpu() for x in (cache.K, cache.Ks, cache.V, cache.Vs)]
             check_prompt(self.shape, q, raw, self.table.cpu(), self.q_len_next.cpu(), self.cu.cpu(), out, lse)
