@@ -41,7 +41,7 @@ struct PromptBlkArgs {
     const int32_t *table, *q_len, *cu;
     uint16_t *out;
     float *lse;
-    int *tickets;                                      // [3][2 * kPbSlots], of the first part of each eight, 64, 512
+    int *tickets;                                      // [3][kPbSlots], of the first part of each eight, 64, 512
     float *ml, *o;                                     // [part][row] (m, l) and [part][row][128]
     int part_rows;
     float c;                                           // sm_scale * log2(e)
@@ -67,10 +67,10 @@ __device__ inline void pb_store(float *p, float a, float b)
 }
 __device__ inline float2 pb_pair(uint64_t v) { return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))}; }
 
-// The requests' rows in blocks, each block's walk in parts of about the cost that there is for a slot (of workgroups at once).  A
-// block has ceil(cost / chunk) parts, chunk = ceil(all blocks' cost / slots): at most slots more than there are blocks, and at most twice slots where
-// there are two or more.  The longest walks come first: a request's narrow blocks, then its wide ones from the last on.  Every workgroup
-// counts all that for itself.
+// The requests' rows in blocks, each block's walk in parts of at least the cost that there is for a slot (of workgroups at once): a block has
+// max(floor(cost / chunk), 1) parts, chunk = ceil(all blocks' cost / slots), so that those of two and more are not more than slots, and run at
+// once (with ceil(cost / chunk), 16 x 8 tokens behind 16384 had 568 parts for 512 slots: 123 us instead of 100).  They come first, then the blocks in
+// one part; of a request the narrow blocks, then the wide ones from the last on, whose walks are the longest.  Every workgroup counts all that for itself.
 __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t *lds, PromptItem &it)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -79,7 +79,7 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
         int at, n, L;
         uint32_t wide, narrow, tiles;
     };
-    auto request = [&](int r) {
+    auto read = [&](int r) {
         Request q;
         q.at = a.cu[r];
         const int end = a.cu[r + 1];
@@ -90,6 +90,9 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
         q.tiles = (uint32_t)max((q.L + 63) >> 6, 1);
         return q;
     };
+    Request mine{0, 0, 0, 0, 0, 1};
+    if (r0 < r1) mine = read(r0);
+    auto request = [&](int r) { return r == r0 ? mine : read(r); };
     uint32_t *sums = (uint32_t *)(lds + 1);            // [2][4] of the waves
     PromptItem *found = (PromptItem *)(lds + 8);
     if (tid == 0) lds[0] = 0, found->r = -1;
@@ -103,15 +106,14 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
     __syncthreads();
     all = lds[0] * a.Hkv;
     const uint32_t chunk = max((uint32_t)((all + kPbSlots - 1) / kPbSlots), (uint32_t)kPbLeast);
-    auto wide_parts = [&](const Request &q) { return min((q.tiles * kPbWideCost + chunk - 1) / chunk, (uint32_t)kPbMost); };
-    auto narrow_parts = [&](const Request &q) { return min((q.tiles + chunk - 1) / chunk, (uint32_t)kPbMost); };
-    uint32_t v[2] = {0, 0};                            // items, and those of walks in two or more parts
+    auto parts_of = [&](uint32_t cost) { return min(max(cost / chunk, 1u), (uint32_t)kPbMost); };
+    uint32_t v[2] = {0, 0};                            // items of walks in two or more parts, and in one
     for (int r = r0; r < r1; ++r) {
         const Request q = request(r);
-        const uint32_t w = wide_parts(q), n = narrow_parts(q);
-        v[0] += q.wide * w + q.narrow * n, v[1] += (w > 1 ? q.wide * w : 0) + (n > 1 ? q.narrow * n : 0);
+        const uint32_t w = parts_of(q.tiles * kPbWideCost), n = parts_of(q.tiles);
+        v[w == 1] += q.wide * w, v[n == 1] += q.narrow * n;
     }
-    const uint32_t items = v[0], split = v[1];
+    const uint32_t items[2] = {v[0], v[1]};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -122,12 +124,15 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
         if (lane == 63) sums[k * 4 + wave] = v[k];
     }
     __syncthreads();
-    uint32_t first = v[0] - items, slot = v[1] - split;
-    for (int w = 0; w < wave; ++w) first += sums[w], slot += sums[4 + w];
-    if (idx >= first && idx - first < items)
+    const uint32_t split = sums[0] + sums[1] + sums[2] + sums[3];
+    const bool whole = idx >= split;                   // what is looked for
+    uint32_t first = whole ? split + v[1] - items[1] : v[0] - items[0];
+    for (int w = 0; w < wave; ++w) first += sums[(whole ? 4 : 0) + w];
+    if (idx >= first && idx - first < items[whole])
         for (int r = r0; r < r1; ++r) {
             const Request q = request(r);
-            const uint32_t w = wide_parts(q), n = narrow_parts(q), at = idx - first, narrow = q.narrow * n, wide = q.wide * w;
+            const uint32_t w = parts_of(q.tiles * kPbWideCost), n = parts_of(q.tiles), at = idx - first;
+            const uint32_t narrow = (n == 1) == whole ? q.narrow * n : 0, wide = (w == 1) == whole ? q.wide * w : 0;
             if (at < narrow + wide) {
                 const bool is_narrow = at < narrow;
                 const uint32_t p = is_narrow ? n : w, i = is_narrow ? at : at - narrow, k = i / p;
@@ -135,10 +140,10 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
                 found->narrow = is_narrow;
                 found->row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
                 found->part = (int)(i - k * p), found->parts = (int)p, found->chunk = (int)((q.tiles + p - 1) / p);
-                found->slot = (int)(slot + (is_narrow ? 0 : n > 1 ? narrow : 0) + k * p);
+                found->slot = (int)(idx - found->part);
                 break;
             }
-            first += narrow + wide, slot += (n > 1 ? narrow : 0) + (w > 1 ? wide : 0);
+            first += narrow + wide;
         }
     __syncthreads();
     it = *found;
@@ -576,34 +581,41 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
         __syncthreads();
         if (n > 1) {
             if (tid == 0) {
-                int *t = a.tickets + level * 2 * kPbSlots + slot_of(first);
+                int *t = a.tickets + level * kPbSlots + slot_of(first);
                 ticket = __hip_atomic_fetch_add(t, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 if (ticket == n - 1) __hip_atomic_store(t, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // ready for the next call
             }
             __syncthreads();
             if (ticket != n - 1) return;
             const bool done = step * kPbJoin >= parts;
-            for (int i = tid >> 5; i < rows; i += 8) {
-                float2 ml[kPbJoin], lo[kPbJoin], hi[kPbJoin];
+            for (int i0 = tid >> 5; i0 < rows; i0 += 16) {             // two rows a round trip
+                float2 ml[2][kPbJoin], lo[2][kPbJoin], hi[2][kPbJoin];
 #pragma unroll
-                for (int j = 0; j < kPbJoin; ++j) {
-                    const int64_t at = (int64_t)slot_of(first + min(j, n - 1) * step) * a.part_rows + i;
-                    ml[j] = pb_pair(pb_load(a.ml + at * 2)), lo[j] = pb_pair(pb_load(a.o + at * kD + quad * 4));
-                    hi[j] = pb_pair(pb_load(a.o + at * kD + quad * 4 + 2));
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int j = 0; j < kPbJoin; ++j) {
+                        const int64_t at = (int64_t)slot_of(first + min(j, n - 1) * step) * a.part_rows + min(i0 + 8 * e, rows - 1);
+                        ml[e][j] = pb_pair(pb_load(a.ml + at * 2)), lo[e][j] = pb_pair(pb_load(a.o + at * kD + quad * 4));
+                        hi[e][j] = pb_pair(pb_load(a.o + at * kD + quad * 4 + 2));
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int i = i0 + 8 * e;
+                    float m = kPbNone, l = 0.0f;
+                    float4 o = float4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < kPbJoin; ++j) m = fmaxf(m, ml[e][j].x);
+#pragma unroll
+                    for (int j = 0; j < kPbJoin; ++j) {
+                        const float f = j < n ? __builtin_amdgcn_exp2f(ml[e][j].x - m) : 0.0f;
+                        l = __builtin_fmaf(ml[e][j].y, f, l);
+                        o.x = __builtin_fmaf(lo[e][j].x, f, o.x), o.y = __builtin_fmaf(lo[e][j].y, f, o.y);
+                        o.z = __builtin_fmaf(hi[e][j].x, f, o.z), o.w = __builtin_fmaf(hi[e][j].y, f, o.w);
+                    }
+                    if (i >= rows) break;
+                    if (done) finish(i, m, l, o);
+                    else keep(slot_of(first), i, m, l, o);
                 }
-                float m = kPbNone, l = 0.0f;
-                float4 o = float4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int j = 0; j < kPbJoin; ++j) m = fmaxf(m, ml[j].x);
-#pragma unroll
-                for (int j = 0; j < kPbJoin; ++j) {
-                    const float f = j < n ? __builtin_amdgcn_exp2f(ml[j].x - m) : 0.0f;
-                    l = __builtin_fmaf(ml[j].y, f, l);
-                    o.x = __builtin_fmaf(lo[j].x, f, o.x), o.y = __builtin_fmaf(lo[j].y, f, o.y);
-                    o.z = __builtin_fmaf(hi[j].x, f, o.z), o.w = __builtin_fmaf(hi[j].y, f, o.w);
-                }
-                if (done) finish(i, m, l, o);
-                else keep(slot_of(first), i, m, l, o);
             }
         }
     }
@@ -618,7 +630,7 @@ static int part_rows(const minikv_blk_shape &s, int32_t T)
 // [tickets][(m, l) of the parts' rows][their outputs]
 size_t prompt_blk_workspace_bytes(const minikv_blk_shape &s, int32_t T)
 {
-    return (size_t)2 * kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
+    return (size_t)kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
 }
 
 int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
@@ -629,7 +641,7 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
     a.table = table, a.q_len = q_len, a.cu = cu, a.out = (uint16_t *)out, a.lse = lse;
     a.R = s.R, a.T = T, a.Hq = s.Hq, a.Hkv = s.Hkv, a.rep = s.Hq / s.Hkv, a.n_blocks = s.n_blocks, a.width = s.max_blocks;
     a.shift = __builtin_ctz(s.block), a.c = sm_scale * kLog2e, a.part_rows = part_rows(s, T);
-    a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * 2 * kPbSlots), a.o = a.ml + (size_t)2 * kPbSlots * a.part_rows * 2;
+    a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * kPbSlots), a.o = a.ml + (size_t)kPbSlots * a.part_rows * 2;
     fast_div_setup((uint32_t)s.Hkv, a.hkv_magic, a.hkv_shift);
     fast_div_setup((uint32_t)a.rep, a.rep_magic, a.rep_shift);
     // row blocks: 128 rows each, and up to two for the rest of each request that has rows
