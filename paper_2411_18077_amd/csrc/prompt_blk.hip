@@ -17,6 +17,7 @@
 // workgroup of each eight to arrive, the results of eight of those by the last of them, and so on, always summed in the parts' order.
 #include "decode_common.h"
 #include "attn_tile.h"
+#include "scan.h"
 
 namespace minikv {
 
@@ -28,7 +29,7 @@ constexpr float kPbNone = -3.0e38f;                    // references before the 
 constexpr float kPbHead = 15.0f;                       // log2 of the largest weight
 constexpr float kPbRange = 60.0f;                      // V scales further below the largest one, as powers of two, count as 0
 constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens for a wide block, 1 for a narrow one
-constexpr int kPbLeast = 4;                            // least cost of a part of a walk
+constexpr int kPbLeastWide = 6, kPbLeastNarrow = 4;    // least tiles of a part of a walk
 constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
@@ -41,7 +42,7 @@ struct PromptBlkArgs {
     const int32_t *table, *q_len, *cu;
     uint16_t *out;
     float *lse;
-    int *tickets;                                      // [3][kPbSlots], of the first part of each eight, 64, 512
+    int *tickets;                                      // [3][2 * kPbSlots], of the first part of each eight, 64, 512
     float *ml, *o;                                     // [part][row] (m, l) and [part][row][128]
     int part_rows;
     float c;                                           // sm_scale * log2(e)
@@ -67,11 +68,24 @@ __device__ inline void pb_store(float *p, float a, float b)
 }
 __device__ inline float2 pb_pair(uint64_t v) { return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))}; }
 
-// The requests' rows in blocks, each block's walk in parts of at least the cost that there is for a slot (of workgroups at once): a block has
-// max(floor(cost / chunk), 1) parts, chunk = ceil(all blocks' cost / slots), so that those of two and more are not more than slots, and run at
-// once (with ceil(cost / chunk), 16 x 8 tokens behind 16384 had 568 parts for 512 slots: 123 us instead of 100).  They come first, then the blocks in
-// one part; of a request the narrow blocks, then the wide ones from the last on, whose walks are the longest.  Every workgroup counts all that for itself.
-__device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t *lds, PromptItem &it)
+// The requests' rows in blocks, each block's walk in cost / share parts, share = ceil(all blocks' cost / slots) (of workgroups at once): rounded up
+// if the items of more than half a share are then not more than slots, so that they run at once and the others fill what is left, else
+// down.  (Always up, 16 x 8 tokens behind 16384 have 568 parts for 512 slots: 123 us instead of 100; always down, a step of 24 uneven
+// requests 59 us instead of 49.)  Blocks in two or more parts, 2 * slots at most, come first, then those in one;
+// of a request the narrow blocks, then the wide ones from the last on, whose walks are the longest.  Every workgroup counts all that for itself.
+template <int CTRL, int ROWS> __device__ inline uint64_t add_dpp64(uint64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+    return v + ((uint64_t)hi << 32 | lo);
+}
+__device__ inline uint64_t wave_sum64(uint64_t v)
+{
+    v = add_dpp64<0x111, 0xf>(v), v = add_dpp64<0x112, 0xf>(v), v = add_dpp64<0x114, 0xf>(v), v = add_dpp64<0x118, 0xf>(v);       // row_shr 1, 2, 4, 8
+    v = add_dpp64<0x142, 0xa>(v), v = add_dpp64<0x143, 0xc>(v);                       // row_bcast 15, 31
+    return (uint64_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, 63);
+}
+
+__device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptItem &it)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (a.R + kPbThreads - 1) / kPbThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
@@ -93,61 +107,79 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, uint64_t 
     Request mine{0, 0, 0, 0, 0, 1};
     if (r0 < r1) mine = read(r0);
     auto request = [&](int r) { return r == r0 ? mine : read(r); };
-    uint32_t *sums = (uint32_t *)(lds + 1);            // [2][4] of the waves
-    PromptItem *found = (PromptItem *)(lds + 8);
-    if (tid == 0) lds[0] = 0, found->r = -1;
-    __syncthreads();
+    __shared__ uint64_t costs[kPbThreads / 64];        // of the waves
+    __shared__ uint32_t larges[kPbThreads / 64], sums[2][kPbThreads / 64];
+    __shared__ PromptItem found;
+    constexpr uint32_t kCap = 0x7fffffff;
+
     uint64_t all = 0;
     for (int r = r0; r < r1; ++r) {
         const Request q = request(r);
         all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles;
     }
-    if (all) atomicAdd((unsigned long long *)lds, (unsigned long long)all);
+    all = wave_sum64(all);
+    if (lane == 0) costs[wave] = all;
+    if (tid == 0) found.r = -1;
     __syncthreads();
-    all = lds[0] * a.Hkv;
-    const uint32_t chunk = max((uint32_t)((all + kPbSlots - 1) / kPbSlots), (uint32_t)kPbLeast);
-    auto parts_of = [&](uint32_t cost) { return min(max(cost / chunk, 1u), (uint32_t)kPbMost); };
-    uint32_t v[2] = {0, 0};                            // items of walks in two or more parts, and in one
+    all = (costs[0] + costs[1] + costs[2] + costs[3]) * a.Hkv;
+    const uint32_t share = (uint32_t)min((all + kPbSlots - 1) / kPbSlots, (uint64_t)1 << 26);          // (at most above any cost)
+    const uint32_t chunk[2] = {max(share, (uint32_t)kPbLeastNarrow), max(share, (uint32_t)kPbLeastWide * kPbWideCost)};
+    const float by[2] = {__builtin_amdgcn_rcpf((float)chunk[0]), __builtin_amdgcn_rcpf((float)chunk[1])};
+    // cost / chunk, rounded up or down, 1 to kPbMost.  (cost < 2^26; a quotient that is off by more than the one that is put right is beyond kPbMost)
+    auto parts_for = [&](const Request &q, int wide, bool up) {
+        const uint32_t cost = wide ? q.tiles * kPbWideCost : q.tiles, c = chunk[wide];
+        uint32_t p = (uint32_t)fminf((float)cost * by[wide], (float)kPbMost);
+        if (p * c > cost) --p;
+        if ((p + 1) * c <= cost) ++p;
+        if (up && p * c < cost) ++p;
+        return min(max(p, 1u), (uint32_t)kPbMost);
+    };
+    uint32_t large = 0;                                // items of more than half a share, rounded up
     for (int r = r0; r < r1; ++r) {
         const Request q = request(r);
-        const uint32_t w = parts_of(q.tiles * kPbWideCost), n = parts_of(q.tiles);
-        v[w == 1] += q.wide * w, v[n == 1] += q.narrow * n;
+        const uint32_t w = parts_for(q, 1, true), n = parts_for(q, 0, true);
+        if (q.tiles * kPbWideCost * 2 > chunk[1] * w) large += q.wide * w;
+        if (q.tiles * 2 > chunk[0] * n) large += q.narrow * n;
     }
-    const uint32_t items[2] = {v[0], v[1]};
+    large = wave_scan(large, kCap);
+    if (lane == 63) larges[wave] = large;
+    __syncthreads();
+    const bool up = (uint64_t)sat_add(sat_add(larges[0], larges[1], kCap), sat_add(larges[2], larges[3], kCap), kCap) * a.Hkv <= kPbSlots;
+    uint32_t items[2] = {0, 0}, v[2];                  // items of walks in two or more parts, and in one
+    for (int r = r0; r < r1; ++r) {
+        const Request q = request(r);
+        const uint32_t w = parts_for(q, 1, up), n = parts_for(q, 0, up);
+        items[w == 1] += q.wide * w, items[n == 1] += q.narrow * n;
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t u = __shfl_up(v[k], d, 64);
-            if (lane >= d) v[k] += u;
-        }
-        if (lane == 63) sums[k * 4 + wave] = v[k];
+        v[k] = wave_scan(items[k], kCap);
+        if (lane == 63) sums[k][wave] = v[k];
     }
     __syncthreads();
-    const uint32_t split = sums[0] + sums[1] + sums[2] + sums[3];
+    const uint32_t split = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
     const bool whole = idx >= split;                   // what is looked for
     uint32_t first = whole ? split + v[1] - items[1] : v[0] - items[0];
-    for (int w = 0; w < wave; ++w) first += sums[(whole ? 4 : 0) + w];
+    for (int w = 0; w < wave; ++w) first += sums[whole][w];
     if (idx >= first && idx - first < items[whole])
         for (int r = r0; r < r1; ++r) {
             const Request q = request(r);
-            const uint32_t w = parts_of(q.tiles * kPbWideCost), n = parts_of(q.tiles), at = idx - first;
+            const uint32_t w = parts_for(q, 1, up), n = parts_for(q, 0, up), at = idx - first;
             const uint32_t narrow = (n == 1) == whole ? q.narrow * n : 0, wide = (w == 1) == whole ? q.wide * w : 0;
             if (at < narrow + wide) {
                 const bool is_narrow = at < narrow;
                 const uint32_t p = is_narrow ? n : w, i = is_narrow ? at : at - narrow, k = i / p;
-                found->at = q.at, found->n = q.n, found->L = q.L, found->r = r;
-                found->narrow = is_narrow;
-                found->row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
-                found->part = (int)(i - k * p), found->parts = (int)p, found->chunk = (int)((q.tiles + p - 1) / p);
-                found->slot = (int)(idx - found->part);
+                found.at = q.at, found.n = q.n, found.L = q.L, found.r = r;
+                found.narrow = is_narrow;
+                found.row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
+                found.part = (int)(i - k * p), found.parts = (int)p, found.chunk = (int)((q.tiles + p - 1) / p);
+                found.slot = (int)(idx - found.part);
                 break;
             }
             first += narrow + wide;
         }
     __syncthreads();
-    it = *found;
-    __syncthreads();
+    it = found;
     int *p = (int *)&it;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(it) / sizeof(int)); ++i) p[i] = __builtin_amdgcn_readfirstlane(p[i]);
@@ -189,21 +221,27 @@ __device__ __forceinline__ void value_places(int (&v_place)[4])
     for (int db = 0; db < 4; ++db) v_place[db] = row * kPfD + (((4 * db + c0) ^ v_swizzle(row)) << 3) + (i & 1) * 4;
 }
 
-// A block's scales as the softmax takes them: ck takes a score to a power of two, lv = log2 Vs, add what is added (lv, or -inf where the block is
-// absent); `most`: the largest lv so far.  zero: its values count as 0.
+// Blocks' scales as the softmax takes them: ck takes a score to a power of two, lv = log2 Vs, add what is added (lv, or -inf where the block is
+// absent).
 struct BlockScale {
     float ck, lv, add;
-    bool zero;
 };
-__device__ __forceinline__ BlockScale block_scale(float ks, float vs, bool there, float c, float most)
+// Scales of NG blocks, block lane % NG in each lane (negative: absent).  none, zero: a bit for each block that is absent or whose values count as
+// 0; most: the largest lv so far.
+template <int NG>
+__device__ __forceinline__ void block_scales(float ks, float vs, float c, float &most, BlockScale (&b)[NG], uint32_t &none, uint32_t &zero)
 {
-    BlockScale b;
     const float l = vs > 0.0f ? log2_scale(vs) : kPbNone;
-    b.zero = !(l >= most - kPbRange) || !there;
-    b.lv = !b.zero ? l : most > -1.0e29f ? most : 0.0f;
-    b.add = there ? b.lv : -INFINITY;
-    b.ck = fmaxf(ks, 0x1p-126f) * c;                   // (not 0: a masked score is -inf)
-    return b;
+    float top = l;
+    if (NG >= 2) top = fmaxf(top, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(top), 0xb1, 0xf, 0xf, false)));        // quad_perm 1, 0, 3, 2
+    if (NG == 4) top = fmaxf(top, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(top), 0x4e, 0xf, 0xf, false)));        // quad_perm 2, 3, 0, 1
+    most = fmaxf(most, top);
+    const bool nil = !(l >= most - kPbRange);
+    none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1), zero = (uint32_t)__ballot(nil) & ((1u << NG) - 1);
+    const float lv = !nil ? l : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv, ck = fmaxf(ks, 0x1p-126f) * c;       // (ck not 0: a masked score is -inf)
+    auto of = [](float v, int k) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k)); };
+#pragma unroll
+    for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].lv = of(lv, k), b[k].add = of(add, k);
 }
 
 // Per lane: a row's references of the weights with and without Vs, the sum of those without (of this half's keys), and O^T:
@@ -286,64 +324,61 @@ struct Pages {
     const float *Ks, *Vs;
     const int32_t *table;                              // the request's row
     int entries, n_blocks, Hkv, kvh, shift, L;
-    __device__ __forceinline__ int id(int token) const { return __builtin_amdgcn_readfirstlane(table[min(token >> shift, entries - 1)]); }
+    __device__ __forceinline__ int id(int token) const { return table[min(token >> shift, entries - 1)]; }
     __device__ __forceinline__ bool there(int id) const { return (uint32_t)id < (uint32_t)n_blocks; }
     __device__ __forceinline__ int64_t head(int id) const { return (int64_t)(there(id) ? id : 0) * Hkv + kvh; }
 };
 
-// NG: blocks that a tile of 64 tokens may hold (4, 2, 1 of 16, 32, 64 and 128 tokens).
+// A tile of 64 tokens on its way: a thread has 16 channels of tokens tid / 8 and tid / 8 + 32.  NG: blocks that a tile may hold (4, 2, 1 of 16, 32,
+// 64 and 128 tokens).
+template <int NG> struct Tile {
+    u4b k[2], v[2];
+    float ks, vs;                                      // of block lane % NG
+    int id;                                            // the same; of the tile two further on, once this one's codes have been requested
+};
+
+// Tiles are requested two steps before they are in local memory: a step is about as long as a round trip to memory
 template <bool BF16, int NG>
 __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &pg, _Float16 *tiles, int t0, int t1, int wt1, int full, int last, const half8 (&qf)[8],
                                           RowState &st)
 {
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // tile loads: thread tid has 16 channels of tokens tid / 8 and tid / 8 + 32
-    const int key0 = tid >> 3, chunk = tid & 7, in_block = (1 << pg.shift) - 1;
-    int ids[NG];
-    float ks[NG], vs[NG];                              // of the tile whose codes are on the way (negative: absent)
-    u4b kraw[2], vraw[2];
-    auto load_ids = [&](int n) {
-#pragma unroll
-        for (int b = 0; b < NG; ++b) ids[b] = pg.id(n * 64 + b * (64 / NG));
-    };
-    // what belongs to the block of the thread's token j (the same for the whole wave)
-    auto of_token = [&](const auto &v, int j) { return NG == 4 ? (wave >> 1 ? v[(2 * j + 1) % NG] : v[2 * j % NG]) : v[j % NG]; };
-    auto load = [&](int n) {
+    const int key0 = tid >> 3, chunk = tid & 7, in_block = (1 << pg.shift) - 1, mine = lane % NG * (64 / NG);
+    auto granule = [&](int j) { return NG == 4 ? 2 * j + (wave >> 1) : NG == 2 ? j : 0; };       // of the thread's token j, the same for the whole wave
+    auto load = [&](Tile<NG> &x, int n) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int64_t off = ((pg.head(of_token(ids, j)) << pg.shift) + ((n * 64 + key0 + 32 * j) & in_block)) * kD + chunk * 16;
-            kraw[j] = *(const u4b *)(pg.K + off), vraw[j] = *(const u4b *)(pg.V + off);
+            const int id = __builtin_amdgcn_readlane(x.id, granule(j));
+            const int64_t off = ((pg.head(id) << pg.shift) + ((n * 64 + key0 + 32 * j) & in_block)) * kD + chunk * 16;
+            x.k[j] = *(const u4b *)(pg.K + off), x.v[j] = *(const u4b *)(pg.V + off);
         }
-#pragma unroll
-        for (int b = 0; b < NG; ++b) {
-            const int64_t at = pg.head(ids[b]);
-            const bool there = pg.there(ids[b]);
-            ks[b] = there ? pg.Ks[at] : -1.0f, vs[b] = there ? pg.Vs[at] : -1.0f;
-        }
+        const int64_t at = pg.head(x.id);
+        const float ks = pg.Ks[at], vs = pg.Vs[at];
+        x.ks = ks, x.vs = pg.there(x.id) ? vs : -1.0f;
+        if (n + 2 < t1) x.id = pg.id((n + 2) * 64 + mine);
     };
     BlockScale scale[NG];                              // of the tile in local memory
     float most = -1.0e30f;
-    auto store = [&](int n) {
-        bool none[NG], zero[NG];
-#pragma unroll
-        for (int b = 0; b < NG; ++b)
-            if (vs[b] > 0.0f) most = fmaxf(most, log2_scale(vs[b]));
-#pragma unroll
-        for (int b = 0; b < NG; ++b) scale[b] = block_scale(ks[b], vs[b], vs[b] >= 0.0f, a.c, most), none[b] = vs[b] < 0.0f, zero[b] = scale[b].zero;
+    auto store = [&](const Tile<NG> &x, int n) {
+        uint32_t none, zero;
+        block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
+        const bool plain = !zero && n * 64 + 64 <= pg.L;               // (absent ones are zero too)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = key0 + 32 * j;
-            const bool in = n * 64 + key < pg.L, no_key = of_token(none, j), no_value = of_token(zero, j);
-            u4b k = kraw[j], v = vraw[j], x[2];
+            u4b k = x.k[j], v = x.v[j], w[2];
+            if (!plain) {
+                const bool in = n * 64 + key < pg.L, no_key = none >> granule(j) & 1, no_value = zero >> granule(j) & 1;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = in && !no_key ? k[e] : 0, v[e] = in && !no_value ? v[e] : 0;
+                for (int e = 0; e < 4; ++e) k[e] = in && !no_key ? k[e] : 0, v[e] = in && !no_value ? v[e] : 0;
+            }
             _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile + key * kPfD, *Vt = Kt + kPfTile;
-            widen<BF16>(k, x);
+            widen<BF16>(k, w);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) *(u4b *)(Kt + (((2 * chunk + e) ^ (key & 15)) << 3)) = x[e];
-            widen<false>(v, x);
+            for (int e = 0; e < 2; ++e) *(u4b *)(Kt + (((2 * chunk + e) ^ (key & 15)) << 3)) = w[e];
+            widen<false>(v, w);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) *(u4b *)(Vt + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = x[e];
+            for (int e = 0; e < 2; ++e) *(u4b *)(Vt + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = w[e];
         }
     };
     int k_place[8], v_place[4];
@@ -351,16 +386,8 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
     for (int s = 0; s < 8; ++s) k_place[s] = tile_place(r, 2 * s + g);
     value_places(v_place);
 
-    load_ids(t0);
-    load(t0);
-    if (t0 + 1 < t1) load_ids(t0 + 1);
-    store(t0);
-    __syncthreads();
-    for (int n = t0; n < t1; ++n) {
-        if (n + 1 < t1) {
-            load(n + 1);
-            if (n + 2 < t1) load_ids(n + 2);
-        }
+    auto step = [&](Tile<NG> &x, const Tile<NG> &y, int n) {           // tile n; n + 2 into x, n + 1 from y
+        if (n + 2 < t1) load(x, n + 2);
         if (n < wt1) {
             const _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile, *Vt = Kt + kPfTile;
             float16v s[2];
@@ -383,16 +410,26 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
             softmax_step<2, NG>(s, scale, st, wb);
             add_values<4>(Vt, v_place, wb, st);
         }
-        if (n + 1 < t1) store(n + 1);
+        if (n + 1 < t1) store(y, n + 1);
         __syncthreads();
+    };
+    Tile<NG> x, y;
+    x.id = pg.id(t0 * 64 + mine), y.id = pg.id(min(t0 + 1, t1 - 1) * 64 + mine);
+    load(x, t0);
+    load(y, min(t0 + 1, t1 - 1));
+    store(x, t0);
+    __syncthreads();
+    for (int n = t0; n < t1; n += 2) {
+        step(x, y, n);
+        if (n + 1 < t1) step(y, x, n + 1);
     }
 }
 
 // A wave's 32 tokens on their way: a lane has channels 64 g .. 64 g + 63 of key r, and 16 channels of the values of tokens lane / 8 + 8 j
 template <int NG> struct Unit {
     u4b k[4], v[4];
-    float ks[NG], vs[NG];
-    int ids[NG];                                       // of the unit after it
+    float ks, vs;                                      // of block lane % NG
+    int id;                                            // the same; of the unit eight further on, once this one's codes have been requested
 };
 
 // Units of 32 tokens u0, u0 + 4, ... below u1.  qf: Q[row][64 g + 8 s ..], the channels in the order in which a lane has the keys'.  NG: 2 blocks of 16 tokens, or 1.
@@ -401,64 +438,59 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
                                             RowState &st)
 {
     const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5, key0 = lane >> 3, chunk = lane & 7, in_block = (1 << pg.shift) - 1;
+    const int mine = lane % NG * 16;
     int v_place[4];
     value_places(v_place);
     float most = -1.0e30f;
-    auto load_ids = [&](Unit<NG> &x, int u) {
-#pragma unroll
-        for (int b = 0; b < NG; ++b) x.ids[b] = pg.id(u * 32 + b * 16);
-    };
     auto load = [&](Unit<NG> &x, int u) {
-        const int of_key = NG == 1 ? x.ids[0] : r & 16 ? x.ids[NG - 1] : x.ids[0];
+        int ids[NG];
+#pragma unroll
+        for (int b = 0; b < NG; ++b) ids[b] = __builtin_amdgcn_readlane(x.id, b);
+        const int of_key = NG == 1 ? ids[0] : r & 16 ? ids[NG - 1] : ids[0];
         const uint8_t *K = pg.K + ((pg.head(of_key) << pg.shift) + ((u * 32 + r) & in_block)) * kD + 64 * g;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.k[j] = *(const u4b *)(K + 16 * j);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            x.v[j] = *(const u4b *)(pg.V + ((pg.head(x.ids[j * NG / 4]) << pg.shift) + ((u * 32 + key0 + 8 * j) & in_block)) * kD + chunk * 16);
-#pragma unroll
-        for (int b = 0; b < NG; ++b) {
-            const int64_t at = pg.head(x.ids[b]);
-            const bool there = pg.there(x.ids[b]);
-            x.ks[b] = there ? pg.Ks[at] : -1.0f, x.vs[b] = there ? pg.Vs[at] : -1.0f;
-        }
+            x.v[j] = *(const u4b *)(pg.V + ((pg.head(ids[j * NG / 4]) << pg.shift) + ((u * 32 + key0 + 8 * j) & in_block)) * kD + chunk * 16);
+        const int64_t at = pg.head(x.id);
+        const float ks = pg.Ks[at], vs = pg.Vs[at];
+        x.ks = ks, x.vs = pg.there(x.id) ? vs : -1.0f;
+        if (u + 8 < u1) x.id = pg.id((u + 8) * 32 + mine);
     };
     auto step = [&](Unit<NG> &x, int u) {
         BlockScale scale[NG];
-#pragma unroll
-        for (int b = 0; b < NG; ++b)
-            if (x.vs[b] > 0.0f) most = fmaxf(most, log2_scale(x.vs[b]));
-#pragma unroll
-        for (int b = 0; b < NG; ++b) scale[b] = block_scale(x.ks[b], x.vs[b], x.vs[b] >= 0.0f, a.c, most);
+        uint32_t none, zero;
+        block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
+        const bool plain = !zero && u * 32 + 32 <= pg.L;               // (absent ones are zero too)
         float16v s[1];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
-        const bool tail = u * 32 + 32 > pg.L;
-        const bool no_key = (tail && u * 32 + r >= pg.L) || (NG == 1 ? x.vs[0] < 0.0f : r & 16 ? x.vs[NG - 1] < 0.0f : x.vs[0] < 0.0f);
+        if (!plain) {
+            const bool no_key = u * 32 + r >= pg.L || (none >> (NG == 1 ? 0 : r >> 4) & 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool no_value = u * 32 + key0 + 8 * j >= pg.L || (zero >> (j * NG / 4) & 1);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x.k[j][e] = no_key ? 0 : x.k[j][e], x.v[j][e] = no_value ? 0 : x.v[j][e];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            u4b k = x.k[j], w[2];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = no_key ? 0 : k[e];
-            widen<BF16>(k, w);
+            u4b w[2];
+            widen<BF16>(x.k[j], w);
             s[0] = mfma32<BF16>(__builtin_bit_cast(half8, w[0]), qf[2 * j], s[0]);
             s[0] = mfma32<BF16>(__builtin_bit_cast(half8, w[1]), qf[2 * j + 1], s[0]);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int key = key0 + 8 * j;
-            const bool no_value = (tail && u * 32 + key >= pg.L) || scale[j * NG / 4].zero;
-            u4b v = x.v[j], w[2];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = no_value ? 0 : v[e];
-            widen<false>(v, w);
+            u4b w[2];
+            widen<false>(x.v[j], w);
 #pragma unroll
             for (int e = 0; e < 2; ++e) *(u4b *)(Vt + key * kPfD + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = w[e];
         }
-        if (u + 8 < u1) {                              // what was in the registers has been taken
-            load(x, u + 8);
-            if (u + 16 < u1) load_ids(x, u + 16);
-        }
+        if (u + 8 < u1) load(x, u + 8);                // (what was in the registers has been taken)
         if (u >= full) {
             const int rel = last - u * 32 - 4 * g;
 #pragma unroll
@@ -470,16 +502,10 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
         add_values<2>(Vt, v_place, wb, st);
     };
     Unit<NG> x, y;
-    if (u0 < u1) load_ids(x, u0);
-    if (u0 + 4 < u1) load_ids(y, u0 + 4);
-    if (u0 < u1) {
-        load(x, u0);
-        if (u0 + 8 < u1) load_ids(x, u0 + 8);
-    }
-    if (u0 + 4 < u1) {
-        load(y, u0 + 4);
-        if (u0 + 12 < u1) load_ids(y, u0 + 12);
-    }
+    if (u0 < u1) x.id = pg.id(u0 * 32 + mine);
+    if (u0 + 4 < u1) y.id = pg.id((u0 + 4) * 32 + mine);
+    if (u0 < u1) load(x, u0);
+    if (u0 + 4 < u1) load(y, u0 + 4);
     for (int u = u0; u < u1; u += 8) {
         step(x, u);
         if (u + 4 < u1) step(y, u + 4);
@@ -497,7 +523,7 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
     const uint32_t idx = fast_div(blockIdx.x, a.hkv_magic, a.hkv_shift);
     const int kvh = (int)(blockIdx.x - idx * a.Hkv);                   // (neighbours on a die walk through the same head)
     PromptItem it;
-    if (!find_item(a, idx, (uint64_t *)tiles, it)) return;
+    if (!find_item(a, idx, it)) return;
 
     const int M = it.n * a.rep, rows = min(M - it.row0, it.narrow ? kPbNarrow : kPbRows), base = it.L - it.n;        // rows of the block; token of the first new one
     auto query_of = [&](int row) { return (int)fast_div(row, a.rep_magic, a.rep_shift); };
@@ -581,40 +607,56 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
         __syncthreads();
         if (n > 1) {
             if (tid == 0) {
-                int *t = a.tickets + level * kPbSlots + slot_of(first);
+                int *t = a.tickets + level * 2 * kPbSlots + slot_of(first);
                 ticket = __hip_atomic_fetch_add(t, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 if (ticket == n - 1) __hip_atomic_store(t, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // ready for the next call
             }
             __syncthreads();
             if (ticket != n - 1) return;
             const bool done = step * kPbJoin >= parts;
-            for (int i0 = tid >> 5; i0 < rows; i0 += 16) {             // two rows a round trip
-                float2 ml[2][kPbJoin], lo[2][kPbJoin], hi[2][kPbJoin];
+            // each row's references and sums first, a factor for each of its results, then four rows a round trip
+            float *factor = (float *)tiles;            // [row][kPbJoin], then m and l
+            float2 *sums = (float2 *)(factor + kPbRows * kPbJoin);
+            if (tid < rows) {
+                float2 ml[kPbJoin];
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int j = 0; j < kPbJoin; ++j) ml[j] = pb_pair(pb_load(a.ml + ((int64_t)slot_of(first + min(j, n - 1) * step) * a.part_rows + tid) * 2));
+                float m = kPbNone, l = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < kPbJoin; ++j) {
-                        const int64_t at = (int64_t)slot_of(first + min(j, n - 1) * step) * a.part_rows + min(i0 + 8 * e, rows - 1);
-                        ml[e][j] = pb_pair(pb_load(a.ml + at * 2)), lo[e][j] = pb_pair(pb_load(a.o + at * kD + quad * 4));
-                        hi[e][j] = pb_pair(pb_load(a.o + at * kD + quad * 4 + 2));
-                    }
+                for (int j = 0; j < kPbJoin; ++j) m = fmaxf(m, ml[j].x);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int j = 0; j < kPbJoin; ++j) {
+                    const float f = j < n ? __builtin_amdgcn_exp2f(ml[j].x - m) : 0.0f;
+                    factor[tid * kPbJoin + j] = f, l = __builtin_fmaf(ml[j].y, f, l);
+                }
+                sums[tid] = float2{m, l};
+            }
+            __syncthreads();
+            for (int i0 = tid >> 5; i0 < rows; i0 += 32) {
+                float2 lo[4][kPbJoin], hi[4][kPbJoin];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i0 + 8 * e < rows)
+#pragma unroll
+                        for (int j = 0; j < kPbJoin; ++j)
+                            if (j < n) {
+                                const float *o = a.o + ((int64_t)slot_of(first + j * step) * a.part_rows + i0 + 8 * e) * kD + quad * 4;
+                                lo[e][j] = pb_pair(pb_load(o)), hi[e][j] = pb_pair(pb_load(o + 2));
+                            }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
                     const int i = i0 + 8 * e;
-                    float m = kPbNone, l = 0.0f;
+                    if (i >= rows) break;
                     float4 o = float4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int j = 0; j < kPbJoin; ++j) m = fmaxf(m, ml[e][j].x);
-#pragma unroll
                     for (int j = 0; j < kPbJoin; ++j) {
-                        const float f = j < n ? __builtin_amdgcn_exp2f(ml[e][j].x - m) : 0.0f;
-                        l = __builtin_fmaf(ml[e][j].y, f, l);
+                        if (j >= n) break;
+                        const float f = factor[i * kPbJoin + j];
                         o.x = __builtin_fmaf(lo[e][j].x, f, o.x), o.y = __builtin_fmaf(lo[e][j].y, f, o.y);
                         o.z = __builtin_fmaf(hi[e][j].x, f, o.z), o.w = __builtin_fmaf(hi[e][j].y, f, o.w);
                     }
-                    if (i >= rows) break;
-                    if (done) finish(i, m, l, o);
-                    else keep(slot_of(first), i, m, l, o);
+                    if (done) finish(i, sums[i].x, sums[i].y, o);
+                    else keep(slot_of(first), i, sums[i].x, sums[i].y, o);
                 }
             }
         }
@@ -630,7 +672,7 @@ static int part_rows(const minikv_blk_shape &s, int32_t T)
 // [tickets][(m, l) of the parts' rows][their outputs]
 size_t prompt_blk_workspace_bytes(const minikv_blk_shape &s, int32_t T)
 {
-    return (size_t)kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
+    return (size_t)2 * kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
 }
 
 int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache &c, const int32_t *table,
@@ -641,7 +683,7 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
     a.table = table, a.q_len = q_len, a.cu = cu, a.out = (uint16_t *)out, a.lse = lse;
     a.R = s.R, a.T = T, a.Hq = s.Hq, a.Hkv = s.Hkv, a.rep = s.Hq / s.Hkv, a.n_blocks = s.n_blocks, a.width = s.max_blocks;
     a.shift = __builtin_ctz(s.block), a.c = sm_scale * kLog2e, a.part_rows = part_rows(s, T);
-    a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * kPbSlots), a.o = a.ml + (size_t)kPbSlots * a.part_rows * 2;
+    a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * 2 * kPbSlots), a.o = a.ml + (size_t)2 * kPbSlots * a.part_rows * 2;
     fast_div_setup((uint32_t)s.Hkv, a.hkv_magic, a.hkv_shift);
     fast_div_setup((uint32_t)a.rep, a.rep_magic, a.rep_shift);
     // row blocks: 128 rows each, and up to two for the rest of each request that has rows

@@ -96,10 +96,10 @@ def test_prompt_attn_refuses_more_row_blocks_than_a_launch_counts(api):
 
 
 def test_prompt_workspace_covers_the_parts(api):
-    """512 parts of up to 128 rows: m, l and 128 sums each; fewer rows where T has fewer."""
+    """1024 parts of up to 128 rows: m, l and 128 sums each; fewer rows where T has fewer."""
     s = shape(api)
-    assert api.minikv_prompt_blk_workspace_bytes(s, 1000) >= 512 * 128 * 130 * 4
-    assert 512 * 4 * 130 * 4 <= api.minikv_prompt_blk_workspace_bytes(s, 1) < 512 * 8 * 130 * 4
+    assert api.minikv_prompt_blk_workspace_bytes(s, 1000) >= 1024 * 128 * 130 * 4
+    assert 1024 * 4 * 130 * 4 <= api.minikv_prompt_blk_workspace_bytes(s, 1) < 1024 * 8 * 130 * 4
     assert api.minikv_prompt_blk_workspace_bytes(s, -1) == 0
 
 
