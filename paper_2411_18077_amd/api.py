@@ -513,6 +513,16 @@ def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X
            "selective_flash_attn_packed")
 
 
+def _int_ptrs(home, names, tensors, sizes):
+    """Pointers of contiguous int32 tensors of at least these sizes (_need written out: one after the other they are half of a call)."""
+    i32 = torch.int32
+    for t, n in zip(tensors, sizes):
+        if t.dtype is not i32 or t.numel() < n or not t.is_contiguous() or t.get_device() != home:
+            for t, n, name in zip(tensors, sizes, names):
+                _need(t, i32, n, name, home)
+    return [t.data_ptr() for t in tensors]
+
+
 def minikv_prompt_blk_workspace_bytes(shape, T):
     return int(lib().minikv_prompt_blk_workspace_bytes(C.byref(shape), int(T)))
 
@@ -523,36 +533,42 @@ def _space(ws, home):
     return _here(ws, home, "workspace"), ws.numel() * ws.element_size()
 
 
+_PROMPT = ("table", "q_len", "cu")
+
+
 def minikv_prompt_attn_blk(shape, T, q, cache, table, q_len, cu, sm_scale, out, lse, workspace, stream=None):
     """q: [T][Hq][128], possibly a slice of a fused projection; out: contiguous; lse: [T][Hq] or None.  cu and q_len are kv_assign_blk's cu
     and q_len_next, behind kv_quantize_blk."""
     home, st = _home(stream)
-    (qs, p), (ws, n) = _rows(q, shape.dtype, shape.Hq, "q", home), _space(workspace, home)
+    R, Hq = shape.R, shape.Hq
+    (qs, p), (ws, n) = _rows(q, shape.dtype, Hq, "q", home), _space(workspace, home)
     if q.shape[0] < T:
         raise ValueError("q has %d rows, fewer than %d" % (q.shape[0], T))
-    _check(lib().minikv_prompt_attn_blk(C.byref(shape), int(T), p, qs, _fits(shape, cache, home),
-                                        _need(table, torch.int32, shape.R * shape.max_blocks, "table", home),
-                                        _need(q_len, torch.int32, shape.R, "q_len", home), _need(cu, torch.int32, shape.R + 1, "cu", home),
-                                        float(sm_scale), _need(out, q.dtype, T * shape.Hq * 128, "out", home),
-                                        None if lse is None else _need(lse, torch.float32, T * shape.Hq, "lse", home), ws, n, st),
+    _check(lib().minikv_prompt_attn_blk(C.byref(shape), T, p, qs, _fits(shape, cache, home),
+                                        *_int_ptrs(home, _PROMPT, (table, q_len, cu), (R * shape.max_blocks, R, R + 1)),
+                                        sm_scale, _need(out, q.dtype, T * Hq * 128, "out", home),
+                                        None if lse is None else _need(lse, torch.float32, T * Hq, "lse", home), ws, n, st),
            "minikv_prompt_attn_blk")
 
 
 def minikv_norm_rope(Hq, Hkv, T, Q, K, w_q, w_k, eps, inv_freq, rot_dim, adjacent, pos, Q_out, K_out, stream=None):
     """Q, Q_out: [T][Hq][128], K, K_out: [T][Hkv][128], possibly slices of a fused projection; Q_out and K_out may be Q and K.  w_q, w_k:
     [128] of the rows' type, or None; inv_freq: float32 [rot_dim / 2]."""
-    dtype, (home, st) = DTYPES.get(Q.dtype, -1), _home(stream)
-    (qs, q), (ks, k) = _rows(Q, dtype, Hq, "Q", home), _rows(K, dtype, Hkv, "K", home)
-    (qos, qo), (kos, ko) = _rows(Q_out, dtype, Hq, "Q_out", home), _rows(K_out, dtype, Hkv, "K_out", home)
-    if min(Q.shape[0], K.shape[0], Q_out.shape[0], K_out.shape[0]) < T:
-        raise ValueError("fewer than %d rows" % T)
+    dt, (home, st) = Q.dtype, _home(stream)
+    dtype, rows = DTYPES.get(dt, -1), []
+    for x, heads, name in ((Q, Hq, "Q"), (K, Hkv, "K"), (Q_out, Hq, "Q_out"), (K_out, Hkv, "K_out")):
+        (n, h, d), (t, side, one) = x.shape, x.stride()                # (_rows written out: four of them are half of the call)
+        if x.dtype is not dt or n < T or h != heads or d != 128 or one != 1 or (side != 128 and h > 1) or x.get_device() != home:
+            _rows(x, dtype, heads, name, home)
+            raise ValueError("%s: fewer than %d rows" % (name, T))
+        rows += (x.data_ptr(), t if n > 1 else heads * 128)
+    q, qs, k, ks, qo, qos, ko, kos = rows
     if T == 1:                                         # (one row has no stride of its own)
         qos, kos = qs if qo == q else qos, ks if ko == k else kos
-    _check(lib().minikv_norm_rope(int(Hq), int(Hkv), int(T), dtype, q, qs, k, ks,
-                                  None if w_q is None else _need(w_q, Q.dtype, 128, "w_q", home),
-                                  None if w_k is None else _need(w_k, Q.dtype, 128, "w_k", home), float(eps),
-                                  _need(inv_freq, torch.float32, rot_dim // 2, "inv_freq", home) if rot_dim else None, int(rot_dim),
-                                  int(bool(adjacent)), _need(pos, torch.int32, T, "pos", home), qo, qos, ko, kos, st), "minikv_norm_rope")
+    _check(lib().minikv_norm_rope(Hq, Hkv, T, dtype, q, qs, k, ks, None if w_q is None else _need(w_q, dt, 128, "w_q", home),
+                                  None if w_k is None else _need(w_k, dt, 128, "w_k", home), eps,
+                                  _need(inv_freq, torch.float32, rot_dim // 2, "inv_freq", home) if rot_dim else None, rot_dim,
+                                  1 if adjacent else 0, _need(pos, torch.int32, T, "pos", home), qo, qos, ko, kos, st), "minikv_norm_rope")
 
 
 class BlkCaches:
@@ -576,14 +592,18 @@ class BlkCaches:
         return len(self._t)
 
 
+_FORK = ("q_len", "parent", "n_keep", "table", "ring", "ring_state", "q_len_next", "table_next", "ring_state_next", "src", "dst")
+
+
 def kv_fork_blk(shape, q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst, stream=None):
-    i32, R, (home, st) = torch.int32, shape.R, _home(stream)
+    R, (home, st) = shape.R, _home(stream)
     rows = R * shape.max_blocks
-    p = [_need(t, i32, n, name, home) for t, n, name in (
-        (q_len, R, "q_len"), (parent, R, "parent"), (n_keep, R, "n_keep"), (table, rows, "table"), (ring, shape.n_blocks, "ring"),
-        (ring_state, 2, "ring_state"), (q_len_next, R, "q_len_next"), (table_next, rows, "table_next"), (ring_state_next, 2, "ring_state_next"),
-        (src, R, "src"), (dst, R, "dst"))]
-    _check(lib().kv_fork_blk(C.byref(shape), *p, st), "kv_fork_blk")
+    _check(lib().kv_fork_blk(C.byref(shape), *_int_ptrs(
+        home, _FORK, (q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst),
+        (R, R, R, rows, shape.n_blocks, 2, R, rows, 2, R, R)), st), "kv_fork_blk")
+
+
+_PAIRS = ("src", "dst")
 
 
 def kv_copy_blk(shape, caches, src, dst, stream=None):
@@ -594,29 +614,32 @@ def kv_copy_blk(shape, caches, src, dst, stream=None):
         raise ValueError("%d sources, %d destinations" % (n, dst.numel()))
     if own is not shape and (own.n_blocks < shape.n_blocks or own.Hkv != shape.Hkv or own.block != shape.block):
         raise ValueError("the caches are ones of %d blocks of %d tokens and %d heads" % (own.n_blocks, own.block, own.Hkv))
-    if len(caches):
-        _here(caches._t[0][0], home, "the caches")
-    _check(lib().kv_copy_blk(C.byref(shape), len(caches), caches._c, n, _need(src, torch.int32, n, "src", home),
-                             _need(dst, torch.int32, n, "dst", home), st), "kv_copy_blk")
+    layers = caches._t
+    if layers:
+        _here(layers[0][0], home, "the caches")
+    _check(lib().kv_copy_blk(C.byref(shape), len(layers), caches._c, n, *_int_ptrs(home, _PAIRS, (src, dst), (n, n)), st), "kv_copy_blk")
 
 
 def kv_free_workspace_bytes(shape):
     return int(lib().kv_free_workspace_bytes(C.byref(shape)))
 
 
+_FREE = ("q_len", "table", "ring", "ring_state")
+
+
 def kv_free_blk(shape, q_len, table, ring, ring_state, workspace, stream=None):
-    i32, (home, st) = torch.int32, _home(stream)
+    R, (home, st) = shape.R, _home(stream)
     ws, n = _space(workspace, home)
-    _check(lib().kv_free_blk(C.byref(shape), _need(q_len, i32, shape.R, "q_len", home), _need(table, i32, shape.R * shape.max_blocks, "table", home),
-                             _need(ring, i32, shape.n_blocks, "ring", home), _need(ring_state, i32, 2, "ring_state", home), ws, n, st),
-           "kv_free_blk")
+    _check(lib().kv_free_blk(C.byref(shape), *_int_ptrs(home, _FREE, (q_len, table, ring, ring_state),
+                                                        (R, R * shape.max_blocks, shape.n_blocks, 2)), ws, n, st), "kv_free_blk")
+
+
+_COMPACT = ("q_len", "table", "table_next", "ring", "ring_state", "src", "dst")
 
 
 def kv_compact_blk(shape, q_len, table, table_next, ring, ring_state, src, dst, workspace, stream=None):
     """At most src.numel() blocks move."""
-    i32, (home, st) = torch.int32, _home(stream)
-    (ws, n), pairs, rows = _space(workspace, home), src.numel(), shape.R * shape.max_blocks
-    _check(lib().kv_compact_blk(C.byref(shape), _need(q_len, i32, shape.R, "q_len", home), _need(table, i32, rows, "table", home),
-                                _need(table_next, i32, rows, "table_next", home), _need(ring, i32, shape.n_blocks, "ring", home),
-                                _need(ring_state, i32, 2, "ring_state", home), pairs, _need(src, i32, pairs, "src", home),
-                                _need(dst, i32, pairs, "dst", home), ws, n, st), "kv_compact_blk")
+    R, (home, st) = shape.R, _home(stream)
+    (ws, n), pairs, rows = _space(workspace, home), src.numel(), R * shape.max_blocks
+    p = _int_ptrs(home, _COMPACT, (q_len, table, table_next, ring, ring_state, src, dst), (R, rows, rows, shape.n_blocks, 2, pairs, pairs))
+    _check(lib().kv_compact_blk(C.byref(shape), *p[:5], pairs, p[5], p[6], ws, n, st), "kv_compact_blk")

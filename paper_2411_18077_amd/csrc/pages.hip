@@ -341,6 +341,61 @@ __global__ __launch_bounds__(256) void retable_blk_kernel(PoolArgs a)
     });
 }
 
+// The whole of it in one workgroup, with nothing but local memory between the steps, where tables and pool are small: what costs then are launches
+// and round trips to memory, one for lengths and table.
+constexpr int kPlSmall = 16384;                        // entries of all rows, and blocks
+
+__global__ __launch_bounds__(kScanThreads) void small_pool_blk_kernel(PoolArgs a)
+{
+    extern __shared__ int lds[];
+    __shared__ uint32_t part[1][kScanThreads / 64];
+    uint32_t *bits = (uint32_t *)lds, *below_of = bits + a.words, *count = bits + 2 * a.words, *to = count + a.rows.R;       // to: of each move
+    const int tid = threadIdx.x, entries = a.rows.R * a.rows.width;
+    uint32_t mine = 0;                                 // the thread's entries that count
+    for (int w = tid; w < a.words; w += kScanThreads) bits[w] = 0;
+    for (int r = tid; r < a.rows.R; r += kScanThreads) count[r] = blocks_of(clamped(a.q_len[r], a.rows.width, a.shift), a.shift);
+    constexpr int kMine = kPlSmall / kScanThreads;     // entries of a thread
+    int entry[kMine];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) entry[j] = tid + j * kScanThreads < entries ? a.table[tid + j * kScanThreads] : -1;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        const int i = tid + j * kScanThreads;
+        if (i >= entries) break;
+        const int r = (int)fast_div(i, a.rows.magic, a.rows.shift);                   // (by the width)
+        const bool counts = i - r * a.rows.width < (int)count[r], there = (uint32_t)entry[j] < (uint32_t)a.N;
+        mine |= (uint32_t)counts << j;
+        if (counts && there) atomicOr(&bits[entry[j] >> 5], 1u << (entry[j] & 31));
+    }
+    __syncthreads();
+    uint32_t n[1] = {tid < a.words ? (uint32_t)__builtin_popcount(bits[tid]) : 0}, total[1];            // (at most 512 words)
+    block_scan(n, {0x7fffffffu}, part, total);
+    if (tid < a.words) below_of[tid] = n[0];
+    __syncthreads();
+    const int used = (int)total[0];
+    auto below = [&](int b) { return (int)below_of[b >> 5] + __builtin_popcount(bits[b >> 5] & ((1u << (b & 31)) - 1)); };        // used blocks below b < N
+    const int moves = used < a.N ? min(used - below(used), a.n_pairs) : 0;
+    for (int b = tid; b < a.N; b += kScanThreads) {
+        const bool is_used = bits[b >> 5] >> (b & 31) & 1;
+        const int low = below(b), free_low = b - low, above = used - low - is_used;
+        const bool gone = is_used && above < moves, taken = !is_used && free_low < moves;
+        if (gone) a.src[above] = b;
+        if (taken) a.dst[free_low] = b, to[free_low] = b;
+        if (gone || (!is_used && !taken)) a.ring[free_low - min(moves, free_low) + moves - min(moves, used - low)] = b;      // (as in sweep_blk_kernel)
+    }
+    for (int k = tid + moves; k < a.n_pairs; k += kScanThreads) a.src[k] = a.dst[k] = -1;
+    if (tid == 0) a.state[0] = 0, a.state[1] = a.N - used;
+    if (!a.table_next) return;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kMine; ++j)
+        if (mine >> j & 1) {
+            const int above = (uint32_t)entry[j] < (uint32_t)a.N ? used - below(entry[j]) - 1 : moves;
+            a.table_next[tid + j * kScanThreads] = above < moves ? (int)to[above] : entry[j];
+        }
+}
+
 size_t pool_workspace_bytes(const minikv_blk_shape &s)
 {
     return 64 + ((size_t)s.n_blocks + 31) / 32 * 4 + (size_t)s.n_blocks * 4;
@@ -353,6 +408,12 @@ int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32
     a.q_len = q_len, a.table = table, a.table_next = table_next, a.ring = ring, a.state = state, a.src = src, a.dst = dst;
     a.rows = rows_of(s), a.N = s.n_blocks, a.words = (s.n_blocks + 31) / 32, a.shift = __builtin_ctz(s.block), a.n_pairs = n_pairs;
     a.header = (int *)workspace, a.bits = (uint32_t *)((char *)workspace + 64), a.rank = (int32_t *)(a.bits + a.words);
+    if ((int64_t)s.R * s.max_blocks <= kPlSmall && s.n_blocks <= kPlSmall) {
+        fast_div_setup((uint32_t)s.max_blocks, a.rows.magic, a.rows.shift);
+        const size_t lds = (size_t)(2 * a.words + s.R + (n_pairs < s.n_blocks / 2 ? n_pairs : s.n_blocks / 2)) * sizeof(uint32_t);
+        hipLaunchKernelGGL(small_pool_blk_kernel, dim3(1), dim3(kScanThreads), lds, st, a);
+        return hipGetLastError() == hipSuccess ? MINIKV_OK : MINIKV_ELAUNCH;
+    }
     const int64_t items = (int64_t)s.R * a.rows.segments, grid = (items + 3) / 4;
     const dim3 rows((unsigned)(grid < kComputeUnits * 8 ? grid : kComputeUnits * 8)), pool((unsigned)((s.n_blocks + kPlBlocks - 1) / kPlBlocks));
     hipLaunchKernelGGL(mark_blk_kernel, rows, dim3(256), 0, st, a);
