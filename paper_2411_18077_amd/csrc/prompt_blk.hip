@@ -29,7 +29,8 @@ constexpr float kPbNone = -3.0e38f;                    // references before the 
 constexpr float kPbHead = 15.0f;                       // log2 of the largest weight
 constexpr float kPbRange = 60.0f;                      // V scales further below the largest one, as powers of two, count as 0
 constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens for a wide block, 1 for a narrow one
-constexpr int kPbLeastWide = 6, kPbLeastNarrow = 4;    // least tiles of a part of a walk
+constexpr int kPbLeastWide = 6, kPbLeastNarrow = 2;    // least tiles of a part of a walk
+constexpr int kPbWholeNarrow = 6;                      // narrow walks of fewer tiles are not made in parts
 constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
@@ -132,6 +133,7 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
         if (p * c > cost) --p;
         if ((p + 1) * c <= cost) ++p;
         if (up && p * c < cost) ++p;
+        if (!wide && q.tiles < (uint32_t)kPbWholeNarrow) p = 1;
         return min(max(p, 1u), (uint32_t)kPbMost);
     };
     uint32_t large = 0;                                // items of more than half a share, rounded up
