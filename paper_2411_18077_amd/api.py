@@ -1,7 +1,8 @@
 """Thin Python binding of libminikv.so: argument marshalling only.
 
 Every function here has the name and the argument order of its C entry point in include/minikv.h and
-forwards device pointers of torch tensors (torch is used for device memory and streams, nothing else).
+forwards device pointers of torch tensors (torch is used for device memory and streams, nothing else).  Some go through _bind.so first,
+which does the same in compiled code.
 There is no CPU fallback: if the HIP library is missing, loading raises.
 """
 import ctypes as C
@@ -54,12 +55,12 @@ class MinikvError(RuntimeError):
         super().__init__("%s: %s (%d)" % (where, lib().minikv_strerror(status).decode(), status))
 
 
-_lib = None
+_lib = _bind = None
 
 
 def lib():
-    """Load libminikv.so (built in-tree by `python -m paper_2411_18077_amd.build`)."""
-    global _lib
+    """Load libminikv.so and _bind.so (built in-tree by `python -m paper_2411_18077_amd.build`)."""
+    global _lib, _bind
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError("libminikv.so is not built: run `python -m paper_2411_18077_amd.build` "
@@ -156,7 +157,11 @@ def lib():
         l.kv_select_hh_rw.argtypes = [C.c_int32, C.c_int32, C.c_int64, P, P, P, P, C.c_int64, P, P, C.c_size_t, P]
         l.kv_pyramid_budget.restype = C.c_int
         l.kv_pyramid_budget.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_int32, C.POINTER(C.c_double)]
-        _lib = l
+        try:
+            from . import _bind as bind
+        except ImportError as e:
+            raise ImportError("_bind.so is not built: run `python -m paper_2411_18077_amd.build`") from e
+        _lib, _bind = l, bind
     return _lib
 
 
@@ -513,6 +518,14 @@ def selective_flash_attn_packed(B, Hq, Hkv, T, max_len, Q, K, V, cu, sm_scale, X
            "selective_flash_attn_packed")
 
 
+def _quick(home):
+    """The compiled calls: each checks its arguments as the function here that uses it does and makes the call, or returns None
+    where one is not plainly right (or no GPU is in use), and has done nothing."""
+    if _lib is None:
+        lib()
+    return _bind if home is not None else None
+
+
 def _int_ptrs(home, names, tensors, sizes):
     """Pointers of contiguous int32 tensors of at least these sizes (_need written out: one after the other they are half of a call)."""
     i32 = torch.int32
@@ -540,6 +553,11 @@ def minikv_prompt_attn_blk(shape, T, q, cache, table, q_len, cu, sm_scale, out, 
     """q: [T][Hq][128], possibly a slice of a fused projection; out: contiguous; lse: [T][Hq] or None.  cu and q_len are kv_assign_blk's cu
     and q_len_next, behind kv_quantize_blk."""
     home, st = _home(stream)
+    quick = _quick(home)
+    if quick and cache.shape is shape:
+        rc = quick.prompt_attn_blk(home, st, C.addressof(shape), T, q, C.addressof(cache._c), cache._t[0], table, q_len, cu, sm_scale, out, lse, workspace)
+        if rc is not None:
+            return _check(rc, "minikv_prompt_attn_blk")
     R, Hq = shape.R, shape.Hq
     (qs, p), (ws, n) = _rows(q, shape.dtype, Hq, "q", home), _space(workspace, home)
     if q.shape[0] < T:
@@ -554,7 +572,13 @@ def minikv_prompt_attn_blk(shape, T, q, cache, table, q_len, cu, sm_scale, out, 
 def minikv_norm_rope(Hq, Hkv, T, Q, K, w_q, w_k, eps, inv_freq, rot_dim, adjacent, pos, Q_out, K_out, stream=None):
     """Q, Q_out: [T][Hq][128], K, K_out: [T][Hkv][128], possibly slices of a fused projection; Q_out and K_out may be Q and K.  w_q, w_k:
     [128] of the rows' type, or None; inv_freq: float32 [rot_dim / 2]."""
-    dt, (home, st) = Q.dtype, _home(stream)
+    home, st = _home(stream)
+    quick = _quick(home)
+    if quick:
+        rc = quick.norm_rope(home, st, Hq, Hkv, T, Q, K, w_q, w_k, eps, inv_freq, rot_dim, adjacent, pos, Q_out, K_out)
+        if rc is not None:
+            return _check(rc, "minikv_norm_rope")
+    dt = Q.dtype
     dtype, rows = DTYPES.get(dt, -1), []
     for x, heads, name in ((Q, Hq, "Q"), (K, Hkv, "K"), (Q_out, Hq, "Q_out"), (K_out, Hkv, "K_out")):
         (n, h, d), (t, side, one) = x.shape, x.stride()                # (_rows written out: four of them are half of the call)
@@ -596,7 +620,13 @@ _FORK = ("q_len", "parent", "n_keep", "table", "ring", "ring_state", "q_len_next
 
 
 def kv_fork_blk(shape, q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst, stream=None):
-    R, (home, st) = shape.R, _home(stream)
+    home, st = _home(stream)
+    quick = _quick(home)
+    if quick:
+        rc = quick.fork_blk(home, st, C.addressof(shape), q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst)
+        if rc is not None:
+            return _check(rc, "kv_fork_blk")
+    R = shape.R
     rows = R * shape.max_blocks
     _check(lib().kv_fork_blk(C.byref(shape), *_int_ptrs(
         home, _FORK, (q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst),
@@ -609,12 +639,16 @@ _PAIRS = ("src", "dst")
 def kv_copy_blk(shape, caches, src, dst, stream=None):
     """caches: BlkCaches; src, dst: a pair per element."""
     home, st = _home(stream)
-    own, n = caches.shape, src.numel()
+    own, layers, quick = caches.shape, caches._t, _quick(home)
+    if quick and own is shape and layers:
+        rc = quick.copy_blk(home, st, C.addressof(shape), len(layers), C.addressof(caches._c), layers[0][0], src, dst)
+        if rc is not None:
+            return _check(rc, "kv_copy_blk")
+    n = src.numel()
     if dst.numel() != n:
         raise ValueError("%d sources, %d destinations" % (n, dst.numel()))
     if own is not shape and (own.n_blocks < shape.n_blocks or own.Hkv != shape.Hkv or own.block != shape.block):
         raise ValueError("the caches are ones of %d blocks of %d tokens and %d heads" % (own.n_blocks, own.block, own.Hkv))
-    layers = caches._t
     if layers:
         _here(layers[0][0], home, "the caches")
     _check(lib().kv_copy_blk(C.byref(shape), len(layers), caches._c, n, *_int_ptrs(home, _PAIRS, (src, dst), (n, n)), st), "kv_copy_blk")
@@ -628,8 +662,13 @@ _FREE = ("q_len", "table", "ring", "ring_state")
 
 
 def kv_free_blk(shape, q_len, table, ring, ring_state, workspace, stream=None):
-    R, (home, st) = shape.R, _home(stream)
-    ws, n = _space(workspace, home)
+    home, st = _home(stream)
+    quick = _quick(home)
+    if quick:
+        rc = quick.free_blk(home, st, C.addressof(shape), q_len, table, ring, ring_state, workspace)
+        if rc is not None:
+            return _check(rc, "kv_free_blk")
+    R, (ws, n) = shape.R, _space(workspace, home)
     _check(lib().kv_free_blk(C.byref(shape), *_int_ptrs(home, _FREE, (q_len, table, ring, ring_state),
                                                         (R, R * shape.max_blocks, shape.n_blocks, 2)), ws, n, st), "kv_free_blk")
 
@@ -639,7 +678,13 @@ _COMPACT = ("q_len", "table", "table_next", "ring", "ring_state", "src", "dst")
 
 def kv_compact_blk(shape, q_len, table, table_next, ring, ring_state, src, dst, workspace, stream=None):
     """At most src.numel() blocks move."""
-    R, (home, st) = shape.R, _home(stream)
+    home, st = _home(stream)
+    quick = _quick(home)
+    if quick:
+        rc = quick.compact_blk(home, st, C.addressof(shape), q_len, table, table_next, ring, ring_state, src, dst, workspace)
+        if rc is not None:
+            return _check(rc, "kv_compact_blk")
+    R = shape.R
     (ws, n), pairs, rows = _space(workspace, home), src.numel(), R * shape.max_blocks
     p = _int_ptrs(home, _COMPACT, (q_len, table, table_next, ring, ring_state, src, dst), (R, rows, rows, shape.n_blocks, 2, pairs, pairs))
     _check(lib().kv_compact_blk(C.byref(shape), *p[:5], pairs, p[5], p[6], ws, n, st), "kv_compact_blk")

@@ -1,4 +1,4 @@
-"""Build libminikv.so (hand-written HIP for gfx950) in-tree with hipcc.
+"""Build libminikv.so (hand-written HIP for gfx950) and _bind.so (its binding's quick calls, host code) in-tree.
 
     python -m paper_2411_18077_amd.build          # compile every translation unit and link
 
@@ -7,6 +7,7 @@ hipcc cross-compiles without a GPU, so this runs anywhere the ROCm toolchain is 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -14,6 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libminikv.so")
+BIND = os.path.join(HERE, "_bind.so")                  # checks and passes on the arguments of the calls between two launches (host code)
 
 SOURCES = ["api.hip", "quantize.hip", "decode_scalar.hip", "decode_tiled.hip", "decode_static.hip", "select.hip",
            "prefill_attn.hip", "pt.hip", "blocks.hip", "decode_blk.hip", "prompt_blk.hip", "norm_rope.hip", "pages.hip"]
@@ -50,10 +52,26 @@ def _compile(src):
     return obj, warn
 
 
+def _compile_bind():
+    import torch
+    root = os.path.dirname(torch.__file__)
+    obj = os.path.join(OBJ, "bind.o")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError("g++ failed for bind.cpp:\n%s\n%s" % (r.stdout, r.stderr))
+    return ["g++", "-shared", obj, "-o", BIND, "-L" + HERE, "-lminikv", "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(root, "lib"), "-ltorch_python",
+            "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose=True):
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=4) as ex:
+        bind = ex.submit(_compile_bind)
         results = list(ex.map(_compile, SOURCES))
+        link_bind = bind.result()
     objs = [o for o, _ in results]
     for _, w in results:
         if w and verbose:
@@ -62,6 +80,9 @@ def build(verbose=True):
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
+    r = subprocess.run(link_bind, capture_output=True, text=True)
+    if r.returncode:
+        raise RuntimeError("link of _bind.so failed:\n%s\n%s" % (r.stdout, r.stderr))
     return LIB
 
 
