@@ -19,6 +19,8 @@
 #include "attn_tile.h"
 #include "scan.h"
 
+#include <type_traits>
+
 namespace minikv {
 
 constexpr int kPbNarrow = 32;                          // rows of a narrow block
@@ -347,21 +349,26 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int key0 = tid >> 3, chunk = tid & 7, in_block = (1 << pg.shift) - 1, mine = lane % NG * (64 / NG);
     auto granule = [&](int j) { return NG == 4 ? 2 * j + (wave >> 1) : NG == 2 ? j : 0; };       // of the thread's token j, the same for the whole wave
+    // (a token's place in its block, in a part of the tile's that is the same for all and one that does not change: addresses are a scalar and a register)
+    const unsigned lane_off = (unsigned)((NG == 4 ? key0 & 15 : key0) * kD + chunk * 16);
     auto load = [&](Tile<NG> &x, int n) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int id = __builtin_amdgcn_readlane(x.id, granule(j));
-            const int64_t off = ((pg.head(id) << pg.shift) + ((n * 64 + key0 + 32 * j) & in_block)) * kD + chunk * 16;
-            x.k[j] = *(const u4b *)(pg.K + off), x.v[j] = *(const u4b *)(pg.V + off);
+            const int id = __builtin_amdgcn_readlane(x.id, granule(j)), first = NG == 1 ? ((n * 64) & in_block) + 32 * j : 0;
+            const int64_t off = ((pg.head(id) << pg.shift) + first) * kD;
+            x.k[j] = *(const u4b *)(pg.K + off + lane_off), x.v[j] = *(const u4b *)(pg.V + off + lane_off);
         }
         const int64_t at = pg.head(x.id);
         const float ks = pg.Ks[at], vs = pg.Vs[at];
         x.ks = ks, x.vs = pg.there(x.id) ? vs : -1.0f;
         if (n + 2 < t1) x.id = pg.id((n + 2) * 64 + mine);
     };
+    int put_key[2], put_value[2];                      // where the thread's 16 bytes go in a tile (32 rows on: the same swizzle)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) put_key[e] = tile_place(key0, 2 * chunk + e), put_value[e] = key0 * kPfD + (((2 * chunk + e) ^ v_swizzle(key0)) << 3);
     BlockScale scale[NG];                              // of the tile in local memory
     float most = -1.0e30f;
-    auto store = [&](const Tile<NG> &x, int n) {
+    auto store = [&](const Tile<NG> &x, int n, auto odd) {             // (odd: which of the two buffers, known when compiling)
         uint32_t none, zero;
         block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
         const bool plain = !zero && n * 64 + 64 <= pg.L;               // (absent ones are zero too)
@@ -374,13 +381,13 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
 #pragma unroll
                 for (int e = 0; e < 4; ++e) k[e] = in && !no_key ? k[e] : 0, v[e] = in && !no_value ? v[e] : 0;
             }
-            _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile + key * kPfD, *Vt = Kt + kPfTile;
+            _Float16 *Kt = tiles + (decltype(odd)::value * 2 * kPfTile + 32 * j * kPfD), *Vt = Kt + kPfTile;
             widen<BF16>(k, w);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) *(u4b *)(Kt + (((2 * chunk + e) ^ (key & 15)) << 3)) = w[e];
+            for (int e = 0; e < 2; ++e) *(u4b *)(Kt + put_key[e]) = w[e];
             widen<false>(v, w);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) *(u4b *)(Vt + (((2 * chunk + e) ^ v_swizzle(key)) << 3)) = w[e];
+            for (int e = 0; e < 2; ++e) *(u4b *)(Vt + put_value[e]) = w[e];
         }
     };
     int k_place[8], v_place[4];
@@ -388,10 +395,10 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
     for (int s = 0; s < 8; ++s) k_place[s] = tile_place(r, 2 * s + g);
     value_places(v_place);
 
-    auto step = [&](Tile<NG> &x, const Tile<NG> &y, int n) {           // tile n; n + 2 into x, n + 1 from y
+    auto step = [&](Tile<NG> &x, const Tile<NG> &y, int n, auto odd, auto even) {         // tile n; n + 2 into x, n + 1 from y
         if (n + 2 < t1) load(x, n + 2);
         if (n < wt1) {
-            const _Float16 *Kt = tiles + (n & 1) * 2 * kPfTile, *Vt = Kt + kPfTile;
+            const _Float16 *Kt = tiles + decltype(odd)::value * 2 * kPfTile, *Vt = Kt + kPfTile;
             float16v s[2];
             half8 wb[4];
 #pragma unroll
@@ -412,18 +419,20 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
             softmax_step<2, NG>(s, scale, st, wb);
             add_values<4>(Vt, v_place, wb, st);
         }
-        if (n + 1 < t1) store(y, n + 1);
+        if (n + 1 < t1) store(y, n + 1, even);
         __syncthreads();
     };
+    const std::integral_constant<int, 0> first;
+    const std::integral_constant<int, 1> second;
     Tile<NG> x, y;
     x.id = pg.id(t0 * 64 + mine), y.id = pg.id(min(t0 + 1, t1 - 1) * 64 + mine);
     load(x, t0);
     load(y, min(t0 + 1, t1 - 1));
-    store(x, t0);
+    store(x, t0, first);
     __syncthreads();
     for (int n = t0; n < t1; n += 2) {
-        step(x, y, n);
-        if (n + 1 < t1) step(y, x, n + 1);
+        step(x, y, n, first, second);
+        if (n + 1 < t1) step(y, x, n + 1, second, first);
     }
 }
 
