@@ -34,6 +34,7 @@ constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens
 constexpr int kPbLeastWide = 6, kPbLeastNarrow = 2;    // least tiles of a part of a walk
 constexpr int kPbWholeNarrow = 6;                      // narrow walks of fewer tiles are not made in parts
 constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
+constexpr int kPbFine = kPbSlots;                      // most narrow blocks that are taken instead of wide ones
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
 
@@ -94,7 +95,13 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
     const int per = (a.R + kPbThreads - 1) / kPbThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
     struct Request {
         int at, n, L;
-        uint32_t wide, narrow, tiles;
+        uint32_t rows, wide, narrow, tiles;
+    };
+    bool fine = false;                                 // all blocks narrow
+    auto cut = [&](Request &q) {
+        const uint32_t rest = q.rows % kPbRows;
+        q.wide = fine ? 0 : q.rows / kPbRows + (rest > kPbTail);
+        q.narrow = fine ? (q.rows + kPbNarrow - 1) / kPbNarrow : rest > kPbTail ? 0 : (rest + kPbNarrow - 1) / kPbNarrow;
     };
     auto read = [&](int r) {
         Request q;
@@ -102,29 +109,34 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
         const int end = a.cu[r + 1];
         q.n = q.at >= 0 && end > q.at && end <= a.T ? end - q.at : 0;
         q.L = (int)min((int64_t)max(a.q_len[r], 0), (int64_t)a.width << a.shift);
-        const uint32_t M = (uint32_t)q.n * a.rep, rest = M % kPbRows;
-        q.wide = M / kPbRows + (rest > kPbTail), q.narrow = rest > kPbTail ? 0 : (rest + kPbNarrow - 1) / kPbNarrow;
+        q.rows = (uint32_t)q.n * a.rep;
         q.tiles = (uint32_t)max((q.L + 63) >> 6, 1);
+        cut(q);
         return q;
     };
-    Request mine{0, 0, 0, 0, 0, 1};
+    Request mine{0, 0, 0, 0, 0, 0, 1};
     if (r0 < r1) mine = read(r0);
     auto request = [&](int r) { return r == r0 ? mine : read(r); };
-    __shared__ uint64_t costs[kPbThreads / 64];        // of the waves
-    __shared__ uint32_t larges[kPbThreads / 64], sums[2][kPbThreads / 64];
+    __shared__ uint64_t costs[2][kPbThreads / 64];     // of the waves
+    __shared__ uint32_t larges[kPbThreads / 64], lots[kPbThreads / 64], sums[2][kPbThreads / 64];
     __shared__ PromptItem found;
     constexpr uint32_t kCap = 0x7fffffff;
 
-    uint64_t all = 0;
+    uint64_t all = 0, all_fine = 0;                    // the blocks' cost, with wide ones and without
+    uint32_t count = 0;                                // of the narrow ones without
     for (int r = r0; r < r1; ++r) {
         const Request q = request(r);
-        all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles;
+        const uint32_t n = (q.rows + kPbNarrow - 1) / kPbNarrow;
+        all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles, all_fine += (uint64_t)n * q.tiles, count = sat_add(count, n, kCap);
     }
-    all = wave_sum64(all);
-    if (lane == 0) costs[wave] = all;
+    all = wave_sum64(all), all_fine = wave_sum64(all_fine), count = wave_scan(count, kCap);
+    if (lane == 63) costs[0][wave] = all, costs[1][wave] = all_fine, larges[wave] = count;
     if (tid == 0) found.r = -1;
     __syncthreads();
-    all = (costs[0] + costs[1] + costs[2] + costs[3]) * a.Hkv;
+    count = sat_add(sat_add(larges[0], larges[1], kCap), sat_add(larges[2], larges[3], kCap), kCap);
+    fine = (uint64_t)count * a.Hkv <= kPbFine;
+    if (fine) cut(mine);
+    all = (costs[fine][0] + costs[fine][1] + costs[fine][2] + costs[fine][3]) * a.Hkv;
     const uint32_t share = (uint32_t)min((all + kPbSlots - 1) / kPbSlots, (uint64_t)1 << 26);          // (at most above any cost)
     const uint32_t chunk[2] = {max(share, (uint32_t)kPbLeastNarrow), max(share, (uint32_t)kPbLeastWide * kPbWideCost)};
     const float by[2] = {__builtin_amdgcn_rcpf((float)chunk[0]), __builtin_amdgcn_rcpf((float)chunk[1])};
@@ -146,9 +158,9 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
         if (q.tiles * 2 > chunk[0] * n) large += q.narrow * n;
     }
     large = wave_scan(large, kCap);
-    if (lane == 63) larges[wave] = large;
+    if (lane == 63) lots[wave] = large;
     __syncthreads();
-    const bool up = (uint64_t)sat_add(sat_add(larges[0], larges[1], kCap), sat_add(larges[2], larges[3], kCap), kCap) * a.Hkv <= kPbSlots;
+    const bool up = (uint64_t)sat_add(sat_add(lots[0], lots[1], kCap), sat_add(lots[2], lots[3], kCap), kCap) * a.Hkv <= kPbSlots;
     uint32_t items[2] = {0, 0}, v[2];                  // items of walks in two or more parts, and in one
     for (int r = r0; r < r1; ++r) {
         const Request q = request(r);
@@ -697,8 +709,17 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
     a.tickets = (int *)workspace, a.ml = (float *)(a.tickets + 3 * 2 * kPbSlots), a.o = a.ml + (size_t)2 * kPbSlots * a.part_rows * 2;
     fast_div_setup((uint32_t)s.Hkv, a.hkv_magic, a.hkv_shift);
     fast_div_setup((uint32_t)a.rep, a.rep_magic, a.rep_shift);
-    // row blocks: 128 rows each, and up to two for the rest of each request that has rows
-    const int64_t blocks = (int64_t)T * a.rep / kPbRows + 2 * (int64_t)(s.R < T ? s.R : T), items = blocks * s.Hkv + kPbSlots;
+    // The grid: the most items that find_item can count.  Row blocks: 128 rows each and up to two for the rest of each request that has rows, and never
+    // more than blocks of 32 rows would be; or those, kPbFine of them at most.  Parts: by the longest walk that the table has room for, and kPbSlots more
+    // than there are blocks.  (Workgroups without an item cost: a step of 3 requests of 75 tokens 8.4 us with 528 of them, 11.5 with 2560.)
+    const int64_t requests = s.R < T ? s.R : T, fine = (int64_t)T * a.rep / kPbNarrow + requests;
+    const int64_t coarse = (int64_t)T * a.rep / kPbRows + 2 * requests;
+    int64_t blocks = (coarse < fine ? coarse : fine) * s.Hkv;
+    const int64_t small = fine * s.Hkv < kPbFine ? fine * s.Hkv : kPbFine;
+    if (blocks < small) blocks = small;
+    const int64_t tiles = ((int64_t)s.max_blocks * s.block + 63) / 64;
+    const int64_t parts = tiles < kPbWholeNarrow ? 1 : (tiles + kPbLeastNarrow - 1) / kPbLeastNarrow;
+    const int64_t items = blocks * parts < blocks + kPbSlots ? blocks * parts : blocks + kPbSlots;
     if (items > 0x7fffff) return MINIKV_EINVAL;
     const dim3 grid((unsigned)items), threads(kPbThreads);
     const bool bf16 = s.dtype == MINIKV_BF16;

@@ -244,6 +244,24 @@ def test_pools(R, block):
             check_pool(q_len, table, N, block, n_pairs)
 
 
+@pytest.mark.parametrize("R,N,width", [(400, 17000, 30), (3, 16385, 40), (4200, 16384, 4), (64, 40003, 300), (2000, 65536, 9)])
+def test_pools_beyond_one_workgroup(R, N, width):
+    """More than 16384 blocks or entries."""
+    rng = random.Random(R + N)
+    q_len, table, _ = some_tables(rng, R, 16, N, width, absent=0.02)
+    ws = check_pool(q_len, table, N, 16, N // 2 + 1)
+    check_pool(q_len[::-1], table, N, 16, 7, ws)
+    check_pool([0] * R, table, N, 16, 0, ws)
+
+
+@pytest.mark.parametrize("R,N,width", [(1, 16384, 16384), (8192, 16384, 2), (4096, 500, 4)])
+def test_pools_at_the_border_of_one_workgroup(R, N, width):
+    rng = random.Random(R)
+    q_len, table, _ = some_tables(rng, R, 16, N, width, absent=0.02)
+    check_pool(q_len, table, N, 16, N // 2)
+    check_pool(q_len, table, N, 16, 3)
+
+
 def test_pools_of_one_and_of_none():
     check_pool([0], [[0]], 1, 16, 1)
     check_pool([16], [[0]], 1, 16, 1)

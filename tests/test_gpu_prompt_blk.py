@@ -74,6 +74,49 @@ def test_walks_in_parts(held, new, Hq, Hkv, dtype):
     Case(held, new, Hq, Hkv, 64, dtype, seed=3).run().check()
 
 
+# Blocks of 32 rows up to 512 of them in all, of 128 beyond: many heads make many.
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("block", [16, 32, 64, 128])
+@pytest.mark.parametrize("held,new,Hq,Hkv", [([0], [150], 128, 128), ([70], [130], 128, 128), ([5, 200], [100, 64], 128, 128), ([333, 0], [40, 90], 256, 128),
+                                             ([64], [200], 192, 64)])
+def test_wide_blocks(held, new, Hq, Hkv, block, dtype):
+    Case(held, new, Hq, Hkv, block, dtype, seed=Hq + block + sum(new)).run().check()
+
+
+@pytest.mark.parametrize("held,new", [([0], [2016]), ([0], [2048]), ([0], [2049]), ([1], [2080])])
+def test_blocks_next_to_the_border_of_512(held, new):
+    """63 and 64 blocks of 32 rows for each of 8 heads, 65 (513 and more: of 128 rows)."""
+    Case(held, new, 8, 8, 64, BF16, seed=30).run().check()
+
+
+@pytest.mark.parametrize("block,dtype", [(16, F16), (64, BF16), (32, BF16)])
+def test_wide_walks_in_parts(block, dtype):
+    """One long walk among many short ones."""
+    Case([6000] + [10] * 12, [130] + [64] * 12, 32, 32, block, dtype, seed=31).run().check()
+    Case([10] * 12 + [3000], [64] * 12 + [100], 64, 32, block, dtype, seed=32).run().check()
+
+
+def test_wide_blocks_in_the_corners():
+    """What the other tests look at, with blocks of 128 rows: more new rows than tokens, absent blocks, scales far apart, zero, of no power of two."""
+    c = Case([64, 40, 100], [100, 100, 100], 64, 64, 16, F16, seed=33, spread=6, gain=2.0 ** -6)
+    c.q_len[0], c.q_len[1] = 70, 3
+    c.Kc, c.Ks = rand_cache(c.N, 64, 16, 81)
+    c.Vs[c.table[0].long()[:3]] = 0.0
+    c.Vs[c.table[2, 4].long()] *= 0.77
+    c.Ks[c.table[2, 5].long()] *= 1.37
+    c.Ks[c.table[2, 6].long()] = 0.0
+    c.table[2, 1], c.table[2, 9] = -1, c.N
+    c.run().check(spread=80)
+
+
+@pytest.mark.parametrize("R", [256, 257, 700])
+def test_many_requests(R):
+    held, new = [(r * 37) % 90 for r in range(R)], [(r * 11) % 4 for r in range(R)]
+    Case(held, new, 2, 1, 16, F16, seed=R).run().check()
+    new[R // 2] = 150
+    Case(held, new, 2, 2, 32, BF16, seed=R).run().check()
+
+
 def test_rows_before_the_first_token():
     """More new rows than tokens: those in front see nothing."""
     c = Case([0, 40], [30, 20], 4, 2, 16, F16, seed=4)
