@@ -462,6 +462,7 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
 {
     const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5, key0 = lane >> 3, chunk = lane & 7, in_block = (1 << pg.shift) - 1;
     const int mine = lane % NG * 16;
+    const unsigned k_off = (NG == 1 ? r : r & 15) * kD + 64 * g, v_off = key0 * kD + chunk * 16;
     int v_place[4];
     value_places(v_place);
     float most = -1.0e30f;
@@ -469,13 +470,14 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
         int ids[NG];
 #pragma unroll
         for (int b = 0; b < NG; ++b) ids[b] = __builtin_amdgcn_readlane(x.id, b);
-        const int of_key = NG == 1 ? ids[0] : r & 16 ? ids[NG - 1] : ids[0];
-        const uint8_t *K = pg.K + ((pg.head(of_key) << pg.shift) + ((u * 32 + r) & in_block)) * kD + 64 * g;
+        int64_t base[NG];                              // of the blocks' rows, or of the 32 in a larger one
+#pragma unroll
+        for (int b = 0; b < NG; ++b) base[b] = ((pg.head(ids[b]) << pg.shift) + (NG == 1 ? (u * 32) & in_block : 0)) * kD;
+        const uint8_t *K = pg.K + (NG == 1 ? base[0] : r & 16 ? base[NG - 1] : base[0]) + k_off;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.k[j] = *(const u4b *)(K + 16 * j);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            x.v[j] = *(const u4b *)(pg.V + ((pg.head(ids[j * NG / 4]) << pg.shift) + ((u * 32 + key0 + 8 * j) & in_block)) * kD + chunk * 16);
+        for (int j = 0; j < 4; ++j) x.v[j] = *(const u4b *)(pg.V + base[j * NG / 4] + (NG == 1 ? 8 * j : 8 * (j & 1)) * kD + v_off);
         const int64_t at = pg.head(x.id);
         const float ks = pg.Ks[at], vs = pg.Vs[at];
         x.ks = ks, x.vs = pg.there(x.id) ? vs : -1.0f;
