@@ -35,6 +35,7 @@ constexpr int kPbLeastWide = 6, kPbLeastNarrow = 2;    // least tiles of a part 
 constexpr int kPbWholeNarrow = 6;                      // narrow walks of fewer tiles are not made in parts
 constexpr int kPbSlots = 2 * kComputeUnits;            // workgroups at once
 constexpr int kPbFine = kPbSlots;                      // most narrow blocks that are taken instead of wide ones
+constexpr int kPbStream = 16384;                       // cost of all blocks, in tiles of 16 KB, from which on caches do not hold them (256 MB beside the memory)
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
 
@@ -60,6 +61,7 @@ struct PromptItem {
     int row0, narrow;                                  // first row of the block, and its kind
     int part, parts, slot;                             // which part of the walk, of how many; part 0's place in the workspace, for parts > 1
     int chunk;                                         // tiles of a part
+    int stream;                                        // the call reads more than caches hold
 };
 
 __device__ inline uint64_t pb_load(const float *p)     // device scope: other dies wrote it in this launch
@@ -190,6 +192,7 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
                 found.row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
                 found.part = (int)(i - k * p), found.parts = (int)p, found.chunk = (int)((q.tiles + p - 1) / p);
                 found.slot = (int)(idx - found.part);
+                found.stream = all >= (uint64_t)kPbStream;
                 break;
             }
             first += narrow + wide;
@@ -455,8 +458,12 @@ template <int NG> struct Unit {
     int id;                                            // the same; of the unit eight further on, once this one's codes have been requested
 };
 
-// Units of 32 tokens u0, u0 + 4, ... below u1.  qf: Q[row][64 g + 8 s ..], the channels in the order in which a lane has the keys'.  NG: 2 blocks of 16 tokens, or 1.
-template <bool BF16, int NG>
+// Units of 32 tokens u0, u0 + 4, ... below u1.  qf: Q[row][64 g + 8 s ..], the channels in the order in which a lane has the keys'.  NG: 2 blocks of 16
+// tokens, or 1.  ALONE: no other block of the request reads the tokens, and the call reads more than caches hold: values are loaded with the streaming hint
+// (16 x 8 tokens behind 16384 98.4 -> 91.8 us, 64 x 4 behind one shared prefix of 8192 103 each; for 44 requests of up to 1841 tokens, which stay in
+// caches between calls, it would cost 17.7 -> 19.8, with six blocks a request 33.0 -> 34.3).  A row of keys takes four loads, which the hint would make
+// as many trips to memory (119 us).
+template <bool BF16, int NG, bool ALONE>
 __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages &pg, _Float16 *Vt, int u0, int u1, int full, int last, const half8 (&qf)[8],
                                             RowState &st)
 {
@@ -476,8 +483,9 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
         const uint8_t *K = pg.K + (NG == 1 ? base[0] : r & 16 ? base[NG - 1] : base[0]) + k_off;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.k[j] = *(const u4b *)(K + 16 * j);
+        auto values = [&](int j) { return (const u4b *)(pg.V + base[j * NG / 4] + (NG == 1 ? 8 * j : 8 * (j & 1)) * kD + v_off); };
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.v[j] = *(const u4b *)(pg.V + base[j * NG / 4] + (NG == 1 ? 8 * j : 8 * (j & 1)) * kD + v_off);
+        for (int j = 0; j < 4; ++j) x.v[j] = ALONE ? __builtin_nontemporal_load(values(j)) : *values(j);
         const int64_t at = pg.head(x.id);
         const float ks = pg.Ks[at], vs = pg.Vs[at];
         x.ks = ks, x.vs = pg.there(x.id) ? vs : -1.0f;
@@ -569,8 +577,10 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
     const Pages pg{a.K, a.V, a.Ks, a.Vs, a.table + (int64_t)it.r * a.width, (it.L + (1 << a.shift) - 1) >> a.shift, a.n_blocks, a.Hkv, kvh, a.shift, it.L};
     RowState st;
     st.clear();
-    if (it.narrow)
-        walk_narrow<BF16, NG == 4 ? 2 : 1>(a, pg, tiles + wave * kPfTile / 2, 2 * t0 + wave, 2 * t1, (low + 1) >> 5, last, qf, st);
+    if (it.narrow && it.stream && M <= kPbNarrow)
+        walk_narrow<BF16, NG == 4 ? 2 : 1, true>(a, pg, tiles + wave * kPfTile / 2, 2 * t0 + wave, 2 * t1, (low + 1) >> 5, last, qf, st);
+    else if (it.narrow)
+        walk_narrow<BF16, NG == 4 ? 2 : 1, false>(a, pg, tiles + wave * kPfTile / 2, 2 * t0 + wave, 2 * t1, (low + 1) >> 5, last, qf, st);
     else if (t0 < t1)
         walk_wide<BF16, NG>(a, pg, tiles, t0, t1, w0 < M ? min(t1, (high + 64) >> 6) : t0, (low + 1) >> 6, last, qf, st);
 

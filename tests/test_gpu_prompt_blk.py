@@ -109,6 +109,22 @@ def test_wide_blocks_in_the_corners():
     c.run().check(spread=80)
 
 
+@pytest.mark.parametrize("block,dtype", [(64, BF16), (32, F16), (16, F16)])
+def test_calls_that_read_more_than_caches_hold(block, dtype):
+    """64 requests behind one prefix of 2048 tokens, 8 KV heads: 16896 tiles of 64 tokens."""
+    R, Hkv, prefix = 64, 8, 2048 // block
+    new = [1 + r % 4 for r in range(R)]
+    c = Case([0], [4], 16, Hkv, block, dtype, seed=34)  # (its own tokens are replaced)
+    c.N, c.width = prefix + R, prefix + 1
+    (c.Kc, c.Ks), (c.Vc, c.Vs) = rand_cache(c.N, Hkv, block, 35), rand_cache(c.N, Hkv, block, 36)
+    c.table = torch.cat([torch.arange(prefix).expand(R, prefix), prefix + torch.arange(R)[:, None]], dim=1).int().contiguous()
+    c.q_len, c.cu, c.T = ints([2048 + n for n in new]), ints([sum(new[:r]) for r in range(R + 1)]), sum(new) + 1
+    c.q = torch.randn(c.T, 16, 128, generator=torch.Generator().manual_seed(37)).to(dtype)
+    c.q_dev = c.q.cuda()
+    c.shape = api.make_blk_shape(R, 16, Hkv, 128, block, c.N, c.width, dtype)
+    c.run().check()
+
+
 @pytest.mark.parametrize("R", [256, 257, 700])
 def test_many_requests(R):
     held, new = [(r * 37) % 90 for r in range(R)], [(r * 11) % 4 for r in range(R)]
