@@ -260,13 +260,20 @@ __global__ __launch_bounds__(256) void mark_blk_kernel(PoolArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     each_segment(a.rows, blockIdx.x * 4 + wave, gridDim.x * 4, [&](int r, int first) {
-        const int n = (int)blocks_of(clamped(a.q_len[r], a.rows.width, a.shift), a.shift);
         const int32_t *row = a.table + (int64_t)r * a.rows.width;
-#pragma unroll 4
-        for (int i = first + lane; i < min(n, first + kPgSegment); i += 64) {
-            const int b = row[i];
+        const int len = a.q_len[r], end = min(a.rows.width, first + kPgSegment);
+        auto mark = [&](int b) {
             if ((uint32_t)b < (uint32_t)a.N) atomicOr(&a.bits[b >> 5], 1u << (b & 31));
-        }
+        };
+        int b[4];                                      // (the first entries come with the length)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = first + lane + 64 * j < end ? row[first + lane + 64 * j] : -1;
+        const int n = min((int)blocks_of(clamped(len, a.rows.width, a.shift), a.shift), end);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (first + lane + 64 * j < n) mark(b[j]);
+#pragma unroll 4
+        for (int i = first + lane + 256; i < n; i += 64) mark(row[i]);
     });
 }
 
@@ -279,6 +286,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     __shared__ uint32_t part[2][kScanThreads / 64], here[kPlWords], below_of[kPlWords], last;
     const int tid = threadIdx.x, first = blockIdx.x * kPlWords;
     uint32_t sums[2] = {0, 0}, totals[2];
+    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.bits[first + tid] : 0;
     for (int w = tid; w < a.words; w += kScanThreads) {
         const uint32_t n = __builtin_popcount(a.bits[w]);
         sums[0] += n, sums[1] += w < first ? n : 0;
@@ -294,7 +302,6 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
         block_scan(n, {0x7fffffffu}, part, total);
         moves = min((int)total[0], a.n_pairs);
     }
-    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.bits[first + tid] : 0;
     uint32_t n[1] = {(uint32_t)__builtin_popcount(word)}, total[1];
     __syncthreads();
     block_scan(n, {0x7fffffffu}, part, total);
