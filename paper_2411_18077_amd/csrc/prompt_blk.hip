@@ -176,6 +176,7 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
     }
     __syncthreads();
     const uint32_t split = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    if ((uint64_t)split * a.Hkv > gridDim.x) return false;             // (cu that falls and rises: not all parts of a walk would come to their join)
     const bool whole = idx >= split;                   // what is looked for
     uint32_t first = whole ? split + v[1] - items[1] : v[0] - items[0];
     for (int w = 0; w < wave; ++w) first += sums[whole][w];

@@ -133,6 +133,13 @@ def test_many_requests(R):
     Case(held, new, 2, 2, 32, BF16, seed=R).run().check()
 
 
+@pytest.mark.parametrize("R,n", [(4097, 1), (8192, 1), (8191, 2)])
+def test_the_most_requests(R, n):
+    held, new = [(r * 7) % 30 for r in range(R)], [(r % 5 == 0) * n for r in range(R)]
+    new[R - 1], held[R - 1] = 40, 3000                 # (in parts)
+    Case(held, new, 2, 1, 64, BF16, seed=R).run().check()
+
+
 def test_rows_before_the_first_token():
     """More new rows than tokens: those in front see nothing."""
     c = Case([0, 40], [30, 20], 4, 2, 16, F16, seed=4)
@@ -154,6 +161,20 @@ def test_rows_out_of_range(cu):
     c = Case([50, 20, 30], [10, 10, 10], 4, 2, 16, F16, seed=6)
     c.cu = ints(cu)
     c.run().check()
+
+
+def test_rows_that_many_requests_claim():
+    """cu that falls and rises: more parts than the launch has workgroups.  What is written is nobody's business, but the workspace stays good."""
+    c = Case([3000] + [0] * 199, [1] + [0] * 199, 4, 2, 64, F16, seed=26)
+    c.run().check()
+    c.table[:] = c.table[0]
+    c.q_len[:], c.cu = 3001, ints([r % 2 for r in range(201)])
+    c.run(ws=c.ws)
+    again = Case([3000, 2000], [1, 3], 4, 2, 64, F16, seed=27)
+    ws = torch.zeros(max(c.ws.numel(), api.minikv_prompt_blk_workspace_bytes(again.shape, again.T)), dtype=torch.uint8, device="cuda")
+    c.run(ws=ws)
+    assert not ws[:3 * 1024 * 4].any()                 # (the tickets)
+    again.run(ws=ws).check()
 
 
 @pytest.mark.parametrize("block", [16, 32, 64])
