@@ -405,7 +405,7 @@ int kv_fork_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32
  * scales of all KV heads.  A pair with an index outside 0 .. n_blocks-1 is skipped (kv_fork_blk and kv_compact_blk fill theirs with -1).  A
  * block that is the destination of one pair must be neither end of another.
  *   caches    minikv_blk_cache [n_caches]                                        (HOST, read before the call returns; buffers written)
- *   src, dst  int32 [n_pairs]                                                    (device, read) */
+ *   src, dst  int32 [n_pairs], n_pairs <= 2^30                                   (device, read) */
 int kv_copy_blk(const minikv_blk_shape *shape, int32_t n_caches, const minikv_blk_cache *caches, int32_t n_pairs, const int32_t *src,
                 const int32_t *dst, void *stream);
 
@@ -416,8 +416,8 @@ int kv_copy_blk(const minikv_blk_shape *shape, int32_t n_caches, const minikv_bl
  *   q_len int32 [R], table int32 [R][max_blocks]                                 (device, read)
  *   ring int32 [n_blocks], ring_state int32 [2]; only the free blocks' entries   (device, written)
  *   workspace  device scratch of at least kv_free_workspace_bytes(shape) bytes, 16-byte aligned, ZERO-FILLED ONCE after allocation (every
- *              call leaves it ready for the next, of the same n_blocks; for another n_blocks zero it again).  Two calls that share one
- *              must be ordered (same stream). */
+ *              call leaves it ready for the next).  Calls of any shapes may take turns on one workspace of sufficient size; two calls
+ *              that share one must be ordered (same stream). */
 size_t kv_free_workspace_bytes(const minikv_blk_shape *shape);
 int kv_free_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *table, int32_t *ring, int32_t *ring_state,
                 void *workspace, size_t workspace_bytes, void *stream);
@@ -427,7 +427,7 @@ int kv_free_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32
  *   table_next   int32 [R][max_blocks]: the ceil(q_len[r] / block) first entries of each row, with the blocks' new places (entries
  *                outside the pool as they are)                                   (device, written; not table)
  *   ring, ring_state  the free blocks after the moves, as above                  (device, written)
- *   src, dst     int32 [n_pairs]: what moved and where to, -1 behind the last move (device, written)
+ *   src, dst     int32 [n_pairs]: what moved and where to, -1 behind the last move; n_pairs <= 2^30 (device, written)
  * kv_copy_blk has to move the contents, in every layer's cache, before table_next is used; ring's blocks may be handed out after that. */
 int kv_compact_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring,
                    int32_t *ring_state, int32_t n_pairs, int32_t *src, int32_t *dst, void *workspace, size_t workspace_bytes, void *stream);

@@ -636,6 +636,13 @@ def kv_fork_blk(shape, q_len, parent, n_keep, table, ring, ring_state, q_len_nex
 _PAIRS = ("src", "dst")
 
 
+def _pairs(src):
+    n = src.numel()
+    if n > 1 << 30:
+        raise ValueError("%d pairs, at most 2^30" % n)
+    return n
+
+
 def kv_copy_blk(shape, caches, src, dst, stream=None):
     """caches: BlkCaches; src, dst: a pair per element."""
     home, st = _home(stream)
@@ -644,7 +651,7 @@ def kv_copy_blk(shape, caches, src, dst, stream=None):
         rc = quick.copy_blk(home, st, C.addressof(shape), len(layers), C.addressof(caches._c), layers[0][0], src, dst)
         if rc is not None:
             return _check(rc, "kv_copy_blk")
-    n = src.numel()
+    n = _pairs(src)
     if dst.numel() != n:
         raise ValueError("%d sources, %d destinations" % (n, dst.numel()))
     if own is not shape and (own.n_blocks < shape.n_blocks or own.Hkv != shape.Hkv or own.block != shape.block):
@@ -685,6 +692,6 @@ def kv_compact_blk(shape, q_len, table, table_next, ring, ring_state, src, dst, 
         if rc is not None:
             return _check(rc, "kv_compact_blk")
     R = shape.R
-    (ws, n), pairs, rows = _space(workspace, home), src.numel(), R * shape.max_blocks
+    (ws, n), pairs, rows = _space(workspace, home), _pairs(src), R * shape.max_blocks
     p = _int_ptrs(home, _COMPACT, (q_len, table, table_next, ring, ring_state, src, dst), (R, rows, rows, shape.n_blocks, 2, pairs, pairs))
     _check(lib().kv_compact_blk(C.byref(shape), *p[:5], pairs, p[5], p[6], ws, n, st), "kv_compact_blk")

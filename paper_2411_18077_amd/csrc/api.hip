@@ -337,7 +337,7 @@ int kv_copy_blk(const minikv_blk_shape *s, int32_t n_caches, const minikv_blk_ca
 {
     const int rc = validate_blk(s);
     if (rc) return rc;
-    if (n_caches < 0 || n_pairs < 0 || (n_caches && !caches)) return MINIKV_EINVAL;
+    if (n_caches < 0 || n_pairs < 0 || n_pairs > kMaxPairs || (n_caches && !caches)) return MINIKV_EINVAL;
     for (int32_t i = 0; i < n_caches; ++i)
         if (!valid_blk_cache(caches + i)) return MINIKV_EINVAL;
     if (n_caches == 0 || n_pairs == 0) return MINIKV_OK;
@@ -367,7 +367,7 @@ int kv_compact_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_
     if (rc) return rc;
     if (!aligned4(q_len) || !aligned4(table) || !aligned4(table_next) || !aligned4(ring) || !aligned4(ring_state) || !aligned16(workspace))
         return MINIKV_EINVAL;
-    if (n_pairs < 0 || (n_pairs && (!aligned4(src) || !aligned4(dst) || src == dst)) || table_next == table) return MINIKV_EINVAL;
+    if (n_pairs < 0 || n_pairs > kMaxPairs || (n_pairs && (!aligned4(src) || !aligned4(dst) || src == dst)) || table_next == table) return MINIKV_EINVAL;
     if (workspace_bytes < pool_workspace_bytes(*s)) return MINIKV_EWORKSPACE;
     return launch_pool_blk(*s, q_len, table, table_next, ring, ring_state, n_pairs, src, dst, workspace, (hipStream_t)stream);
 }

@@ -99,6 +99,7 @@ bool aligned16(const void *p);
 
 // the paged 8-bit cache
 constexpr int kMaxRequests = 8192;   // a workgroup holds a few words per request in local memory
+constexpr int kMaxPairs = 1 << 30;    // of blocks in one call: loops over them count in 32 bits
 constexpr int kBlkTile = 64;         // tokens a wave of the attention takes at once
 constexpr int kBlkGroups = kComputeUnits;            // most workgroups of the attention
 constexpr int kBlkTickets = kBlkGroups * (1 + kMaxRep / 2);     // of units in several workgroups' parts: see decode_blk.hip

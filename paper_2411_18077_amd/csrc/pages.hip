@@ -241,14 +241,17 @@ int launch_copy_blk(const minikv_blk_shape &s, int32_t n_caches, const minikv_bl
 // =====================================================================================================================
 // kv_free_blk, kv_compact_blk
 
-// Workspace: a ticket and the number of moves, a bit for every block that a table names (zero between calls), and for every block that
-// moves its place among them.
+// Workspace: a ticket, the numbers of moves and of used blocks, and for 32 blocks each a PoolWord, at the same places for every shape.
+struct PoolWord {
+    uint32_t bits;                                     // the blocks that a table names (zero between calls)
+    uint32_t spare;
+    uint32_t kept, low;                                // for the new rows: bits, and how many used blocks lie below
+};
 struct PoolArgs {
     const int32_t *q_len, *table;
     int32_t *table_next, *ring, *state, *src, *dst;
-    int *header;                                       // ticket, moves
-    uint32_t *bits;
-    int32_t *rank;
+    int *header;                                       // ticket, moves, used blocks
+    PoolWord *marks;
     Rows rows;
     int N, words, shift, n_pairs;
 };
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(256) void mark_blk_kernel(PoolArgs a)
         const int32_t *row = a.table + (int64_t)r * a.rows.width;
         const int len = a.q_len[r], end = min(a.rows.width, first + kPgSegment);
         auto mark = [&](int b) {
-            if ((uint32_t)b < (uint32_t)a.N) atomicOr(&a.bits[b >> 5], 1u << (b & 31));
+            if ((uint32_t)b < (uint32_t)a.N) atomicOr(&a.marks[b >> 5].bits, 1u << (b & 31));
         };
         int b[4];                                      // (the first entries come with the length)
 #pragma unroll
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(256) void mark_blk_kernel(PoolArgs a)
     });
 }
 
-// A workgroup has 4096 blocks and counts for itself what lies below them (a bit a block: 7.5 KB for 60000 of them).  With U blocks used, the
+// A workgroup has 4096 blocks and counts for itself what lies below them (sixteen bytes for 32 of them: 30 KB for 60000).  With U blocks used, the
 // used ones from U on move, the highest first, each to the lowest block that is left: of a used block count those above, of a free one those
 // below, and it moves, or is moved into, if that is less than the number of moves.  The ring's place of a block follows from the same counts.
 // The last workgroup clears the bits for the next call.
@@ -286,9 +289,9 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     __shared__ uint32_t part[2][kScanThreads / 64], here[kPlWords], below_of[kPlWords], last;
     const int tid = threadIdx.x, first = blockIdx.x * kPlWords;
     uint32_t sums[2] = {0, 0}, totals[2];
-    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.bits[first + tid] : 0;
+    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.marks[first + tid].bits : 0;
     for (int w = tid; w < a.words; w += kScanThreads) {
-        const uint32_t n = __builtin_popcount(a.bits[w]);
+        const uint32_t n = __builtin_popcount(a.marks[w].bits);
         sums[0] += n, sums[1] += w < first ? n : 0;
     }
     block_scan(sums, {0x7fffffffu, 0x7fffffffu}, part, totals);
@@ -297,7 +300,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     if (a.n_pairs) {
         uint32_t n[1] = {0}, total[1];
         for (int w = (used >> 5) + tid; w < a.words; w += kScanThreads)
-            n[0] += __builtin_popcount(a.bits[w] & (w == used >> 5 ? ~0u << (used & 31) : ~0u));
+            n[0] += __builtin_popcount(a.marks[w].bits & (w == used >> 5 ? ~0u << (used & 31) : ~0u));
         __syncthreads();
         block_scan(n, {0x7fffffffu}, part, total);
         moves = min((int)total[0], a.n_pairs);
@@ -306,6 +309,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     __syncthreads();
     block_scan(n, {0x7fffffffu}, part, total);
     if (tid < kPlWords) here[tid] = word, below_of[tid] = n[0];
+    if (a.table_next && tid < kPlWords && first + tid < a.words) a.marks[first + tid].kept = word, a.marks[first + tid].low = below + n[0];
     __syncthreads();
     if (tid == 0) last = atomicAdd(&a.header[0], 1) == (int)gridDim.x - 1;
 
@@ -318,16 +322,16 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
         const int low = below + (int)below_of[at >> 5] + __builtin_popcount(bits & ((1u << (at & 31)) - 1));      // used blocks below b
         const int free_low = b - low, above = used - low - is_used;
         const bool gone = is_used && above < moves, taken = !is_used && free_low < moves;
-        if (gone) a.src[above] = b, a.rank[b] = above;
+        if (gone) a.src[above] = b;
         if (taken) a.dst[free_low] = b;
         // free afterwards below b: the free ones that were not taken, and the moved ones
         if (gone || (!is_used && !taken)) a.ring[free_low - min(moves, free_low) + moves - min(moves, used - low)] = b;
     }
     for (int64_t k = (int64_t)blockIdx.x * kScanThreads + tid + moves; k < a.n_pairs; k += (int64_t)gridDim.x * kScanThreads) a.src[k] = a.dst[k] = -1;
-    if (blockIdx.x == 0 && tid == 0) a.state[0] = 0, a.state[1] = a.N - used, a.header[1] = moves;
+    if (blockIdx.x == 0 && tid == 0) a.state[0] = 0, a.state[1] = a.N - used, a.header[1] = moves, a.header[2] = used;
     __syncthreads();
     if (last) {                                        // (everybody has read the bits)
-        for (int w = tid; w < a.words; w += kScanThreads) a.bits[w] = 0;
+        for (int w = tid; w < a.words; w += kScanThreads) a.marks[w].bits = 0;
         if (tid == 0) a.header[0] = 0;
     }
 }
@@ -335,15 +339,19 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
 __global__ __launch_bounds__(256) void retable_blk_kernel(PoolArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int moves = a.header[1], lowest = moves ? a.src[moves - 1] : a.N;          // named blocks from there on have moved
+    const int moves = a.header[1], used = a.header[2], lowest = moves ? a.src[moves - 1] : a.N;          // named blocks from there on have moved
     each_segment(a.rows, blockIdx.x * 4 + wave, gridDim.x * 4, [&](int r, int first) {
         const int n = (int)blocks_of(clamped(a.q_len[r], a.rows.width, a.shift), a.shift);
         const int32_t *in = a.table + (int64_t)r * a.rows.width;
         int32_t *out = a.table_next + (int64_t)r * a.rows.width;
 #pragma unroll 4
         for (int i = first + lane; i < min(n, first + kPgSegment); i += 64) {
-            const int b = in[i];
-            out[i] = b >= lowest && b < a.N ? a.dst[a.rank[b]] : b;
+            int b = in[i];
+            if (b >= lowest && b < a.N) {
+                const PoolWord &w = a.marks[b >> 5];
+                b = a.dst[used - 1 - (int)(w.low + __builtin_popcount(w.kept & ((1u << (b & 31)) - 1)))];       // (by the used blocks above it)
+            }
+            out[i] = b;
         }
     });
 }
@@ -405,7 +413,7 @@ __global__ __launch_bounds__(kScanThreads) void small_pool_blk_kernel(PoolArgs a
 
 size_t pool_workspace_bytes(const minikv_blk_shape &s)
 {
-    return 64 + ((size_t)s.n_blocks + 31) / 32 * 4 + (size_t)s.n_blocks * 4;
+    return 64 + ((size_t)s.n_blocks + 31) / 32 * sizeof(PoolWord);
 }
 
 int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring, int32_t *state,
@@ -414,7 +422,7 @@ int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32
     PoolArgs a;
     a.q_len = q_len, a.table = table, a.table_next = table_next, a.ring = ring, a.state = state, a.src = src, a.dst = dst;
     a.rows = rows_of(s), a.N = s.n_blocks, a.words = (s.n_blocks + 31) / 32, a.shift = __builtin_ctz(s.block), a.n_pairs = n_pairs;
-    a.header = (int *)workspace, a.bits = (uint32_t *)((char *)workspace + 64), a.rank = (int32_t *)(a.bits + a.words);
+    a.header = (int *)workspace, a.marks = (PoolWord *)((char *)workspace + 64);
     if ((int64_t)s.R * s.max_blocks <= kPlSmall && s.n_blocks <= kPlSmall) {
         fast_div_setup((uint32_t)s.max_blocks, a.rows.magic, a.rows.shift);
         const size_t lds = (size_t)(2 * a.words + s.R + (n_pairs < s.n_blocks / 2 ? n_pairs : s.n_blocks / 2)) * sizeof(uint32_t);

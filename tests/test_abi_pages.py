@@ -118,6 +118,7 @@ def test_copy_refuses(api):
     copy = lambda *a: call(api, "kv_copy_blk", [b, *a, None])  # noqa: E731
     assert copy(-1, c, 3, 0x1000, 0x2000) == -1 and copy(2, c, -1, 0x1000, 0x2000) == -1 and copy(2, None, 3, 0x1000, 0x2000) == -1
     assert copy(2, c, 3, None, 0x2000) == -1 and copy(2, c, 3, 0x1000, 0x2001) == -1 and copy(2, c, 3, 0x1000, 0x1000) == -1
+    assert copy(2, c, 2 ** 30 + 1, 0x1000, 0x2000) == -1 and copy(2, c, 2 ** 31 - 1, 0x1000, 0x2000) == -1
     assert copy(0, None, 3, None, None) == 0 and copy(2, c, 0, None, None) == 0
     c[1].Vs = None
     assert copy(2, c, 3, 0x1000, 0x2000) == -1
@@ -137,12 +138,12 @@ def test_compact_refuses(api, which):
     go = lambda q, n=3, size=1 << 40: call(api, "kv_compact_blk", [C.byref(shape(api)), *q[:5], n, *q[5:], size, None])  # noqa: E731
     for v in (None, 0x1002):
         assert go(p[:which] + [v] + p[which + 1:]) == -1
-    assert go(p, n=-1) == -1 and go(p, size=100) == -3
+    assert go(p, n=-1) == -1 and go(p, n=2 ** 30 + 1) == -1 and go(p, size=api.kv_free_workspace_bytes(shape(api)) - 1) == -3
     assert go(p[:2] + [p[1]] + p[3:]) == -1 and go(p[:6] + [p[5]] + p[7:]) == -1
 
 
 def test_free_workspace_grows_with_the_pool(api):
-    assert api.kv_free_workspace_bytes(shape(api, n_blocks=100000)) >= 100000 * 4 + 12500
+    assert api.kv_free_workspace_bytes(shape(api, n_blocks=100000)) >= 64 + 100000 // 32 * 16
 
 
 # ---------------------------------------------------------------------------------------------------------
@@ -170,6 +171,8 @@ def test_binding_refuses_types_sizes_and_places(api):
                   lambda: api.kv_compact_blk(s, z(4), z(4, 6), z(4, 6), z(40), z(2), z(5), z(5), z(100)),
                   lambda: api.kv_fork_blk(s, z(4), z(4), z(4), z(4, 6), z(40), z(2), z(4), z(4, 6), z(2), z(4), z(4)),
                   lambda: api.kv_copy_blk(s, api.BlkCaches(s, []), z(3), z(3)),
+                  lambda: api.kv_copy_blk(s, api.BlkCaches(s, []), z(1).expand(2 ** 32 + 3), z(1).expand(2 ** 32 + 3)),
+                  lambda: api.kv_compact_blk(s, z(4), z(4, 6), z(4, 6), z(40), z(2), z(1).expand(2 ** 32), z(1).expand(2 ** 32), z(64 + 2 * 16)),
                   lambda: api.kv_copy_blk(s, api.BlkCaches(s, []), z(3), z(4))):
         with pytest.raises(ValueError):
             call_()

@@ -106,6 +106,17 @@ def test_fork_long_rows():
     run_fork([5000 * 16 - 3, 1024 * 16, 1], [1, 0, 0], [10 ** 9, 10 ** 9, 3000 * 16 + 5], table, order[2 * width:], 16, N, head=N - 1)
 
 
+@pytest.mark.parametrize("R", [4096, 8191, 8192])
+def test_forks_of_the_most_requests(R):
+    rng = random.Random(R)
+    N = R * 3
+    q_len, table, free = some_tables(rng, R, 16, N, 3)
+    parent = [rng.choice([r, rng.randrange(R), R - 1, rng.randrange(3)]) for r in range(R)]
+    n_keep = [rng.choice([10 ** 9, rng.randint(0, 48)]) for _ in range(R)]
+    for some in (len(free), len(free) // 2):
+        run_fork(q_len, parent, n_keep, table, free[:some], 16, N, N - 2)
+
+
 def test_fork_captured():
     up = lambda v: ints(v).cuda()  # noqa: E731
     shape = pool_shape(3, 16, 12, 3)
@@ -229,8 +240,8 @@ def check_pool(q_len, table, N, block, n_pairs, ws=None):
     rest = [-1] * (n_pairs - len(moves))
     assert src.tolist() == [m[0] for m in moves] + rest and dst.tolist() == [m[1] for m in moves] + rest
     assert cut(new, rows) == rows and all(set(x) <= {77} for x in behind(new, rows))
-    bits = 64 + -(-N // 32) * 4
-    assert int(ws[:4].sum()) == 0 and int(ws[64:bits].sum()) == 0      # ready for the next call
+    words = ws[64:64 + -(-N // 32) * 16].view(torch.int32).view(-1, 4)
+    assert int(ws[:4].sum()) == 0 and not words[:, 0].any()            # ready for the next call
     return ws
 
 
@@ -289,6 +300,14 @@ def test_one_workspace_for_many_calls():
     for _ in range(12):
         q_len, table, _ = some_tables(rng, 20, 16, 333, 6)
         ws = check_pool(q_len, table, 333, 16, 40, ws)
+
+
+def test_one_workspace_for_pools_of_any_size():
+    rng = random.Random(5)
+    ws = torch.zeros(api.kv_free_workspace_bytes(pool_shape(1, 16, 70000, 1)), dtype=torch.uint8, device="cuda")
+    for N in (70000, 333, 20001, 16400, 40, 69999, 17000, 70000):
+        q_len, table, _ = some_tables(rng, 60, 16, N, 300)
+        check_pool(q_len, table, N, 16, N // 3, ws)
 
 
 def test_pool_captured():
