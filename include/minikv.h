@@ -347,8 +347,8 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  * A row without tokens (n > q_len[r], or all of them absent) gives zeros and -infinity.  Table entries outside 0 .. n_blocks-1 count as absent:
  * their tokens contribute nothing.  Lengths are clamped to 0 .. max_blocks * block; a request whose rows do not lie inside 0 .. T-1 is
  * left alone, as are the rows of no request.  What lies behind a request's last token in its last block is not used, whatever it holds.
- * Scales are finite, 0 or at least 2^-126.  The raw products q . codes and the sums of exp(score - largest score) times value are formed in
- * binary32 and must not overflow there.  Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is
+ * Scales are finite, 0 or at least 2^-126.  The raw products q . codes, the scores and the sums of exp(score - largest score) times value are
+ * formed in binary32 and must not overflow there, nor K's scales times 2 sm_scale.  Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is
  * below 2^-29 of the largest such product of the row by at most 2^-40 of that one.  Values of a block whose V scale is below 2^-60 of one in
  * front of it in the request's head may count as 0.
  *   T       rows of q, out and lse (a host-side bound of cu[R])
@@ -377,7 +377,8 @@ int minikv_prompt_attn_blk(const minikv_blk_shape *shape, int32_t T, const void 
  *   Q_out, K_out  as Q and K, tokens q_out_stride, k_out_stride elements apart; they may be Q and K themselves with the same strides, and
  *           must not overlap them otherwise                                      (device, written)
  * dtype a minikv_dtype; rot_dim a multiple of 16, 0 .. 128; eps finite and >= 0; strides as above, multiples of 8, at most 2^23;
- * T <= 2^25.  Squares are formed in binary32 and must not overflow there.  T == 0 is no error. */
+ * T <= 2^25.  Squares are formed in binary32 and must not overflow there; with eps == 0 a row of smaller ones than 2^-126 is not a number or
+ * infinite.  T == 0 is no error. */
 int minikv_norm_rope(int32_t Hq, int32_t Hkv, int32_t T, int32_t dtype, const void *Q, int64_t q_stride, const void *K, int64_t k_stride,
                      const void *w_q, const void *w_k, float eps, const float *inv_freq, int32_t rot_dim, int32_t adjacent,
                      const int32_t *pos, void *Q_out, int64_t q_out_stride, void *K_out, int64_t k_out_stride, void *stream);

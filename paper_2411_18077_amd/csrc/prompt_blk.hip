@@ -258,7 +258,7 @@ __device__ __forceinline__ void block_scales(float ks, float vs, float c, float 
     most = fmaxf(most, top);
     const bool nil = !(l >= most - kPbRange);
     none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1), zero = (uint32_t)__ballot(nil) & ((1u << NG) - 1);
-    const float lv = !nil ? l : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv, ck = fmaxf(ks, 0x1p-126f) * c;       // (ck not 0: a masked score is -inf)
+    const float lv = !nil ? l : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv, ck = fmaxf(ks * c, 0x1p-126f);       // (ck not 0: a masked score is -inf)
     auto of = [](float v, int k) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k)); };
 #pragma unroll
     for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].lv = of(lv, k), b[k].add = of(add, k);

@@ -220,6 +220,19 @@ def test_scales_of_zero_and_of_no_power_of_two(dtype):
     assert (c.out[20:24] == 0).all() and (c.lse[20:24].abs() < 100).all()
 
 
+@pytest.mark.parametrize("sm", [1e-45, 1e-30, 1e-6])
+@pytest.mark.parametrize("held,new", [([90, 40], [20, 33]), ([200, 0], [150, 170])])
+def test_small_factors_of_scores(held, new, sm):
+    """Scores of next to nothing, so that a row is the mean of what it sees: what it does not see stays out."""
+    c = Case(held, new, 16, 4, 16, BF16, seed=28)
+    b = c.table[0].long()
+    c.Ks[b[0]], c.Ks[b[5]], c.Ks[b[6]] = 0.0, 0.0, 2.0 ** -126
+    c.run()
+    c.out.fill_(7.0), c.lse.fill_(7.0)
+    api.minikv_prompt_attn_blk(*c.args[:7], sm, *c.args[8:])
+    check_prompt(c.shape, c.q, (c.Kc, c.Ks, c.Vc, c.Vs), c.table, c.q_len, c.cu, c.out, c.lse, sm=sm)
+
+
 def test_bf16_scales_at_the_ends_of_the_range():
     """V scales 2^200 apart: what lies 2^60 below may count as 0, weights do not change by it."""
     c = Case([64], [4], 2, 2, 16, BF16, seed=11)
