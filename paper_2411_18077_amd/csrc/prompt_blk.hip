@@ -38,6 +38,8 @@ constexpr int kPbFine = kPbSlots;                      // most narrow blocks tha
 constexpr int kPbStream = 16384;                       // cost of all blocks, in tiles of 16 KB, from which on caches do not hold them (256 MB beside the memory)
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
+constexpr int kPbGroups = 4;                           // of items, by the length of their walks
+constexpr uint32_t kPbCut = 1 << 22;                   // 2^8 threads and four groups: sums below 2^32
 
 struct PromptBlkArgs {
     const uint16_t *q;
@@ -77,7 +79,7 @@ __device__ inline float2 pb_pair(uint64_t v) { return float2{__uint_as_float((ui
 // The requests' rows in blocks, each block's walk in cost / share parts, share = ceil(all blocks' cost / slots) (of workgroups at once): rounded up
 // if the items of more than half a share are then not more than slots, so that they run at once and the others fill what is left, else
 // down.  (Always up, 16 x 8 tokens behind 16384 have 568 parts for 512 slots: 123 us instead of 100; always down, a step of 24 uneven
-// requests 59 us instead of 49.)  Blocks in two or more parts, 2 * slots at most, come first, then those in one;
+// requests 59 us instead of 49.)  Blocks in two or more parts, 2 * slots at most, come first, then those in one, long ones first;
 // of a request the narrow blocks, then the wide ones from the last on, whose walks are the longest.  Every workgroup counts all that for itself.
 template <int CTRL, int ROWS> __device__ inline uint64_t add_dpp64(uint64_t v)
 {
@@ -91,10 +93,23 @@ __device__ inline uint64_t wave_sum64(uint64_t v)
     return (uint64_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, 63);
 }
 
-__device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptItem &it)
+template <int CTRL, int ROWS> __device__ inline uint32_t add_dpp(uint32_t v)
+{
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Sum of the lanes up to this one.  (Not saturating, as that of scan.h: counts of a thread are cut to kPbCut, and no valid call has so many.)
+__device__ inline uint32_t wave_prefix(uint32_t v)
+{
+    v = add_dpp<0x111, 0xf>(v), v = add_dpp<0x112, 0xf>(v), v = add_dpp<0x114, 0xf>(v), v = add_dpp<0x118, 0xf>(v);
+    return add_dpp<0x143, 0xc>(add_dpp<0x142, 0xa>(v));
+}
+
+// WAVE: up to 64 requests, one a lane, and every wave finds for itself; else every thread has some in a row, and the workgroup meets between the steps.
+template <bool WAVE>
+__device__ inline bool find_item_in(const PromptBlkArgs &a, uint32_t idx, PromptItem &it)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (a.R + kPbThreads - 1) / kPbThreads, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+    const int per = WAVE ? 1 : (a.R + kPbThreads - 1) / kPbThreads, r0 = min(WAVE ? lane : tid * per, a.R), r1 = min(r0 + per, a.R);
     struct Request {
         int at, n, L;
         uint32_t rows, wide, narrow, tiles;
@@ -118,27 +133,42 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
     };
     Request mine{0, 0, 0, 0, 0, 0, 1};
     if (r0 < r1) mine = read(r0);
-    auto request = [&](int r) { return r == r0 ? mine : read(r); };
+    auto each = [&](auto take) {                       // until one takes the item
+        if constexpr (WAVE)
+            take(mine, r0);
+        else
+            for (int r = r0; r < r1; ++r)
+                if (take(r == r0 ? mine : read(r), r)) break;
+    };
     __shared__ uint64_t costs[2][kPbThreads / 64];     // of the waves
-    __shared__ uint32_t larges[kPbThreads / 64], lots[kPbThreads / 64], sums[2][kPbThreads / 64];
+    __shared__ uint32_t counts[2 + kPbGroups][kPbThreads / 64];
     __shared__ PromptItem found;
-    constexpr uint32_t kCap = 0x7fffffff;
+    // the workgroup's sum of the counts whose prefix v is, behind a barrier
+    auto total = [&](int k, uint32_t v) {
+        return WAVE ? (uint32_t)__builtin_amdgcn_readlane(v, 63) : counts[k][0] + counts[k][1] + counts[k][2] + counts[k][3];
+    };
+    auto meet = [&](int k, uint32_t v) {
+        if (!WAVE && lane == 63) counts[k][wave] = v;
+    };
 
     uint64_t all = 0, all_fine = 0;                    // the blocks' cost, with wide ones and without
     uint32_t count = 0;                                // of the narrow ones without
-    for (int r = r0; r < r1; ++r) {
-        const Request q = request(r);
+    each([&](const Request &q, int) {
         const uint32_t n = (q.rows + kPbNarrow - 1) / kPbNarrow;
-        all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles, all_fine += (uint64_t)n * q.tiles, count = sat_add(count, n, kCap);
+        all += (uint64_t)(q.wide * kPbWideCost + q.narrow) * q.tiles, all_fine += (uint64_t)n * q.tiles, count += n;
+        return false;
+    });
+    all = wave_sum64(all), all_fine = wave_sum64(all_fine), count = wave_prefix(min(count, kPbCut));
+    meet(0, count);
+    if constexpr (!WAVE) {
+        if (lane == 63) costs[0][wave] = all, costs[1][wave] = all_fine;
+        if (tid == 0) found.r = -1;
+        __syncthreads();
+        all = costs[0][0] + costs[0][1] + costs[0][2] + costs[0][3], all_fine = costs[1][0] + costs[1][1] + costs[1][2] + costs[1][3];
     }
-    all = wave_sum64(all), all_fine = wave_sum64(all_fine), count = wave_scan(count, kCap);
-    if (lane == 63) costs[0][wave] = all, costs[1][wave] = all_fine, larges[wave] = count;
-    if (tid == 0) found.r = -1;
-    __syncthreads();
-    count = sat_add(sat_add(larges[0], larges[1], kCap), sat_add(larges[2], larges[3], kCap), kCap);
-    fine = (uint64_t)count * a.Hkv <= kPbFine;
-    if (fine) cut(mine);
-    all = (costs[fine][0] + costs[fine][1] + costs[fine][2] + costs[fine][3]) * a.Hkv;
+    fine = (uint64_t)total(0, count) * a.Hkv <= kPbFine;
+    if (fine) cut(mine), all = all_fine;
+    all *= a.Hkv;
     const uint32_t share = (uint32_t)min((all + kPbSlots - 1) / kPbSlots, (uint64_t)1 << 26);          // (at most above any cost)
     const uint32_t chunk[2] = {max(share, (uint32_t)kPbLeastNarrow), max(share, (uint32_t)kPbLeastWide * kPbWideCost)};
     const float by[2] = {__builtin_amdgcn_rcpf((float)chunk[0]), __builtin_amdgcn_rcpf((float)chunk[1])};
@@ -153,57 +183,77 @@ __device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptIte
         return min(max(p, 1u), (uint32_t)kPbMost);
     };
     uint32_t large = 0;                                // items of more than half a share, rounded up
-    for (int r = r0; r < r1; ++r) {
-        const Request q = request(r);
+    each([&](const Request &q, int) {
         const uint32_t w = parts_for(q, 1, true), n = parts_for(q, 0, true);
         if (q.tiles * kPbWideCost * 2 > chunk[1] * w) large += q.wide * w;
         if (q.tiles * 2 > chunk[0] * n) large += q.narrow * n;
-    }
-    large = wave_scan(large, kCap);
-    if (lane == 63) lots[wave] = large;
-    __syncthreads();
-    const bool up = (uint64_t)sat_add(sat_add(lots[0], lots[1], kCap), sat_add(lots[2], lots[3], kCap), kCap) * a.Hkv <= kPbSlots;
-    uint32_t items[2] = {0, 0}, v[2];                  // items of walks in two or more parts, and in one
-    for (int r = r0; r < r1; ++r) {
-        const Request q = request(r);
+        return false;
+    });
+    large = wave_prefix(min(large, kPbCut));
+    meet(1, large);
+    if constexpr (!WAVE) __syncthreads();
+    const bool up = (uint64_t)total(1, large) * a.Hkv <= kPbSlots;
+    // Groups: of walks in two or more parts, and in one of more than half a share, a quarter, less.  (25 requests of 226 new tokens behind up to 482, 16
+    // heads, two groups: 54 us instead of 44.)
+    auto group_of = [&](uint32_t cost, uint32_t p) { return p > 1 ? 0 : cost * 2 > share ? 1 : cost * 4 > share ? 2 : 3; };
+    uint32_t items[kPbGroups] = {}, v[kPbGroups];
+    each([&](const Request &q, int) {
         const uint32_t w = parts_for(q, 1, up), n = parts_for(q, 0, up);
-        items[w == 1] += q.wide * w, items[n == 1] += q.narrow * n;
-    }
+        const int gw = group_of(q.tiles * kPbWideCost, w), gn = group_of(q.tiles, n);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        v[k] = wave_scan(items[k], kCap);
-        if (lane == 63) sums[k][wave] = v[k];
+        for (int k = 0; k < kPbGroups; ++k) items[k] += (gw == k ? q.wide * w : 0) + (gn == k ? q.narrow * n : 0);
+        return false;
+    });
+#pragma unroll
+    for (int k = 0; k < kPbGroups; ++k) items[k] = min(items[k], kPbCut), v[k] = wave_prefix(items[k]), meet(2 + k, v[k]);
+    if constexpr (!WAVE) __syncthreads();
+    if ((uint64_t)total(2, v[0]) * a.Hkv > gridDim.x) return false;    // (cu that falls and rises: not all parts of a walk would come to their join)
+    int group = 0;                                     // what is looked for, and where the thread's own begin
+    uint32_t start = 0, own = items[0], before = v[0] - items[0];
+#pragma unroll
+    for (int k = 1; k < kPbGroups; ++k) {
+        const uint32_t next = start + total(1 + k, v[k - 1]);
+        if (group == k - 1 && idx >= next) start = next, group = k, own = items[k], before = v[k] - items[k];
     }
-    __syncthreads();
-    const uint32_t split = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    if ((uint64_t)split * a.Hkv > gridDim.x) return false;             // (cu that falls and rises: not all parts of a walk would come to their join)
-    const bool whole = idx >= split;                   // what is looked for
-    uint32_t first = whole ? split + v[1] - items[1] : v[0] - items[0];
-    for (int w = 0; w < wave; ++w) first += sums[whole][w];
-    if (idx >= first && idx - first < items[whole])
-        for (int r = r0; r < r1; ++r) {
-            const Request q = request(r);
+    uint32_t first = start + before;
+    if (!WAVE)
+        for (int w = 0; w < wave; ++w) first += counts[2 + group][w];
+    PromptItem got;
+    got.r = -1;
+    if (idx >= first && idx - first < own)
+        each([&](const Request &q, int r) {
             const uint32_t w = parts_for(q, 1, up), n = parts_for(q, 0, up), at = idx - first;
-            const uint32_t narrow = (n == 1) == whole ? q.narrow * n : 0, wide = (w == 1) == whole ? q.wide * w : 0;
-            if (at < narrow + wide) {
-                const bool is_narrow = at < narrow;
-                const uint32_t p = is_narrow ? n : w, i = is_narrow ? at : at - narrow, k = i / p;
-                found.at = q.at, found.n = q.n, found.L = q.L, found.r = r;
-                found.narrow = is_narrow;
-                found.row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
-                found.part = (int)(i - k * p), found.parts = (int)p, found.chunk = (int)((q.tiles + p - 1) / p);
-                found.slot = (int)(idx - found.part);
-                found.stream = all >= (uint64_t)kPbStream;
-                break;
-            }
+            const uint32_t narrow = group_of(q.tiles, n) == group ? q.narrow * n : 0, wide = group_of(q.tiles * kPbWideCost, w) == group ? q.wide * w : 0;
             first += narrow + wide;
-        }
-    __syncthreads();
-    it = found;
+            if (at >= narrow + wide) return false;
+            const bool is_narrow = at < narrow;
+            const uint32_t p = is_narrow ? n : w, i = is_narrow ? at : at - narrow, k = i / p;
+            got.at = q.at, got.n = q.n, got.L = q.L, got.r = r;
+            got.narrow = is_narrow;
+            got.row0 = (int)(is_narrow ? q.wide * kPbRows + k * kPbNarrow : (q.wide - 1 - k) * kPbRows);
+            got.part = (int)(i - k * p), got.parts = (int)p, got.chunk = (int)((q.tiles + p - 1) / p);
+            got.slot = (int)(idx - got.part);
+            got.stream = all >= (uint64_t)kPbStream;
+            return true;
+        });
+    int src = 0;                                       // the lane that has it
+    if constexpr (WAVE) {
+        const uint64_t who = __ballot(got.r >= 0);
+        if (!who) return false;
+        it = got, src = __builtin_ctzll(who);
+    } else {
+        if (got.r >= 0) found = got;
+        __syncthreads();
+        it = found;
+    }
     int *p = (int *)&it;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(it) / sizeof(int)); ++i) p[i] = __builtin_amdgcn_readfirstlane(p[i]);
+    for (int i = 0; i < (int)(sizeof(it) / sizeof(int)); ++i) p[i] = __builtin_amdgcn_readlane(p[i], src);
     return it.r >= 0;
+}
+__device__ inline bool find_item(const PromptBlkArgs &a, uint32_t idx, PromptItem &it)
+{
+    return a.R <= 64 ? find_item_in<true>(a, idx, it) : find_item_in<false>(a, idx, it);
 }
 
 typedef _Float16 half2p __attribute__((ext_vector_type(2)));

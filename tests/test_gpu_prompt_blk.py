@@ -133,6 +133,13 @@ def test_many_requests(R):
     Case(held, new, 2, 2, 32, BF16, seed=R).run().check()
 
 
+@pytest.mark.parametrize("R", [63, 64, 65, 128])
+def test_requests_of_all_lengths(R):
+    """Walks in parts, long and short ones in one, more of them than run at once."""
+    held, new = [(3000, 700, 90, 5, 0)[r % 5] + r for r in range(R)], [(40, 1, 130, 70, 9, 0, 260)[r % 7] for r in range(R)]
+    Case(held, new, 8, 4, 16, F16, seed=R).run().check()
+
+
 @pytest.mark.parametrize("R,n", [(4097, 1), (8192, 1), (8191, 2)])
 def test_the_most_requests(R, n):
     held, new = [(r * 7) % 30 for r in range(R)], [(r % 5 == 0) * n for r in range(R)]
