@@ -241,19 +241,21 @@ int launch_copy_blk(const minikv_blk_shape &s, int32_t n_caches, const minikv_bl
 // =====================================================================================================================
 // kv_free_blk, kv_compact_blk
 
-// Workspace: a ticket, the numbers of moves and of used blocks, and for 32 blocks each a PoolWord, at the same places for every shape.
-struct PoolWord {
-    uint32_t bits;                                     // the blocks that a table names (zero between calls)
-    uint32_t spare;
-    uint32_t kept, low;                                // for the new rows: bits, and how many used blocks lie below
+// Workspace: a ticket, the numbers of moves and of used blocks, and PoolWords for 1024 blocks each, at the same places for every shape.
+struct PoolWords {
+    uint32_t bits[32];                                 // the blocks that a table names (zero between calls)
+    uint2 kept[32];                                    // for the new rows: bits, and how many used blocks lie below them
 };
+constexpr int kPlHeader = 128;
 struct PoolArgs {
     const int32_t *q_len, *table;
     int32_t *table_next, *ring, *state, *src, *dst;
     int *header;                                       // ticket, moves, used blocks
-    PoolWord *marks;
+    PoolWords *marks;
     Rows rows;
     int N, words, shift, n_pairs;
+    __device__ uint32_t &bits(int w) const { return marks[w >> 5].bits[w & 31]; }
+    __device__ uint2 &kept(int w) const { return marks[w >> 5].kept[w & 31]; }
 };
 
 constexpr int kPlPer = 4;                              // blocks of a thread of the second launch
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(256) void mark_blk_kernel(PoolArgs a)
         const int32_t *row = a.table + (int64_t)r * a.rows.width;
         const int len = a.q_len[r], end = min(a.rows.width, first + kPgSegment);
         auto mark = [&](int b) {
-            if ((uint32_t)b < (uint32_t)a.N) atomicOr(&a.marks[b >> 5].bits, 1u << (b & 31));
+            if ((uint32_t)b < (uint32_t)a.N) atomicOr(&a.bits(b >> 5), 1u << (b & 31));
         };
         int b[4];                                      // (the first entries come with the length)
 #pragma unroll
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(256) void mark_blk_kernel(PoolArgs a)
     });
 }
 
-// A workgroup has 4096 blocks and counts for itself what lies below them (sixteen bytes for 32 of them: 30 KB for 60000).  With U blocks used, the
+// A workgroup has 4096 blocks and counts for itself what lies below them (a bit a block: 7.5 KB for 60000 of them).  With U blocks used, the
 // used ones from U on move, the highest first, each to the lowest block that is left: of a used block count those above, of a free one those
 // below, and it moves, or is moved into, if that is less than the number of moves.  The ring's place of a block follows from the same counts.
 // The last workgroup clears the bits for the next call.
@@ -289,9 +291,9 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     __shared__ uint32_t part[2][kScanThreads / 64], here[kPlWords], below_of[kPlWords], last;
     const int tid = threadIdx.x, first = blockIdx.x * kPlWords;
     uint32_t sums[2] = {0, 0}, totals[2];
-    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.marks[first + tid].bits : 0;
+    const uint32_t word = tid < kPlWords && first + tid < a.words ? a.bits(first + tid) : 0;
     for (int w = tid; w < a.words; w += kScanThreads) {
-        const uint32_t n = __builtin_popcount(a.marks[w].bits);
+        const uint32_t n = __builtin_popcount(a.bits(w));
         sums[0] += n, sums[1] += w < first ? n : 0;
     }
     block_scan(sums, {0x7fffffffu, 0x7fffffffu}, part, totals);
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     if (a.n_pairs) {
         uint32_t n[1] = {0}, total[1];
         for (int w = (used >> 5) + tid; w < a.words; w += kScanThreads)
-            n[0] += __builtin_popcount(a.marks[w].bits & (w == used >> 5 ? ~0u << (used & 31) : ~0u));
+            n[0] += __builtin_popcount(a.bits(w) & (w == used >> 5 ? ~0u << (used & 31) : ~0u));
         __syncthreads();
         block_scan(n, {0x7fffffffu}, part, total);
         moves = min((int)total[0], a.n_pairs);
@@ -309,7 +311,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     __syncthreads();
     block_scan(n, {0x7fffffffu}, part, total);
     if (tid < kPlWords) here[tid] = word, below_of[tid] = n[0];
-    if (a.table_next && tid < kPlWords && first + tid < a.words) a.marks[first + tid].kept = word, a.marks[first + tid].low = below + n[0];
+    if (a.table_next && tid < kPlWords && first + tid < a.words) a.kept(first + tid) = uint2{word, below + n[0]};
     __syncthreads();
     if (tid == 0) last = atomicAdd(&a.header[0], 1) == (int)gridDim.x - 1;
 
@@ -331,7 +333,7 @@ __global__ __launch_bounds__(kScanThreads) void sweep_blk_kernel(PoolArgs a)
     if (blockIdx.x == 0 && tid == 0) a.state[0] = 0, a.state[1] = a.N - used, a.header[1] = moves, a.header[2] = used;
     __syncthreads();
     if (last) {                                        // (everybody has read the bits)
-        for (int w = tid; w < a.words; w += kScanThreads) a.marks[w].bits = 0;
+        for (int w = tid; w < a.words; w += kScanThreads) a.bits(w) = 0;
         if (tid == 0) a.header[0] = 0;
     }
 }
@@ -348,8 +350,8 @@ __global__ __launch_bounds__(256) void retable_blk_kernel(PoolArgs a)
         for (int i = first + lane; i < min(n, first + kPgSegment); i += 64) {
             int b = in[i];
             if (b >= lowest && b < a.N) {
-                const PoolWord &w = a.marks[b >> 5];
-                b = a.dst[used - 1 - (int)(w.low + __builtin_popcount(w.kept & ((1u << (b & 31)) - 1)))];       // (by the used blocks above it)
+                const uint2 k = a.kept(b >> 5);
+                b = a.dst[used - 1 - (int)(k.y + __builtin_popcount(k.x & ((1u << (b & 31)) - 1)))];            // (by the used blocks above it)
             }
             out[i] = b;
         }
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(kScanThreads) void small_pool_blk_kernel(PoolArgs a
 
 size_t pool_workspace_bytes(const minikv_blk_shape &s)
 {
-    return 64 + ((size_t)s.n_blocks + 31) / 32 * sizeof(PoolWord);
+    return kPlHeader + ((size_t)s.n_blocks + 1023) / 1024 * sizeof(PoolWords);
 }
 
 int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32_t *table, int32_t *table_next, int32_t *ring, int32_t *state,
@@ -422,7 +424,7 @@ int launch_pool_blk(const minikv_blk_shape &s, const int32_t *q_len, const int32
     PoolArgs a;
     a.q_len = q_len, a.table = table, a.table_next = table_next, a.ring = ring, a.state = state, a.src = src, a.dst = dst;
     a.rows = rows_of(s), a.N = s.n_blocks, a.words = (s.n_blocks + 31) / 32, a.shift = __builtin_ctz(s.block), a.n_pairs = n_pairs;
-    a.header = (int *)workspace, a.marks = (PoolWord *)((char *)workspace + 64);
+    a.header = (int *)workspace, a.marks = (PoolWords *)((char *)workspace + kPlHeader);
     if ((int64_t)s.R * s.max_blocks <= kPlSmall && s.n_blocks <= kPlSmall) {
         fast_div_setup((uint32_t)s.max_blocks, a.rows.magic, a.rows.shift);
         const size_t lds = (size_t)(2 * a.words + s.R + (n_pairs < s.n_blocks / 2 ? n_pairs : s.n_blocks / 2)) * sizeof(uint32_t);

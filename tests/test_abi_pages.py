@@ -143,7 +143,7 @@ def test_compact_refuses(api, which):
 
 
 def test_free_workspace_grows_with_the_pool(api):
-    assert api.kv_free_workspace_bytes(shape(api, n_blocks=100000)) >= 64 + 100000 // 32 * 16
+    assert api.kv_free_workspace_bytes(shape(api, n_blocks=100000)) >= 128 + 100000 // 1024 * 384
 
 
 # ---------------------------------------------------------------------------------------------------------

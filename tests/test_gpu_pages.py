@@ -240,8 +240,8 @@ def check_pool(q_len, table, N, block, n_pairs, ws=None):
     rest = [-1] * (n_pairs - len(moves))
     assert src.tolist() == [m[0] for m in moves] + rest and dst.tolist() == [m[1] for m in moves] + rest
     assert cut(new, rows) == rows and all(set(x) <= {77} for x in behind(new, rows))
-    words = ws[64:64 + -(-N // 32) * 16].view(torch.int32).view(-1, 4)
-    assert int(ws[:4].sum()) == 0 and not words[:, 0].any()            # ready for the next call
+    words = ws[128:128 + -(-N // 1024) * 384].view(torch.int32).view(-1, 96)
+    assert int(ws[:4].sum()) == 0 and not words[:, :32].any()          # ready for the next call
     return ws
 
 
