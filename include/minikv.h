@@ -415,7 +415,7 @@ int kv_copy_blk(const minikv_blk_shape *shape, int32_t n_caches, const minikv_bl
  * does, so this ends requests that share blocks: set q_len[r] = 0, then call.  (A prefix that no request holds at the moment is kept
  * by a row of its own.)  Lengths are clamped, entries outside the pool name nothing.
  *   q_len int32 [R], table int32 [R][max_blocks]                                 (device, read)
- *   ring int32 [n_blocks], ring_state int32 [2]; only the free blocks' entries   (device, written)
+ *   ring int32 [n_blocks], ring_state int32 [2]; only the free blocks' entries   (device, written; nothing that is read)
  *   workspace  device scratch of at least kv_free_workspace_bytes(shape) bytes, 16-byte aligned, ZERO-FILLED ONCE after allocation (every
  *              call leaves it ready for the next).  Calls of any shapes may take turns on one workspace of sufficient size; two calls
  *              that share one must be ordered (same stream). */
@@ -426,7 +426,7 @@ int kv_free_blk(const minikv_blk_shape *shape, const int32_t *q_len, const int32
 /* kv_free_blk that also moves used blocks to the front of the pool, at most n_pairs of them: with U blocks used, those from U on move, the
  * highest one first, each to the lowest free block that no other one moves to.
  *   table_next   int32 [R][max_blocks]: the ceil(q_len[r] / block) first entries of each row, with the blocks' new places (entries
- *                outside the pool as they are)                                   (device, written; not table)
+ *                outside the pool as they are)                                   (device, written; nothing that is read)
  *   ring, ring_state  the free blocks after the moves, as above                  (device, written)
  *   src, dst     int32 [n_pairs]: what moved and where to, -1 behind the last move; n_pairs <= 2^30 (device, written)
  * kv_copy_blk has to move the contents, in every layer's cache, before table_next is used; ring's blocks may be handed out after that. */

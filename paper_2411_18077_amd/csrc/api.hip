@@ -3,6 +3,7 @@
 #include "minikv_diag.h"
 
 #include <atomic>
+#include <initializer_list>
 
 namespace minikv {
 
@@ -311,23 +312,28 @@ int minikv_norm_rope(int32_t Hq, int32_t Hkv, int32_t T, int32_t dtype, const vo
                             K_out, k_out_stride, (hipStream_t)stream);
 }
 
+// What is written: aligned, nothing that is read, nothing twice
+static bool apart(std::initializer_list<const int32_t *> in, std::initializer_list<const int32_t *> out)
+{
+    for (const int32_t *p : in)
+        if (!aligned4(p)) return false;
+    for (auto o = out.begin(); o != out.end(); ++o) {
+        if (!aligned4(*o)) return false;
+        for (const int32_t *p : in)
+            if (p == *o) return false;
+        for (auto p = out.begin(); p != o; ++p)
+            if (*p == *o) return false;
+    }
+    return true;
+}
+
 int kv_fork_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *parent, const int32_t *n_keep, const int32_t *table,
                 const int32_t *ring, const int32_t *ring_state, int32_t *q_len_next, int32_t *table_next, int32_t *ring_state_next,
                 int32_t *src, int32_t *dst, void *stream)
 {
     const int rc = validate_blk(s);
     if (rc) return rc;
-    const int32_t *in[] = {q_len, parent, n_keep, table, ring, ring_state};
-    const int32_t *out[] = {q_len_next, table_next, ring_state_next, src, dst};
-    for (const int32_t *p : in)
-        if (!aligned4(p)) return MINIKV_EINVAL;
-    for (int i = 0; i < 5; ++i) {
-        if (!aligned4(out[i])) return MINIKV_EINVAL;
-        for (const int32_t *p : in)
-            if (p == out[i]) return MINIKV_EINVAL;
-        for (int j = 0; j < i; ++j)
-            if (out[j] == out[i]) return MINIKV_EINVAL;
-    }
+    if (!apart({q_len, parent, n_keep, table, ring, ring_state}, {q_len_next, table_next, ring_state_next, src, dst})) return MINIKV_EINVAL;
     return launch_fork_blk(*s, q_len, parent, n_keep, table, ring, ring_state, q_len_next, table_next, ring_state_next, src, dst,
                            (hipStream_t)stream);
 }
@@ -355,7 +361,7 @@ int kv_free_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_t *
 {
     const int rc = validate_blk(s);
     if (rc) return rc;
-    if (!aligned4(q_len) || !aligned4(table) || !aligned4(ring) || !aligned4(ring_state) || !aligned16(workspace)) return MINIKV_EINVAL;
+    if (!apart({q_len, table}, {ring, ring_state}) || !aligned16(workspace)) return MINIKV_EINVAL;
     if (workspace_bytes < pool_workspace_bytes(*s)) return MINIKV_EWORKSPACE;
     return launch_pool_blk(*s, q_len, table, nullptr, ring, ring_state, 0, nullptr, nullptr, workspace, (hipStream_t)stream);
 }
@@ -365,9 +371,8 @@ int kv_compact_blk(const minikv_blk_shape *s, const int32_t *q_len, const int32_
 {
     const int rc = validate_blk(s);
     if (rc) return rc;
-    if (!aligned4(q_len) || !aligned4(table) || !aligned4(table_next) || !aligned4(ring) || !aligned4(ring_state) || !aligned16(workspace))
-        return MINIKV_EINVAL;
-    if (n_pairs < 0 || n_pairs > kMaxPairs || (n_pairs && (!aligned4(src) || !aligned4(dst) || src == dst)) || table_next == table) return MINIKV_EINVAL;
+    if (n_pairs < 0 || n_pairs > kMaxPairs || !aligned16(workspace)) return MINIKV_EINVAL;
+    if (n_pairs ? !apart({q_len, table}, {table_next, ring, ring_state, src, dst}) : !apart({q_len, table}, {table_next, ring, ring_state})) return MINIKV_EINVAL;
     if (workspace_bytes < pool_workspace_bytes(*s)) return MINIKV_EWORKSPACE;
     return launch_pool_blk(*s, q_len, table, table_next, ring, ring_state, n_pairs, src, dst, workspace, (hipStream_t)stream);
 }

@@ -129,6 +129,9 @@ def test_free_refuses(api, which):
     p = [0x1000 * (i + 1) for i in range(5)]
     for v in (None, 0x1002):
         assert call(api, "kv_free_blk", [C.byref(shape(api)), *p[:which], v, *p[which + 1:], 1 << 40, None]) == -1
+    if which in (2, 3):
+        for other in range(which):                     # written: nothing that is read, nothing twice
+            assert call(api, "kv_free_blk", [C.byref(shape(api)), *p[:which], p[other], *p[which + 1:], 1 << 40, None]) == -1
     assert call(api, "kv_free_blk", [C.byref(shape(api)), *p, api.kv_free_workspace_bytes(shape(api)) - 1, None]) == -3
 
 
@@ -138,6 +141,9 @@ def test_compact_refuses(api, which):
     go = lambda q, n=3, size=1 << 40: call(api, "kv_compact_blk", [C.byref(shape(api)), *q[:5], n, *q[5:], size, None])  # noqa: E731
     for v in (None, 0x1002):
         assert go(p[:which] + [v] + p[which + 1:]) == -1
+    if 2 <= which <= 6:
+        for other in range(which):
+            assert go(p[:which] + [p[other]] + p[which + 1:]) == -1
     assert go(p, n=-1) == -1 and go(p, n=2 ** 30 + 1) == -1 and go(p, size=api.kv_free_workspace_bytes(shape(api)) - 1) == -3
     assert go(p[:2] + [p[1]] + p[3:]) == -1 and go(p[:6] + [p[5]] + p[7:]) == -1
 
