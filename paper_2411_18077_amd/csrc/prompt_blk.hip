@@ -30,6 +30,7 @@ constexpr int kPbThreads = 256;
 constexpr float kPbNone = -3.0e38f;                    // references before the first token: finite, so that no difference is NaN
 constexpr float kPbHead = 15.0f;                       // log2 of the largest weight
 constexpr float kPbRange = 60.0f;                      // V scales further below the largest one, as powers of two, count as 0
+constexpr float kPbNothing = -1024.0f;                 // log2 of a V scale that counts as 0: its products are below all that binary32 holds
 constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens for a wide block, 1 for a narrow one
 constexpr int kPbLeastWide = 6, kPbLeastNarrow = 2;    // least tiles of a part of a walk
 constexpr int kPbWholeNarrow = 6;                      // narrow walks of fewer tiles are not made in parts
@@ -292,14 +293,15 @@ __device__ __forceinline__ void value_places(int (&v_place)[4])
 }
 
 // Blocks' scales as the softmax takes them: ck takes a score to a power of two, lv = log2 Vs, add what is added (lv, or -inf where the block is
-// absent).
+// absent), add_m = add - lv, sum what takes a sum of weights with Vs to one without (-inf for a block whose values count as 0 but whose keys weigh: there
+// the weights without Vs are summed by themselves).
 struct BlockScale {
-    float ck, lv, add;
+    float ck, add, add_m, sum;
 };
 // Scales of NG blocks, block lane % NG in each lane (negative: absent).  none, zero: a bit for each block that is absent or whose values count as
-// 0; most: the largest lv so far.
+// 0; most: the largest lv so far.  Returns whether a block's weights have to be summed by themselves.
 template <int NG>
-__device__ __forceinline__ void block_scales(float ks, float vs, float c, float &most, BlockScale (&b)[NG], uint32_t &none, uint32_t &zero)
+__device__ __forceinline__ bool block_scales(float ks, float vs, float c, float &most, BlockScale (&b)[NG], uint32_t &none, uint32_t &zero)
 {
     const float l = vs > 0.0f ? log2_scale(vs) : kPbNone;
     float top = l;
@@ -308,10 +310,13 @@ __device__ __forceinline__ void block_scales(float ks, float vs, float c, float 
     most = fmaxf(most, top);
     const bool nil = !(l >= most - kPbRange);
     none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1), zero = (uint32_t)__ballot(nil) & ((1u << NG) - 1);
-    const float lv = !nil ? l : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv, ck = fmaxf(ks * c, 0x1p-126f);       // (ck not 0: a masked score is -inf)
+    const bool apart = nil && vs >= 0.0f;
+    const float lv = !nil ? l : apart ? kPbNothing : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv;
+    const float add_m = vs < 0.0f ? -INFINITY : 0.0f, sum = apart ? -INFINITY : -lv - kPbHead, ck = fmaxf(ks * c, 0x1p-126f);       // (ck not 0: a masked score is -inf)
     auto of = [](float v, int k) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k)); };
 #pragma unroll
-    for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].lv = of(lv, k), b[k].add = of(add, k);
+    for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].add = of(add, k), b[k].add_m = of(add_m, k), b[k].sum = of(sum, k);
+    return zero != none;
 }
 
 // Per lane: a row's references of the weights with and without Vs, the sum of those without (of this half's keys), and O^T:
@@ -332,7 +337,7 @@ struct RowState {
 
 // 32 TILES scores a row (16 TILES a lane) of NG blocks to weights
 template <int TILES, int NG>
-__device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockScale (&b)[NG], RowState &st, half8 (&wb)[2 * TILES])
+__device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockScale (&b)[NG], bool apart, RowState &st, half8 (&wb)[2 * TILES])
 {
     constexpr int kOf = 16 * TILES / NG;               // scores of a block
     float top = -INFINITY, top_v = -INFINITY;
@@ -342,7 +347,7 @@ __device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockSc
 #pragma unroll
         for (int e = k * kOf; e < (k + 1) * kOf; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
         top_v = fmaxf(top_v, __builtin_fmaf(mx, b[k].ck, b[k].add));
-        top = fmaxf(top, __builtin_fmaf(mx, b[k].ck, b[k].add - b[k].lv));
+        top = fmaxf(top, __builtin_fmaf(mx, b[k].ck, b[k].add_m));
     }
     auto both = [&](float v) {                         // (the other half-wave holds the row's other keys)
         const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -353,13 +358,19 @@ __device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockSc
         const float to = fmaxf(top, st.m);
         st.l *= __builtin_amdgcn_exp2f(st.m - to), st.m = to;
     }
-    if (__any(top_v > st.mv)) {
+    if (apart || __any(top_v > st.mv)) {
         const float to = fmaxf(top_v, st.mv), alpha = __builtin_amdgcn_exp2f(st.mv - to);
         st.mv = to;
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) st.o[db][i] *= alpha;
+        if (apart)                                     // (in here, as a branch of its own costs 3 %)
+#pragma unroll
+            for (int k = 0; k < NG; ++k)
+                if (b[k].sum == -INFINITY)
+#pragma unroll
+                    for (int e = k * kOf; e < (k + 1) * kOf; ++e) st.l += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], b[k].ck, b[k].add_m - st.m));
     }
 #pragma unroll
     for (int k = 0; k < NG; ++k) {
@@ -370,7 +381,7 @@ __device__ __forceinline__ void softmax_step(float16v (&s)[TILES], const BlockSc
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], b[k].ck, off));
             sum += w, wb[e >> 3][e & 7] = (_Float16)w;
         }
-        st.l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(st.mv - st.m - b[k].lv - kPbHead), st.l);
+        st.l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(st.mv - st.m + b[k].sum), st.l);
     }
 }
 
@@ -433,10 +444,11 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
 #pragma unroll
     for (int e = 0; e < 2; ++e) put_key[e] = tile_place(key0, 2 * chunk + e), put_value[e] = key0 * kPfD + (((2 * chunk + e) ^ v_swizzle(key0)) << 3);
     BlockScale scale[NG];                              // of the tile in local memory
+    bool apart;
     float most = -1.0e30f;
     auto store = [&](const Tile<NG> &x, int n, auto odd) {             // (odd: which of the two buffers, known when compiling)
         uint32_t none, zero;
-        block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
+        apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
         const bool plain = !zero && n * 64 + 64 <= pg.L;               // (absent ones are zero too)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -482,7 +494,7 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
                     for (int i = 0; i < 16; ++i)
                         if (t * 32 + acc_row(i, 0) > rel) s[t][i] = -INFINITY;
             }
-            softmax_step<2, NG>(s, scale, st, wb);
+            softmax_step<2, NG>(s, scale, apart, st, wb);
             add_values<4>(Vt, v_place, wb, st);
         }
         if (n + 1 < t1) store(y, n + 1, even);
@@ -545,7 +557,7 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
     auto step = [&](Unit<NG> &x, int u) {
         BlockScale scale[NG];
         uint32_t none, zero;
-        block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
+        const bool apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
         const bool plain = !zero && u * 32 + 32 <= pg.L;               // (absent ones are zero too)
         float16v s[1];
 #pragma unroll
@@ -582,7 +594,7 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
                 if (acc_row(i, 0) > rel) s[0][i] = -INFINITY;
         }
         half8 wb[2];
-        softmax_step<1, NG>(s, scale, st, wb);
+        softmax_step<1, NG>(s, scale, apart, st, wb);
         add_values<2>(Vt, v_place, wb, st);
     };
     Unit<NG> x, y;
