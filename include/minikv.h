@@ -349,8 +349,7 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  * left alone, as are the rows of no request.  What lies behind a request's last token in its last block is not used, whatever it holds.
  * Scales are finite, 0 or at least 2^-126.  The raw products q . codes, the scores and the sums of exp(score - largest score) times value are
  * formed in binary32 and must not overflow there, nor K's scales times 2 sm_scale.  Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is
- * below 2^-29 of the largest such product of the row by at most 2^-40 of that one.  Values of a block whose V scale is below 2^-60 of one in
- * front of it in the request's head may count as 0.
+ * below 2^-29 of the largest such product of the row by at most 2^-40 of that one, whatever the scales of the row's blocks.
  *   T       rows of q, out and lse (a host-side bound of cu[R])
  *   q       fp16 / bf16 [T][Hq][128], tokens q_stride elements apart            (device, read)
  *   cu      int32 [R+1], non-decreasing                                         (device, read)

@@ -29,8 +29,8 @@ constexpr int kPbTail = 64;                            // most rows behind the l
 constexpr int kPbThreads = 256;
 constexpr float kPbNone = -3.0e38f;                    // references before the first token: finite, so that no difference is NaN
 constexpr float kPbHead = 15.0f;                       // log2 of the largest weight
-constexpr float kPbRange = 60.0f;                      // V scales further below the largest one, as powers of two, count as 0
-constexpr float kPbNothing = -1024.0f;                 // log2 of a V scale that counts as 0: its products are below all that binary32 holds
+constexpr float kPbRange = 60.0f;                      // V scales, as powers of two, further below the largest one: weights with them do not give those without
+constexpr float kPbNothing = -1024.0f;                 // log2 of a V scale of 0: its products are below all that binary32 holds
 constexpr int kPbWideCost = 2;                         // of a tile of 64 tokens for a wide block, 1 for a narrow one
 constexpr int kPbLeastWide = 6, kPbLeastNarrow = 2;    // least tiles of a part of a walk
 constexpr int kPbWholeNarrow = 6;                      // narrow walks of fewer tiles are not made in parts
@@ -293,30 +293,29 @@ __device__ __forceinline__ void value_places(int (&v_place)[4])
 }
 
 // Blocks' scales as the softmax takes them: ck takes a score to a power of two, lv = log2 Vs, add what is added (lv, or -inf where the block is
-// absent), add_m = add - lv, sum what takes a sum of weights with Vs to one without (-inf for a block whose values count as 0 but whose keys weigh: there
-// the weights without Vs are summed by themselves).
+// absent), add_m = add - lv, sum what takes a sum of weights with Vs to one without (-inf for a block whose Vs is 0 or far below the largest, where
+// a weight with it may be 0 and the one without all there is: there these are summed by themselves).
 struct BlockScale {
     float ck, add, add_m, sum;
 };
-// Scales of NG blocks, block lane % NG in each lane (negative: absent).  none, zero: a bit for each block that is absent or whose values count as
-// 0; most: the largest lv so far.  Returns whether a block's weights have to be summed by themselves.
+// Scales of NG blocks, block lane % NG in each lane (negative: absent).  none: a bit for each block that is absent; most: the largest lv so far.
+// Returns whether a block's weights have to be summed by themselves.
 template <int NG>
-__device__ __forceinline__ bool block_scales(float ks, float vs, float c, float &most, BlockScale (&b)[NG], uint32_t &none, uint32_t &zero)
+__device__ __forceinline__ bool block_scales(float ks, float vs, float c, float &most, BlockScale (&b)[NG], uint32_t &none)
 {
     const float l = vs > 0.0f ? log2_scale(vs) : kPbNone;
     float top = l;
     if (NG >= 2) top = fmaxf(top, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(top), 0xb1, 0xf, 0xf, false)));        // quad_perm 1, 0, 3, 2
     if (NG == 4) top = fmaxf(top, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(top), 0x4e, 0xf, 0xf, false)));        // quad_perm 2, 3, 0, 1
     most = fmaxf(most, top);
-    const bool nil = !(l >= most - kPbRange);
-    none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1), zero = (uint32_t)__ballot(nil) & ((1u << NG) - 1);
-    const bool apart = nil && vs >= 0.0f;
-    const float lv = !nil ? l : apart ? kPbNothing : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv;
+    none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1);
+    const bool apart = vs >= 0.0f && !(l >= most - kPbRange);
+    const float lv = vs > 0.0f ? l : vs == 0.0f ? kPbNothing : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv;
     const float add_m = vs < 0.0f ? -INFINITY : 0.0f, sum = apart ? -INFINITY : -lv - kPbHead, ck = fmaxf(ks * c, 0x1p-126f);       // (ck not 0: a masked score is -inf)
     auto of = [](float v, int k) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k)); };
 #pragma unroll
     for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].add = of(add, k), b[k].add_m = of(add_m, k), b[k].sum = of(sum, k);
-    return zero != none;
+    return __any(apart);
 }
 
 // Per lane: a row's references of the weights with and without Vs, the sum of those without (of this half's keys), and O^T:
@@ -447,17 +446,17 @@ __device__ __forceinline__ void walk_wide(const PromptBlkArgs &a, const Pages &p
     bool apart;
     float most = -1.0e30f;
     auto store = [&](const Tile<NG> &x, int n, auto odd) {             // (odd: which of the two buffers, known when compiling)
-        uint32_t none, zero;
-        apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
-        const bool plain = !zero && n * 64 + 64 <= pg.L;               // (absent ones are zero too)
+        uint32_t none;
+        apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none);
+        const bool plain = !none && n * 64 + 64 <= pg.L;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int key = key0 + 32 * j;
             u4b k = x.k[j], v = x.v[j], w[2];
             if (!plain) {
-                const bool in = n * 64 + key < pg.L, no_key = none >> granule(j) & 1, no_value = zero >> granule(j) & 1;
+                const bool in = n * 64 + key < pg.L && !(none >> granule(j) & 1);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) k[e] = in && !no_key ? k[e] : 0, v[e] = in && !no_value ? v[e] : 0;
+                for (int e = 0; e < 4; ++e) k[e] = in ? k[e] : 0, v[e] = in ? v[e] : 0;
             }
             _Float16 *Kt = tiles + (decltype(odd)::value * 2 * kPfTile + 32 * j * kPfD), *Vt = Kt + kPfTile;
             widen<BF16>(k, w);
@@ -556,9 +555,9 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
     };
     auto step = [&](Unit<NG> &x, int u) {
         BlockScale scale[NG];
-        uint32_t none, zero;
-        const bool apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none, zero);
-        const bool plain = !zero && u * 32 + 32 <= pg.L;               // (absent ones are zero too)
+        uint32_t none;
+        const bool apart = block_scales<NG>(x.ks, x.vs, a.c, most, scale, none);
+        const bool plain = !none && u * 32 + 32 <= pg.L;
         float16v s[1];
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
@@ -566,7 +565,7 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
             const bool no_key = u * 32 + r >= pg.L || (none >> (NG == 1 ? 0 : r >> 4) & 1);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bool no_value = u * 32 + key0 + 8 * j >= pg.L || (zero >> (j * NG / 4) & 1);
+                const bool no_value = u * 32 + key0 + 8 * j >= pg.L || (none >> (j * NG / 4) & 1);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x.k[j][e] = no_key ? 0 : x.k[j][e], x.v[j][e] = no_value ? 0 : x.v[j][e];
             }

@@ -71,3 +71,29 @@ def test_values_of_zero_with_all_the_weight(Hq, Hkv, n, block):
     c.q, c.q_dev = x, x.cuda()
     want = check_relative(c.run())
     assert 0.0 < float(want.abs().max()) < 2.0 ** -50  # (the test's own premise)
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 70), (128, 128, 150)])
+@pytest.mark.parametrize("block", [16, 32, 64])
+def test_larger_scales_behind_take_nothing_from_those_in_front(Hq, Hkv, n, block):
+    """Each block's V scale 2^70 above the one before it: rows that end inside a block do not see the next one, whose values they share a tile with."""
+    c = Case([0], [n], Hq, Hkv, block, BF16, seed=40 + block)
+    for i, b in enumerate(c.table[0].tolist()):
+        if b >= 0:
+            c.Vs[b] = 2.0 ** (-100 + 70 * (i % 4))     # -100, -30, 40, 110
+    want = check_relative(c.run())
+    assert float(want[:16].abs().max()) < 2.0 ** -90         # (the test's own premise)
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 70), (128, 128, 150)])
+@pytest.mark.parametrize("block", [16, 32, 64])
+def test_smaller_scales_behind_that_have_all_the_weight(Hq, Hkv, n, block):
+    """V scales fall by 2^70 and the keys' weights rise by 2^115: each block's values are those of the rows that end in it."""
+    c = Case([0], [n], Hq, Hkv, block, BF16, seed=45 + block)
+    c.Kc[:] = 0x38
+    for i, b in enumerate(c.table[0].tolist()):
+        if b >= 0:
+            c.Vs[b], c.Ks[b] = 2.0 ** (100 - 70 * (i % 4)), 2.0 * (i % 4) + (0 if i < 4 else 8)
+    x = torch.full_like(c.q, 3.5)
+    c.q, c.q_dev = x, x.cuda()
+    check_relative(c.run())
