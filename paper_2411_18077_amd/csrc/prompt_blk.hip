@@ -331,7 +331,12 @@ struct RowState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
     }
-    __device__ float by() const { return __builtin_amdgcn_exp2f(mv - m - kPbHead); }         // of o, to the weights over m
+    // o * by().x * by().y is o to the weights over m: two factors, as one may be below the numbers that the instruction makes (mv - m is a scale's logarithm)
+    __device__ float2 by() const
+    {
+        const float half = __builtin_amdgcn_exp2f(0.5f * (mv - m));
+        return float2{half, half * 0x1p-15f};          // 2^-kPbHead
+    }
 };
 
 // 32 TILES scores a row (16 TILES a lane) of NG blocks to weights
@@ -652,13 +657,14 @@ __global__ __launch_bounds__(kPbThreads, 2) void prompt_blk_kernel(PromptBlkArgs
     {
         const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.l), __float_as_uint(st.l), false, false);
         if (g == 0) wave_ml[wave][r] = float2{st.m, __uint_as_float(h[0]) + __uint_as_float(h[1])};
-        const float by = st.by();
+        const float2 by = st.by();
+        auto weighed = [&](float v) { return v * by.x * by.y; };
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *(float4 *)(rows_of + (wave * 32 + r) * kD + (((db * 8 + (i >> 1) + g) ^ r) << 2)) =
-                    float4{st.o[db][i] * by, st.o[db][i + 1] * by, st.o[db][i + 2] * by, st.o[db][i + 3] * by};
+                    float4{weighed(st.o[db][i]), weighed(st.o[db][i + 1]), weighed(st.o[db][i + 2]), weighed(st.o[db][i + 3])};
     }
     __syncthreads();
     const int quad = tid & 31;                         // a thread's four channels, of rows tid / 32 + 8 k

@@ -97,3 +97,19 @@ def test_smaller_scales_behind_that_have_all_the_weight(Hq, Hkv, n, block):
     x = torch.full_like(c.q, 3.5)
     c.q, c.q_dev = x, x.cuda()
     check_relative(c.run())
+
+
+@pytest.mark.parametrize("held,n,Hq,Hkv", [(70, 20, 4, 2), (70, 150, 128, 128), (5000, 3, 2, 1)])
+@pytest.mark.parametrize("exponent", [-112, -115, -126])
+def test_the_smallest_scales(held, n, Hq, Hkv, exponent):
+    """All of a row's V scales next to the smallest normal number: outputs are normal numbers of bf16 all the same."""
+    c = Case([held], [n], Hq, Hkv, 32, BF16, seed=70)
+    c.Vs[:] = 2.0 ** exponent
+    assert float(check_relative(c.run()).abs().max()) > 2.0 ** exponent
+
+
+@pytest.mark.parametrize("held,n,Hq,Hkv", [(70, 20, 4, 2), (70, 150, 128, 128)])
+def test_the_largest_scales(held, n, Hq, Hkv):
+    c = Case([held], [n], Hq, Hkv, 16, BF16, seed=71)
+    c.Vs[:] = 2.0 ** 117                               # (times 448: below 2^126)
+    check_relative(c.run())
