@@ -113,3 +113,13 @@ def test_the_largest_scales(held, n, Hq, Hkv):
     c = Case([held], [n], Hq, Hkv, 16, BF16, seed=71)
     c.Vs[:] = 2.0 ** 117                               # (times 448: below 2^126)
     check_relative(c.run())
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 30), (128, 128, 150)])
+def test_keys_of_nothing_and_queries_of_any_size(Hq, Hkv, n):
+    """Raw products of up to 2^126 with keys of scale 0: scores of 0."""
+    c = Case([64], [n], Hq, Hkv, 16, BF16, seed=80, gain=2.0 ** 112)
+    c.Ks *= 2.0 ** -112
+    zero = c.table[0, 1].long()
+    c.Kc[zero], c.Ks[zero] = 0x7e, 0.0
+    check_relative(c.run())
