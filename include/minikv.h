@@ -347,7 +347,7 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  * A row without tokens (n > q_len[r], or all of them absent) gives zeros and -infinity.  Table entries outside 0 .. n_blocks-1 count as absent:
  * their tokens contribute nothing.  Lengths are clamped to 0 .. max_blocks * block; a request whose rows do not lie inside 0 .. T-1 is
  * left alone, as are the rows of no request.  What lies behind a request's last token in its last block is not used, whatever it holds.
- * Scales are finite, 0 or at least 2^-126.  The raw products q . codes, the scores and the sums of exp(score - largest score) times value are
+ * The scales of the blocks that a request names are finite, 0 or at least 2^-126; other blocks' are not used.  The raw products q . codes, the scores and the sums of exp(score - largest score) times value are
  * formed in binary32 and must not overflow there, nor K's scales times 2 sm_scale.  Each weight times its block's V scale is rounded to 11 bits for the second product, or where it is
  * below 2^-29 of the largest such product of the row by at most 2^-40 of that one, whatever the scales of the row's blocks.
  *   T       rows of q, out and lse (a host-side bound of cu[R])

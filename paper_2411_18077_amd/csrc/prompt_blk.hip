@@ -311,7 +311,8 @@ __device__ __forceinline__ bool block_scales(float ks, float vs, float c, float 
     none = (uint32_t)__ballot(vs < 0.0f) & ((1u << NG) - 1);
     const bool apart = vs >= 0.0f && !(l >= most - kPbRange);
     const float lv = vs > 0.0f ? l : vs == 0.0f ? kPbNothing : most > -1.0e29f ? most : 0.0f, add = vs < 0.0f ? -INFINITY : lv;
-    const float add_m = vs < 0.0f ? -INFINITY : 0.0f, sum = apart ? -INFINITY : -lv - kPbHead, ck = fmaxf(ks * c, 0x1p-149f);       // (ck not 0: a masked score is -inf; the least there is, as raw products may be large)
+    const float add_m = vs < 0.0f ? -INFINITY : 0.0f, sum = apart ? -INFINITY : -lv - kPbHead;
+    const float ck = fmaxf(vs < 0.0f ? 0.0f : ks * c, 0x1p-149f);      // (not 0: a masked score is -inf; the least there is, as raw products may be large)
     auto of = [](float v, int k) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k)); };
 #pragma unroll
     for (int k = 0; k < NG; ++k) b[k].ck = of(ck, k), b[k].add = of(add, k), b[k].add_m = of(add_m, k), b[k].sum = of(sum, k);

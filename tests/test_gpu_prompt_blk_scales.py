@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from pages_common import HALF, SM, lse_tolerance
+from pages_common import HALF, SM, check_prompt, lse_tolerance
 from oracle import pages
 from test_gpu_prompt_blk import Case
 
@@ -123,3 +123,18 @@ def test_keys_of_nothing_and_queries_of_any_size(Hq, Hkv, n):
     zero = c.table[0, 1].long()
     c.Kc[zero], c.Ks[zero] = 0x7e, 0.0
     check_relative(c.run())
+
+
+@pytest.mark.parametrize("Hq,Hkv,n", [(4, 2, 30), (128, 128, 150)])
+@pytest.mark.parametrize("block", [16, 32, 64])
+@pytest.mark.parametrize("scale", [math.inf, math.nan, 3e38])
+def test_absent_blocks_beside_a_free_block_of_any_scale(Hq, Hkv, n, block, scale):
+    """Block 0 is in no table, and holds what its memory held."""
+    c = Case([3 * block], [n], Hq, Hkv, block, F16, seed=90)
+    spare = (set(range(c.N)) - set(c.table[0].tolist())).pop()
+    c.table[c.table == 0] = spare
+    c.table[0, 1] = -1
+    c.Ks[0], c.Vs[0], c.Kc[0], c.Vc[0] = scale, scale, 0x7f, 0xff
+    c.run()
+    c.Ks[0], c.Vs[0] = 1.0, 1.0
+    check_prompt(c.shape, c.q, (c.Kc, c.Ks, c.Vc, c.Vs), c.table, c.q_len, c.cu, c.out, c.lse)
