@@ -52,4 +52,12 @@ __device__ __forceinline__ half4 read_transposed(const _Float16 *p)
     return (half4)__builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4 *)p);
 }
 
+// Local memory that one wave writes and reads: its operations are done in order, the compiler is told to keep them so.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 }  // namespace minikv

@@ -125,13 +125,6 @@ __device__ __forceinline__ unsigned lds_offset(const void *p)
 {
     return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
 }
-// Local memory that one wave writes and reads: its operations are done in order, the compiler is told to keep them so.
-__device__ __forceinline__ void wave_order()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 // A workgroup of WAVES waves owns 32 queries per wave (their Q rows in registers) and walks the keys in tiles of 64.
 // Scores are computed TRANSPOSED, S^T = K Q^T, so that a lane holds one query column (see the top of the file).  One

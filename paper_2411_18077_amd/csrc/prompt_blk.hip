@@ -600,7 +600,9 @@ __device__ __forceinline__ void walk_narrow(const PromptBlkArgs &a, const Pages 
         }
         half8 wb[2];
         softmax_step<1, NG>(s, scale, apart, st, wb);
+        wave_order();                                  // (other lanes' values, and their places for the next ones)
         add_values<2>(Vt, v_place, wb, st);
+        wave_order();
     };
     Unit<NG> x, y;
     if (u0 < u1) x.id = pg.id(u0 * 32 + mine);
