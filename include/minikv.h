@@ -357,7 +357,7 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  *   workspace  device scratch of at least minikv_prompt_blk_workspace_bytes(shape, T) bytes, 16-byte aligned, ZERO-FILLED ONCE after
  *              allocation (every call returns its ticket counters to zero).  Calls of any shapes may take turns on one workspace of
  *              sufficient size; two calls that share a workspace must be ordered (same stream).
- * T * Hq < 2^31, (T * Hq / 128 / Hkv + 2 min(R, T)) * Hkv < 2^23 - 512, sm_scale finite and > 0.  T == 0 is no error and writes nothing. */
+ * T * Hq < 2^31; n = T * Hq / 128 / Hkv + 2 min(R, T) <= 2^22 - 512, n * Hkv < 2^23 - 512; sm_scale finite and > 0.  T == 0 is no error and writes nothing. */
 size_t minikv_prompt_blk_workspace_bytes(const minikv_blk_shape *shape, int32_t T);
 int minikv_prompt_attn_blk(const minikv_blk_shape *shape, int32_t T, const void *q, int64_t q_stride, const minikv_blk_cache *cache,
                            const int32_t *table, const int32_t *q_len, const int32_t *cu, float sm_scale, void *out, float *lse,

@@ -40,7 +40,7 @@ constexpr int kPbStream = 16384;                       // cost of all blocks, in
 constexpr int kPbJoin = 8;                             // parts joined at once
 constexpr int kPbMost = 512;                           // parts of a walk: three rounds of joins
 constexpr int kPbGroups = 4;                           // of items, by the length of their walks
-constexpr uint32_t kPbCut = 1 << 22;                   // 2^8 threads and four groups: sums below 2^32
+constexpr uint32_t kPbCut = 1 << 22;                   // most items of a thread in a group; 2^8 threads and four groups: sums below 2^32
 
 struct PromptBlkArgs {
     const uint16_t *q;
@@ -98,7 +98,7 @@ template <int CTRL, int ROWS> __device__ inline uint32_t add_dpp(uint32_t v)
 {
     return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
 }
-// Sum of the lanes up to this one.  (Not saturating, as that of scan.h: counts of a thread are cut to kPbCut, and no valid call has so many.)
+// Sum of the lanes up to this one.  (Not saturating, as that of scan.h: counts of a thread are cut to kPbCut, and the launch refuses calls that have more.)
 __device__ inline uint32_t wave_prefix(uint32_t v)
 {
     v = add_dpp<0x111, 0xf>(v), v = add_dpp<0x112, 0xf>(v), v = add_dpp<0x114, 0xf>(v), v = add_dpp<0x118, 0xf>(v);
@@ -803,7 +803,7 @@ int launch_prompt_blk(const minikv_blk_shape &s, int32_t T, const void *q, int64
     const int64_t tiles = ((int64_t)s.max_blocks * s.block + 63) / 64;
     const int64_t parts = tiles < kPbWholeNarrow ? 1 : (tiles + kPbLeastNarrow - 1) / kPbLeastNarrow;
     const int64_t items = blocks * parts < blocks + kPbSlots ? blocks * parts : blocks + kPbSlots;
-    if (items > 0x7fffff) return MINIKV_EINVAL;
+    if (items > 0x7fffff || blocks / s.Hkv > (int64_t)kPbCut - kPbSlots) return MINIKV_EINVAL;
     const dim3 grid((unsigned)items), threads(kPbThreads);
     const bool bf16 = s.dtype == MINIKV_BF16;
 #define LAUNCH(NG)                                                                                        \

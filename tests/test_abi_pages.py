@@ -95,6 +95,13 @@ def test_prompt_attn_refuses_more_row_blocks_than_a_launch_counts(api):
     assert call(api, "minikv_prompt_attn_blk", prompt_args(api, s, T=T, qs=65536)) == -1
 
 
+@pytest.mark.parametrize("R,T", [(1, (1 << 26) + 1024), (1, (1 << 26) - (1 << 13)), (8192, 1 << 26)])
+def test_prompt_attn_refuses_more_row_blocks_of_a_head_than_it_counts(api, R, T):
+    """8 heads over one: blocks of 128 rows are T / 16, and two a request beside them; 2^22 - 512 at most."""
+    s = shape(api, R=R, Hkv=1, n_blocks=1000)
+    assert call(api, "minikv_prompt_attn_blk", prompt_args(api, s, T=T, out=1 << 45, lse=1 << 46)) == -1
+
+
 def test_prompt_workspace_covers_the_parts(api):
     """1024 parts of up to 128 rows: m, l and 128 sums each; fewer rows where T has fewer."""
     s = shape(api)
