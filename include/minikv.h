@@ -353,7 +353,7 @@ int minikv_decode_attn_blk(const minikv_blk_shape *shape, const void *q, int64_t
  *   T       rows of q, out and lse (a host-side bound of cu[R])
  *   q       fp16 / bf16 [T][Hq][128], tokens q_stride elements apart            (device, read)
  *   cu      int32 [R+1], non-decreasing                                         (device, read)
- *   out     fp16 / bf16 [T][Hq][128], contiguous; lse fp32 [T][Hq] or NULL      (device, written)
+ *   out     fp16 / bf16 [T][Hq][128], contiguous; lse fp32 [T][Hq] or NULL      (device, written; nothing that is read, nor one the other)
  *   workspace  device scratch of at least minikv_prompt_blk_workspace_bytes(shape, T) bytes, 16-byte aligned, ZERO-FILLED ONCE after
  *              allocation (every call returns its ticket counters to zero).  Calls of any shapes may take turns on one workspace of
  *              sufficient size; two calls that share a workspace must be ordered (same stream).

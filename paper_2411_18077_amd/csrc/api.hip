@@ -275,6 +275,13 @@ int minikv_decode_attn_blk(const minikv_blk_shape *s, const void *q, int64_t q_s
     return launch_decode_blk(*s, q, q_stride, *c, table, q_len, sm_scale, out, workspace, (hipStream_t)stream);
 }
 
+// Whether p's `bytes` bytes meet one of `rows` rows of `row` bytes that begin `stride` bytes apart
+static bool meets_rows(const void *first, int64_t rows, int64_t row, int64_t stride, const void *p, int64_t bytes)
+{
+    const int64_t d = (int64_t)((uintptr_t)p - (uintptr_t)first), t = d < row ? 0 : (d - row) / stride + 1;        // the first row that ends behind p
+    return t < rows && t * stride < d + bytes;
+}
+
 size_t minikv_prompt_blk_workspace_bytes(const minikv_blk_shape *s, int32_t T)
 {
     return validate_blk(s) == MINIKV_OK && T >= 0 && (int64_t)T * s->Hq <= 0x7fffffff ? prompt_blk_workspace_bytes(*s, T) : 0;
@@ -292,6 +299,9 @@ int minikv_prompt_attn_blk(const minikv_blk_shape *s, int32_t T, const void *q, 
     if (T == 0) return MINIKV_OK;                                                      // (a null pointer is one of an empty tensor)
     if (!aligned16(q) || !aligned16(out) || (lse && !aligned4(lse)) || !aligned16(workspace)) return MINIKV_EINVAL;
     if (workspace_bytes < prompt_blk_workspace_bytes(*s, T)) return MINIKV_EWORKSPACE;
+    const int64_t heads = s->Hq, row = heads * kD * 2, sums = T * heads * 4;          // (a workgroup that is done writes rows that others have not read yet)
+    if (meets_rows(q, T, row, q_stride * 2, out, T * row)) return MINIKV_EINVAL;
+    if (lse && (meets_rows(q, T, row, q_stride * 2, lse, sums) || meets_rows(out, 1, T * row, T * row, lse, sums))) return MINIKV_EINVAL;
     return launch_prompt_blk(*s, T, q, q_stride, *c, table, q_len, cu, sm_scale, out, lse, workspace, (hipStream_t)stream);
 }
 

@@ -102,6 +102,16 @@ def test_prompt_attn_refuses_more_row_blocks_of_a_head_than_it_counts(api, R, T)
     assert call(api, "minikv_prompt_attn_blk", prompt_args(api, s, T=T, out=1 << 45, lse=1 << 46)) == -1
 
 
+@pytest.mark.parametrize("out,lse", [
+    (0x100000, None), (0x100000 + 2032, None), (0x100000 + 4 * 8192 + 2032, None), (0x100000 + 2048, None), (0x100000 - 5 * 2048 + 16, None),
+    (1 << 40, 0x100000 + 2044), (1 << 40, 0x100000 + 8192 - 156), (1 << 40, 0x100000 - 156), (1 << 40, 1 << 40), (1 << 40, (1 << 40) + 5 * 2048 - 4),
+    (1 << 40, (1 << 40) - 156),
+])
+def test_prompt_attn_refuses_outputs_over_what_is_read(api, out, lse):
+    """Five rows of 2048 bytes, 8192 apart, and outputs of five rows one behind the other; sums of 160 bytes."""
+    assert call(api, "minikv_prompt_attn_blk", prompt_args(api, q=0x100000, qs=4096, out=out, lse=lse)) == -1
+
+
 def test_prompt_workspace_covers_the_parts(api):
     """1024 parts of up to 128 rows: m, l and 128 sums each; fewer rows where T has fewer."""
     s = shape(api)

@@ -359,3 +359,28 @@ def test_blocks_far_into_a_large_pool():
     api.minikv_prompt_attn_blk(shape, 10, q.cuda(), cache, at[None].int().cuda(), ints([180]).cuda(), ints([0, 10]).cuda(), SM, out, lse, ws)
     (Kc, ks), (Vc, vs) = small
     check_prompt(shape, q, (Kc, ks, Vc, vs), torch.arange(3)[None].int(), ints([180]), ints([0, 10]), out, lse)
+
+
+def test_outputs_between_the_rows_of_queries():
+    """Rows of q far apart, out and lse in the room between them: no overlap, no refusal."""
+    c = Case([40], [2], 4, 2, 16, F16, seed=38, extra_rows=0).run()
+    want, lse = c.out.clone(), c.lse.clone()
+    buf = torch.zeros(2, 8 * 1024, dtype=F16, device="cuda")
+    q = buf.as_strided((2, 4, 128), (8 * 1024, 128, 1))
+    q.copy_(c.q_dev)
+    out, sums = buf[0, 512:1536].view(2, 4, 128), buf[0, 1536:1552].view(torch.float32).view(2, 4)
+    api.minikv_prompt_attn_blk(*c.args[:2], q, *c.args[3:8], out, sums, c.ws)
+    assert torch.equal(out, want) and torch.equal(sums, lse) and torch.equal(q, c.q_dev)
+
+
+def test_outputs_over_queries_are_refused():
+    c = Case([40], [2], 4, 2, 16, F16, seed=39, extra_rows=0).run()
+    flat = torch.zeros(4096, dtype=F16, device="cuda")
+    q = flat[1024:2048].view(2, 4, 128)
+    for out, lse in ((q, c.lse), (flat[:1032][8:].view(2, 4, 128), c.lse), (flat[2040:3064].view(2, 4, 128), c.lse),
+                     (c.out, flat[2040:2056].view(torch.float32).view(2, 4)), (c.out, c.out.view(-1)[1008:].view(torch.float32).view(2, 4))):
+        before = flat.clone(), c.out.clone()
+        with pytest.raises(api.MinikvError):
+            api.minikv_prompt_attn_blk(*c.args[:2], q, *c.args[3:8], out, lse, c.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(flat, before[0]) and torch.equal(c.out, before[1])
