@@ -7,6 +7,7 @@ There is no CPU fallback: if the HIP library is missing, loading raises.
 """
 import ctypes as C
 import os
+import warnings
 
 import torch
 
@@ -59,7 +60,7 @@ _lib = _bind = None
 
 
 def lib():
-    """Load libminikv.so and _bind.so (built in-tree by `python -m paper_2411_18077_amd.build`)."""
+    """Load libminikv.so, and _bind.so if it is there (built in-tree by `python -m paper_2411_18077_amd.build`)."""
     global _lib, _bind
     if _lib is None:
         if not os.path.exists(LIB_PATH):
@@ -157,12 +158,23 @@ def lib():
         l.kv_select_hh_rw.argtypes = [C.c_int32, C.c_int32, C.c_int64, P, P, P, P, C.c_int64, P, P, C.c_size_t, P]
         l.kv_pyramid_budget.restype = C.c_int
         l.kv_pyramid_budget.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_int32, C.POINTER(C.c_double)]
-        try:
-            from . import _bind as bind
-        except ImportError as e:
-            raise ImportError("_bind.so is not built: run `python -m paper_2411_18077_amd.build`") from e
-        _lib, _bind = l, bind
+        _lib, _bind = l, _compiled()
     return _lib
+
+
+def _compiled():
+    """_bind.so, or None, and a warning, where it cannot be used: its calls are then made from here."""
+    from .build import bound_to
+    try:
+        from . import _bind as bind
+        if bind.built_for == bound_to():
+            return bind
+        why = "it is built for %s" % bind.built_for
+    except ImportError as e:
+        why = str(e)
+    warnings.warn("the compiled calls of _bind.so are not in use, some calls take longer (`python -m paper_2411_18077_amd.build` makes it for %s): %s"
+                  % (bound_to(), why), RuntimeWarning, stacklevel=3)
+    return None
 
 
 def _ptr(t):

@@ -52,11 +52,17 @@ def _compile(src):
     return obj, warn
 
 
+def bound_to():
+    """What _bind.so is built for and has to run with: it takes tensors and objects as these lay them out."""
+    import torch
+    return "torch %s, Python %d.%d" % ((torch.__version__,) + sys.version_info[:2])
+
+
 def _compile_bind():
     import torch
     root = os.path.dirname(torch.__file__)
     obj = os.path.join(OBJ, "bind.o")
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", '-DMINIKV_BUILT_FOR="%s"' % bound_to(), "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            "-I" + os.path.join(ROOT, "include"), "-I" + sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -71,7 +77,6 @@ def build(verbose=True):
     with ThreadPoolExecutor(max_workers=4) as ex:
         bind = ex.submit(_compile_bind)
         results = list(ex.map(_compile, SOURCES))
-        link_bind = bind.result()
     objs = [o for o, _ in results]
     for _, w in results:
         if w and verbose:
@@ -80,6 +85,7 @@ def build(verbose=True):
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError("link failed:\n%s\n%s" % (r.stdout, r.stderr))
+    link_bind = bind.result()                          # (what was wrong there, now that the library is there)
     r = subprocess.run(link_bind, capture_output=True, text=True)
     if r.returncode:
         raise RuntimeError("link of _bind.so failed:\n%s\n%s" % (r.stdout, r.stderr))

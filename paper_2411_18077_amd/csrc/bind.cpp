@@ -220,4 +220,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__bind() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__bind()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", MINIKV_BUILT_FOR) < 0) Py_CLEAR(m);
+    return m;
+}

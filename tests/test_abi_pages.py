@@ -203,3 +203,48 @@ def test_binding_refuses_types_sizes_and_places(api):
         api.BlkCaches(s, [dict(K=z(1), V=z(1), Ks=z(1), Vs=z(1))])
     with pytest.raises(ValueError):
         api.BlkCaches(shape(api, block=8), [dict(K=z(1), V=z(1), Ks=z(1), Vs=z(1))])
+
+
+def test_without_the_compiled_calls(api, monkeypatch):
+    """_bind.so is a quicker way to make some calls: a program runs without it, and is told why it is slower."""
+    import sys
+    import paper_2411_18077_amd as package
+    api.lib()
+    monkeypatch.setitem(sys.modules, "paper_2411_18077_amd._bind", None)
+    monkeypatch.delattr(package, "_bind", raising=False)
+    monkeypatch.setattr(api, "_lib", None)
+    monkeypatch.setattr(api, "_bind", None)
+    with pytest.warns(RuntimeWarning, match="_bind"):
+        assert api.lib() is api.lib()
+    assert not api._quick(0)
+    assert api.kv_free_workspace_bytes(shape(api)) > 0
+    with pytest.raises(ValueError):
+        api.kv_fork_blk(shape(api), z(4), z(4), z(4), z(4, 6), z(40), z(2), z(4), z(4, 6), z(2), z(4), z(3))
+
+
+def test_a_build_without_a_compiler_for_the_compiled_calls(monkeypatch, tmp_path):
+    """The library is there before the build says that _bind.so is not."""
+    from paper_2411_18077_amd import build
+    monkeypatch.setattr(build, "OBJ", str(tmp_path))
+    monkeypatch.setattr(build, "LIB", str(tmp_path / "libminikv.so"))
+    monkeypatch.setattr(build, "BIND", str(tmp_path / "_bind.so"))
+    monkeypatch.setattr(build, "SOURCES", ["scalar.hip"])
+    monkeypatch.setattr(build, "_compile", lambda src: (str(empty), ""))
+
+    def fails():
+        raise RuntimeError("g++ failed for bind.cpp")
+    monkeypatch.setattr(build, "_compile_bind", fails)
+    empty = tmp_path / "empty.o"
+    import subprocess
+    subprocess.run(["gcc", "-x", "c", "-fPIC", "-c", "/dev/null", "-o", str(empty)], check=True)
+    with pytest.raises(RuntimeError, match="bind.cpp"):
+        build.build(verbose=False)
+    assert (tmp_path / "libminikv.so").exists()
+
+
+def test_compiled_calls_for_another_torch_are_not_used(api, monkeypatch):
+    from paper_2411_18077_amd import build
+    assert api._compiled() is not None
+    monkeypatch.setattr(build, "bound_to", lambda: "torch 1.0, Python 2.7")
+    with pytest.warns(RuntimeWarning, match="built for torch"):
+        assert api._compiled() is None
