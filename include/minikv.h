@@ -368,7 +368,7 @@ int minikv_prompt_attn_blk(const minikv_blk_shape *shape, int32_t T, const void 
  *   y = x * w / sqrt(mean(x^2) + eps), y = x where the weights are NULL;
  *   pair i < rot_dim / 2 of y, channels i and rot_dim/2 + i, or 2i and 2i+1 if `adjacent`: (u, v) becomes
  *   (u cos a - v sin a, v cos a + u sin a), a = p * inv_freq[i]; channels from rot_dim on stay.
- * In binary32 (the angle is right to 2^-20 of a radian whatever the position), rounded once.  A token with pos[t] < 0 (padding) is left alone.
+ * In binary32 (an angle up to 2^31, that is any position where |inv_freq| <= 1, is right to 2^-20 of a radian; beyond that its error grows with it), rounded once.  A token with pos[t] < 0 (padding) is left alone.
  *   Q, K    fp16 / bf16 [T][Hq or Hkv][128], tokens q_stride, k_stride elements apart              (device, read)
  *   w_q, w_k   fp16 / bf16 [128], or NULL                                        (device, read)
  *   inv_freq   fp32 [rot_dim / 2], finite, or NULL if rot_dim == 0               (device, read)

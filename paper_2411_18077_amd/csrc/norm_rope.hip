@@ -7,8 +7,9 @@
 // channels i and rot/2 + i, the other half of a pair comes from another lane as the two bytes it was loaded as (the row's norm is
 // the same there, the weight is a register).  All in binary32, rounded once at the end.
 //
-// Angles.  A far position times a frequency has more bits than binary32: pos * inv_freq / (2 pi) is formed in binary64, whole turns are dropped
-// there, and what is left of a turn, within 2^-24 of it, goes on in binary32.  Sine and cosine of the eighth of a turn around the nearest
+// Angles.  A far position times a frequency has more bits than binary32: pos * inv_freq / (2 pi) is formed in binary64 and whole turns are dropped
+// there.  For angles up to 2^31 the product's rounding and that of 1 / (2 pi) leave 2^-21.3 of a radian, and what is left of a turn goes on in binary32,
+// rounded to 2^-26 of a turn.  Sine and cosine of the eighth of a turn around the nearest
 // quarter are their Taylor sums up to x^9 and x^8 (the next terms are below 2^-28 and 2^-25 at pi/4); quarters swap and negate them.  A token's
 // angles are formed once per wave, which takes several heads.
 //
@@ -56,8 +57,9 @@ template <int CTRL> __device__ inline float add_ror(float v)
 
 __device__ inline void turn(int pos, float freq, float &c, float &s)
 {
-    const double turns = (double)pos * (double)freq * 0.15915494309189533577;
-    const float part = (float)(turns - __builtin_rint(turns));           // [-1/2, 1/2]
+    constexpr double kTurn = 0.15915494309189533577;
+    const double angle = (double)pos * (double)freq;
+    const float part = (float)__builtin_fma(angle, kTurn, -__builtin_rint(angle * kTurn));              // [-1/2, 1/2]
     const float quarter = __builtin_rintf(4.0f * part), x = __builtin_fmaf(-0.25f, quarter, part) * 6.28318530717958647692f, z = x * x;
     const float sn = x * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), 1.0f);
     const float cs = __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 1.0f / 40320, -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);

@@ -1,4 +1,7 @@
 """minikv_norm_rope against its definition in 64 bits."""
+import math
+from fractions import Fraction
+
 import pytest
 import torch
 
@@ -141,3 +144,31 @@ def test_many_tokens():
     for got, h in ((q, 0), (k, 1)):
         want, size = pages.norm_rope(src[:, h:h + 1], None, 0.0, inv, 128, False, pos)
         assert ((got.cpu().double() - want).abs() <= tolerance(want, size, BF16)).all()
+
+
+def exact_turn(pos, freq):
+    """cos and sin of pos * freq, the whole turns dropped in rational numbers."""
+    two_pi = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459")
+    a = Fraction(pos) * Fraction(freq)
+    a -= two_pi * round(a / two_pi)
+    return math.cos(a), math.sin(a)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("top", [1.0, 1000.0, 2.0 ** 20, 2.0 ** 24])
+def test_angles_of_any_frequency(top, adjacent):
+    """Angles up to 2^31 radians are right to 2^-20: pairs (1, 0) become (cos, sin)."""
+    most = int((2 ** 31 - 1) / top)
+    pos = [max(most - 2 * i, 0) for i in range(6)] + [most // 175, 1, 0]
+    inv = [(-1) ** i * top * (1 - i / 1024.1) for i in range(64)]
+    inv = torch.tensor(inv, dtype=torch.float32)
+    q = torch.zeros(len(pos), 1, 128, dtype=BF16)
+    u, v = (slice(0, None, 2), slice(1, None, 2)) if adjacent else (slice(0, 64), slice(64, None))
+    q[:, :, u] = 1.0
+    out, ko = torch.zeros_like(q).cuda(), torch.zeros_like(q).cuda()
+    api.minikv_norm_rope(1, 1, len(pos), q.cuda(), q.cuda(), None, None, 0.0, inv.cuda(), 128, adjacent, torch.tensor(pos, dtype=torch.int32).cuda(), out, ko)
+    got = out.cpu().double()[:, 0]
+    want = torch.tensor([[exact_turn(p, float(f)) for f in inv] for p in pos], dtype=torch.float64)
+    for k, part in enumerate((u, v)):
+        off = (got[:, part] - want[:, :, k]).abs()
+        assert (off <= want[:, :, k].abs() * HALF[BF16] + 2.0 ** -19).all(), float(off.max())
