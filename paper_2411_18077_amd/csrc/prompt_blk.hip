@@ -17,7 +17,6 @@
 // workgroup of each eight to arrive, the results of eight of those by the last of them, and so on, always summed in the parts' order.
 #include "decode_common.h"
 #include "attn_tile.h"
-#include "scan.h"
 
 #include <type_traits>
 
@@ -80,7 +79,8 @@ __device__ inline float2 pb_pair(uint64_t v) { return float2{__uint_as_float((ui
 // The requests' rows in blocks, each block's walk in cost / share parts, share = ceil(all blocks' cost / slots) (of workgroups at once): rounded up
 // if the items of more than half a share are then not more than slots, so that they run at once and the others fill what is left, else
 // down.  (Always up, 16 x 8 tokens behind 16384 have 568 parts for 512 slots: 123 us instead of 100; always down, a step of 24 uneven
-// requests 59 us instead of 49.)  Blocks in two or more parts, 2 * slots at most, come first, then those in one, long ones first;
+// requests 59 us instead of 49.)  Blocks in two or more parts, slots of these at most (rounded down, a part has at least a share; rounded up, more than half
+// of one, and those were counted), come first, then those in one, long ones first;
 // of a request the narrow blocks, then the wide ones from the last on, whose walks are the longest.  Every workgroup counts all that for itself.
 template <int CTRL, int ROWS> __device__ inline uint64_t add_dpp64(uint64_t v)
 {
@@ -775,7 +775,7 @@ static int part_rows(const minikv_blk_shape &s, int32_t T)
     return (int)(rows < kPbRows ? rows : kPbRows);
 }
 
-// [tickets][(m, l) of the parts' rows][their outputs]
+// [tickets][(m, l) of the parts' rows][their outputs], for twice as many parts as there can be
 size_t prompt_blk_workspace_bytes(const minikv_blk_shape &s, int32_t T)
 {
     return (size_t)2 * kPbSlots * (3 * sizeof(int) + (size_t)part_rows(s, T) * (2 + kD) * sizeof(float));
