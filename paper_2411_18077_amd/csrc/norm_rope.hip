@@ -13,7 +13,7 @@
 // quarter are their Taylor sums up to x^9 and x^8 (the next terms are below 2^-28 and 2^-25 at pi/4); quarters swap and negate them.  A token's
 // angles are formed once per wave, which takes several heads.
 //
-// What bounds it: memory (32768 tokens of 40 heads 122 us, 5.5 TB/s), for few tokens two dependent round trips (64 of 40 heads 3.2 us, one 3.0).
+// What bounds it: memory (32768 tokens of 40 heads 122 us, 5.5 TB/s), for few tokens two dependent round trips (64 of 40 heads 3.7 us).
 #include "decode_common.h"
 
 namespace minikv {
