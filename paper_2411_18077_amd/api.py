@@ -167,9 +167,10 @@ def _compiled():
     from .build import bound_to
     try:
         from . import _bind as bind
-        if bind.built_for == bound_to():
+        what = getattr(bind, "built_for", "something that it does not name")
+        if what == bound_to():
             return bind
-        why = "it is built for %s" % bind.built_for
+        why = "it is built for %s" % what
     except ImportError as e:
         why = str(e)
     warnings.warn("the compiled calls of _bind.so are not in use, some calls take longer (`python -m paper_2411_18077_amd.build` makes it for %s): %s"

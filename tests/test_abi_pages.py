@@ -248,3 +248,11 @@ def test_compiled_calls_for_another_torch_are_not_used(api, monkeypatch):
     monkeypatch.setattr(build, "bound_to", lambda: "torch 1.0, Python 2.7")
     with pytest.warns(RuntimeWarning, match="built for torch"):
         assert api._compiled() is None
+
+
+def test_compiled_calls_that_do_not_say_what_they_are_for_are_not_used(api, monkeypatch):
+    import types
+    import paper_2411_18077_amd as package
+    monkeypatch.setattr(package, "_bind", types.ModuleType("_bind"), raising=False)
+    with pytest.warns(RuntimeWarning, match="_bind"):
+        assert api._compiled() is None
